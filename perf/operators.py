@@ -1,0 +1,467 @@
+"""The operators on a language model's logits and their cases: log-probabilities of given tokens, distillation from a
+teacher's top logits, the clipped policy loss, and the preference loss, each in its plain form and as the framework's call.
+
+Write z for the logits of one position (a row), s = 1/temperature, u = s z, lse = log sum_j exp(u_j), p_j = exp(u_j - lse).
+  logprob     logp = u_y - lse of the label y, and the entropy H = lse - sum_j p_j u_j.  A negative label is ignored: zeros.
+  distill     q = softmax of the teacher's scaled top logits; loss = sum_k q_k (log q_k - log p_k); or, with the teacher's own
+              log-sum-exp, q_k = exp(s a_k - lse_t) and one more outcome for the rest of the vocabulary on both sides.
+  policy      x = logp - old, r = exp(x): loss = -min(r A, clip(r) A) + c_kl KL(logp, ref) - c_H H.
+  preference  delta = beta ((sum of logp - ref over the chosen answer) - (the same over the rejected one)); loss of delta.
+Every loss is scale * sum of weight * (loss of a row or pair), and comes with its gradient with respect to the logits."""
+import math
+
+import torch
+
+own = False
+DEV = "cuda"
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+SIZE = {"f32": 4, "bf16": 2, "f16": 2}
+
+
+def listed():
+    return [
+        # scoring the next token of a few running requests: the length of one call
+        dict(name="logprob_decode", op="logprob", dtype="bf16", rows=8, vocab=32768, entropy=True, ignored=0.0, padded=0, temperature=0.8),
+        # reference log-probabilities of a batch of answers, a vocabulary that no power of two divides
+        dict(name="logprob_ragged", op="logprob", dtype="f16", rows=3001, vocab=50021, entropy=False, ignored=0.2, padded=0, temperature=1.0),
+        # the same over a long batch: more than 2^31 logits, the vocabulary's last entries are padding
+        dict(name="logprob_long", op="logprob", dtype="bf16", rows=16400, vocab=131072, entropy=True, ignored=0.0, padded=72, temperature=1.0),
+        # a student's last few positions in 32 bits
+        dict(name="distill_small", op="distill", dtype="f32", rows=16, vocab=32768, top=8, rest=False, index="i64", short=0.0, temperature=2.0),
+        # an ordinary step of distillation: one sequence batch, 64 logits kept for each position
+        dict(name="distill_step", op="distill", dtype="bf16", rows=4096, vocab=65536, top=64, rest=False, index="i32", short=0.0, temperature=1.0),
+        # odd sizes, rows with fewer teacher entries than the others, the rest of the teacher's mass kept
+        dict(name="distill_rest", op="distill", dtype="f32", rows=1001, vocab=100003, top=100, rest=True, index="i64", short=0.3, temperature=1.0),
+        # one short rollout
+        dict(name="policy_small", op="policy", dtype="bf16", rows=32, vocab=32768, kl="k3", entropy=False, mean="token", ignored=0.0, temperature=1.0),
+        # rollouts of different lengths, a mean for each, with the entropy's bonus and a 16-bit loss scale
+        dict(name="policy_step", op="policy", dtype="f16", rows=4099, vocab=50021, kl="k3", entropy=True, mean="sequence", ignored=0.25, temperature=1.0),
+        # a large batch of rollouts
+        dict(name="policy_large", op="policy", dtype="bf16", rows=8192, vocab=131072, kl="k3", entropy=False, mean="token", ignored=0.0, temperature=1.0),
+        # two pairs of short answers in 32 bits
+        dict(name="preference_small", op="preference", dtype="f32", rows=96, vocab=32768, pairs=2, loss="sigmoid", normalised=False, ignored=0.0),
+        # an ordinary batch of pairs, prompts left out of the loss
+        dict(name="preference_step", op="preference", dtype="bf16", rows=4501, vocab=65536, pairs=16, loss="sigmoid", normalised=False, ignored=0.3),
+        # a large one, lengths taken out
+        dict(name="preference_large", op="preference", dtype="bf16", rows=8192, vocab=131072, pairs=24, loss="ipo", normalised=True, ignored=0.0),
+    ]
+
+
+def draw(rng):
+    op = rng.choice(("logprob", "distill", "policy", "preference"))
+    dtype = rng.choice(("f32", "bf16", "f16"))
+    vocab = int(math.exp(rng.uniform(math.log(1000), math.log(140000))))
+    most = 4.2e9 / (SIZE[dtype] * vocab * (1 if op == "logprob" else 2))      # the largest listed cases move 4.3e9 bytes
+    least = 64 if op == "preference" else 1
+    rows = int(math.exp(rng.uniform(math.log(least), math.log(max(least + 1, min(16400, most))))))
+    case = dict(op=op, dtype=dtype, rows=rows, vocab=vocab)
+    if op == "logprob":
+        case.update(entropy=rng.random() < 0.5, ignored=rng.choice((0.0, 0.2)), padded=rng.choice((0, 40)), temperature=rng.choice((0.7, 1.0)))
+    elif op == "distill":
+        case.update(top=int(math.exp(rng.uniform(0, math.log(257)))), rest=rng.random() < 0.5, index=rng.choice(("i32", "i64")),
+                    short=rng.choice((0.0, 0.3)), temperature=rng.choice((1.0, 2.0)))
+    elif op == "policy":
+        case.update(kl=rng.choice(("none", "k1", "k2", "k3")), entropy=rng.random() < 0.5, mean=rng.choice(("token", "sequence")),
+                    ignored=rng.choice((0.0, 0.25)), temperature=rng.choice((0.7, 1.0)))
+    else:
+        case.update(pairs=max(1, min(64, rows // 32)), loss=rng.choice(("sigmoid", "hinge", "ipo")), normalised=rng.random() < 0.5,
+                    ignored=rng.choice((0.0, 0.3)))
+    return case
+
+
+def _read_rows(case):
+    """Rows whose logits count: a token whose label is ignored needs none of them."""
+    return case["rows"] - int(case.get("ignored", 0.0) * case["rows"])
+
+
+def work(case):
+    rows, vocab, b = case["rows"], case["vocab"], SIZE[case["dtype"]]
+    read = _read_rows(case)
+    bytes_ = read * vocab * b
+    flops = 4 * read * vocab                                         # scale, maximum, exponential, sum
+    if case["op"] == "logprob":
+        return {"bytes": bytes_ + rows * (8 + 8 + 4 * case["entropy"]), "flops": flops + 2 * read * vocab * case["entropy"]}
+    bytes_ += rows * vocab * b                                       # the gradient is written whole
+    flops += 4 * read * vocab
+    if case["op"] == "distill":
+        bytes_ += rows * (case["top"] * (4 + (4 if case["index"] == "i32" else 8)) + 4 + 4)
+    elif case["op"] == "policy":
+        bytes_ += rows * (8 + 5 * 4 + 2 * 4)
+    else:
+        bytes_ += rows * (8 + 4 + 4) + 24 * case["pairs"]
+    return {"bytes": bytes_, "flops": flops}
+
+
+# ---- inputs ---------------------------------------------------------------------------------------------------------------
+
+
+def _logits(case, gen):
+    """Logits as a model gives them: most of the mass on a few dozen entries, the rest spread wide."""
+    rows, vocab = case["rows"], case["vocab"]
+    z = torch.empty(rows, vocab, dtype=TYPES[case["dtype"]], device=DEV)
+    for a in range(0, rows, 2048):                                   # (in pieces: the numbers are drawn in 32 bits)
+        part = torch.randn(min(2048, rows - a), vocab, device=DEV, generator=gen)
+        z[a:a + 2048] = part.mul_(2.2)
+    return z
+
+
+def _labels(case, z, gen):
+    """A label for each row, likely under its logits; `ignored` of them, somewhere, are -100."""
+    rows, vocab = z.shape
+    seen = vocab - case.get("padded", 0)
+    y = torch.randint(0, seen, (rows,), device=DEV, generator=gen)
+    z[torch.arange(rows, device=DEV), y] = (math.log(vocab) + 1.5 + 1.5 * torch.randn(rows, device=DEV, generator=gen)).to(z.dtype)
+    if case.get("padded"):
+        z[:, seen:] = -math.inf
+    out = torch.randperm(rows, device=DEV, generator=gen)[: rows - _read_rows(case)]
+    y[out] = -100
+    return y
+
+
+def _logp_of(z, y, s):
+    """log-probabilities of the labels, in pieces (for inputs that stand near them)"""
+    got = []
+    for a in range(0, z.shape[0], 1024):
+        u = z[a:a + 1024].float() * s
+        got.append(u.gather(1, y[a:a + 1024].clamp(min=0)[:, None])[:, 0] - torch.logsumexp(u, 1))
+    return torch.cat(got)
+
+
+def _lengths(count, total, gen):
+    """`count` positive lengths of different size that add up to `total`"""
+    share = torch.rand(count, device=DEV, generator=gen) + 0.2
+    ends = (torch.cumsum(share, 0) / share.sum() * (total - count)).round().long() + torch.arange(1, count + 1, device=DEV)
+    ends[-1] = total
+    return torch.cat([torch.zeros(1, dtype=torch.long, device=DEV), ends])
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(seed)
+    rows, vocab = case["rows"], case["vocab"]
+    st = dict(case=case, z=_logits(case, gen))
+
+    def randn(*shape):
+        return torch.randn(*shape, device=DEV, generator=gen)
+
+    if case["op"] == "distill":
+        top = case["top"]
+        stride = torch.randint(1, max(2, vocab // top), (rows, 1), device=DEV, generator=gen)   # (so that no index comes twice)
+        first = torch.randint(0, vocab, (rows, 1), device=DEV, generator=gen)
+        index = (first + stride * torch.arange(top, device=DEV)) % vocab
+        a = torch.sort(math.log(vocab) + 2.0 * randn(rows, top), dim=1, descending=True).values
+        st["z"].scatter_(1, index, (a + 0.7 * randn(rows, top)).to(st["z"].dtype))              # a student on its way to the teacher
+        if case["short"]:                                            # some rows end early: padding, whatever its logits
+            few = torch.randint(1, top + 1, (rows, 1), device=DEV, generator=gen)
+            few = torch.where(torch.rand(rows, 1, device=DEV, generator=gen) < case["short"], few, top)
+            gone = torch.arange(top, device=DEV) >= few
+            index = torch.where(gone, -1, index)
+        st["index"] = index.to(torch.int32 if case["index"] == "i32" else torch.int64)
+        st["a"] = a
+        st["lse_t"] = None
+        if case["rest"]:
+            scaled = (a / case["temperature"]).masked_fill(index < 0, -math.inf)
+            st["lse_t"] = torch.logsumexp(scaled, 1) + 0.05 + 0.2 * torch.rand(rows, device=DEV, generator=gen)
+        st["weight"] = torch.full((rows,), 1.0 / rows, device=DEV) * (0.5 + torch.rand(rows, device=DEV, generator=gen))
+        st["scale"] = 1024.0 if case["dtype"] == "f16" else 1.0
+        return st
+    st["y"] = _labels(case, st["z"], gen)
+    if case["op"] == "logprob":
+        return st
+    st["scale"] = 1.0 if case["dtype"] != "f16" else 65536.0 if case["op"] == "policy" else 256.0   # 16-bit gradients need a loss scale
+    if case["op"] == "policy":
+        logp = _logp_of(st["z"], st["y"], 1.0 / case["temperature"])
+        x = 0.15 * randn(rows)
+        for edge in (math.log(1.2), math.log(0.8)):                  # a token on the very edge of the range has either gradient: none is
+            x = torch.where((x - edge).abs() < 1e-3, edge + 3e-3, x)
+        st["old"] = logp - x
+        st["ref"] = logp - 0.3 * randn(rows) if case["kl"] != "none" else None
+        st["adv"] = 0.5 + randn(rows)
+        kept = (st["y"] >= 0).float()
+        if case["mean"] == "token":
+            st["weight"] = kept / kept.sum().clamp(min=1)
+        else:
+            count = max(1, min(64, rows // 64))
+            off = _lengths(count, rows, gen)
+            seq = torch.searchsorted(off[1:], torch.arange(rows, device=DEV), right=True)
+            n = torch.zeros(count, device=DEV).index_add_(0, seq, kept).clamp(min=1)
+            st["weight"] = kept / (n[seq] * count)
+        return st
+    st["off"] = _lengths(2 * case["pairs"], rows, gen)               # the chosen answers, then the rejected ones
+    st["ref"] = _logp_of(st["z"], st["y"], 1.0) + 0.2 * randn(rows)
+    st["mask"] = st["y"] >= 0
+    st["weight"] = torch.full((case["pairs"],), 1.0 / case["pairs"], device=DEV)
+    st["beta"] = 0.1
+    return st
+
+
+CLIP_LOW, CLIP_HIGH, KL_COEF, ENTROPY_COEF = 0.2, 0.2, 0.05, 0.01
+
+
+# ---- one pass -------------------------------------------------------------------------------------------------------------
+
+
+def run(st):
+    case = st["case"]
+    return _framework(st, case) if own else PLAIN[case["op"]](st, case)
+
+
+def _framework(st, case):
+    import paper_2203_16340_amd as L
+    if case["op"] == "logprob":
+        r = L.token_logprob(st["z"], st["y"], temperature=case["temperature"], entropy=case["entropy"])
+        return {"logp": r.logp, "lse": r.lse, "entropy": r.entropy}
+    if case["op"] == "distill":
+        r = L.distill_loss(st["z"], st["index"], st["a"], teacher_lse=st["lse_t"], temperature=case["temperature"],
+                           weight=st["weight"], scale=st["scale"])
+        return {"loss": r.loss, "row_loss": r.row_loss, "grad": r.grad}
+    if case["op"] == "policy":
+        r = L.policy_loss(st["z"], st["y"], st["old"], st["adv"], ref_logp=st["ref"], weight=st["weight"], clip_low=CLIP_LOW,
+                          clip_high=CLIP_HIGH, kl_coef=0.0 if case["kl"] == "none" else KL_COEF,
+                          kl_kind="k3" if case["kl"] == "none" else case["kl"], entropy_coef=ENTROPY_COEF if case["entropy"] else 0.0,
+                          temperature=case["temperature"], scale=st["scale"])
+        return {"loss": r.loss, "row_loss": r.row_loss, "logp": r.logp, "grad": r.grad}
+    t = L.token_logprob(st["z"], st["y"])
+    r = L.preference_loss(t.logp, st["ref"], st["off"], mask=st["mask"], weight=st["weight"], beta=st["beta"], kind=case["loss"],
+                          length_normalised=case["normalised"], label_smoothing=0.1 if case["loss"] == "sigmoid" else 0.0,
+                          scale=st["scale"])
+    grad = L.token_logprob_grad(st["z"], st["y"], t.lse, r.grad)
+    return {"loss": r.loss, "pair_loss": r.pair_loss, "rewards": r.rewards, "logp": t.logp, "grad": grad}
+
+
+def _softmax_parts(z, s):
+    """u, lse and p of every row, in 32 bits"""
+    u = z.float() * s
+    top = u.amax(1, keepdim=True)
+    e = torch.exp(u - top)
+    total = e.sum(1, keepdim=True)
+    return u, (top + torch.log(total))[:, 0], e / total
+
+
+def _label_logit(u, y):
+    return u.gather(1, y.clamp(min=0)[:, None])[:, 0]
+
+
+def _entropy(u, lse, p):
+    return lse - torch.where(p > 0, p * u, 0.0).sum(1)
+
+
+def _add_at_label(grad, y, g):
+    return grad.scatter_add_(1, y.clamp(min=0)[:, None], g[:, None])
+
+
+def _plain_logprob(st, case):
+    z, y = st["z"], st["y"]
+    u, lse, p = _softmax_parts(z, 1.0 / case["temperature"])
+    kept = y >= 0
+    return {"logp": torch.where(kept, _label_logit(u, y) - lse, 0.0), "lse": torch.where(kept, lse, 0.0),
+            "entropy": torch.where(kept, _entropy(u, lse, p), 0.0) if case["entropy"] else None}
+
+
+def _plain_distill(st, case):
+    s = 1.0 / case["temperature"]
+    u, lse, p = _softmax_parts(st["z"], s)
+    index = st["index"].long()
+    some = index >= 0
+    at = index.clamp(min=0)
+    a = (st["a"] * s).masked_fill(~some, -math.inf)
+    logq = a - (torch.logsumexp(a, 1) if st["lse_t"] is None else st["lse_t"])[:, None]
+    q = torch.exp(logq)
+    logp = u.gather(1, at) - lse[:, None]
+    row = torch.where(some, q * (logq - logp), 0.0).sum(1)
+    w = (st["weight"] * (st["scale"] * s))[:, None]
+    if st["lse_t"] is None:
+        grad = (w * p).scatter_add_(1, at, -w * torch.where(some, q, 0.0))
+    else:
+        rest_t = (1.0 - q.sum(1)).clamp(min=0)
+        in_top = torch.zeros_like(u).scatter_add_(1, at, some.float()) > 0
+        rest = torch.where(in_top, 0.0, p).sum(1)
+        row = row + torch.where(rest_t > 0, rest_t * (torch.log(rest_t) - torch.log(rest)), 0.0)
+        grad = torch.where(in_top, p, p * (1.0 - rest_t / rest)[:, None]) * w
+        grad = grad.scatter_add_(1, at, -w * torch.where(some, q, 0.0))
+    return {"loss": (st["weight"] * row).sum() * st["scale"], "row_loss": row, "grad": grad.to(st["z"].dtype)}
+
+
+def _plain_policy(st, case):
+    s, y, w = 1.0 / case["temperature"], st["y"], st["weight"]
+    u, lse, p = _softmax_parts(st["z"], s)
+    kept = (y >= 0) & (w != 0)
+    logp = torch.where(kept, _label_logit(u, y) - lse, 0.0)
+    r = torch.exp(logp - st["old"])
+    free, held = r * st["adv"], r.clamp(1 - CLIP_LOW, 1 + CLIP_HIGH) * st["adv"]
+    row = -torch.minimum(free, held)
+    g = torch.where(free <= held, -free, 0.0)
+    if case["kl"] != "none":
+        d = logp - st["ref"]
+        row = row + KL_COEF * {"k1": d, "k2": 0.5 * d * d, "k3": torch.expm1(-d) + d}[case["kl"]]
+        g = g + KL_COEF * {"k1": torch.ones_like(d), "k2": d, "k3": -torch.expm1(-d)}[case["kl"]]
+    w = torch.where(kept, w, 0.0)
+    g = g * w * (st["scale"] * s)
+    grad = _add_at_label(-g[:, None] * p, y, g)
+    if case["entropy"]:
+        h = _entropy(u, lse, p)
+        row = row - ENTROPY_COEF * h
+        more = p * (u - lse[:, None] + h[:, None]) * (w * (st["scale"] * s * ENTROPY_COEF))[:, None]
+        grad = grad + torch.where(p > 0, more, 0.0)
+    row = torch.where(kept, row, 0.0)
+    return {"loss": (w * row).sum() * st["scale"], "row_loss": row, "logp": logp, "grad": grad.to(st["z"].dtype)}
+
+
+def _pair_loss(kind, delta, beta, smoothing):
+    """The loss of a pair and its derivative with respect to delta."""
+    if kind == "sigmoid":
+        soft = torch.log1p(torch.exp(-delta.abs())) + (-delta).clamp(min=0)      # -log sigmoid(delta)
+        return soft + smoothing * delta, torch.sigmoid(delta) - (1.0 - smoothing)
+    if kind == "hinge":
+        return (1 - delta).clamp(min=0), -(delta < 1).to(delta.dtype)
+    return ((delta - 0.5) / beta) ** 2, 2 * (delta - 0.5) / beta ** 2
+
+
+def _plain_preference(st, case):
+    y, pairs = st["y"], case["pairs"]
+    u, lse, p = _softmax_parts(st["z"], 1.0)
+    logp = torch.where(y >= 0, _label_logit(u, y) - lse, 0.0)
+    t = torch.arange(case["rows"], device=DEV)
+    of = (t >= st["off"][:-1, None]) & (t < st["off"][1:, None]) & st["mask"]    # which tokens each answer has
+    total = torch.where(of, logp - st["ref"], 0.0).sum(1)
+    n = of.sum(1).clamp(min=1).float() if case["normalised"] else torch.ones_like(total)
+    reward = st["beta"] * total / n
+    loss, slope = _pair_loss(case["loss"], reward[:pairs] - reward[pairs:], st["beta"], 0.1 if case["loss"] == "sigmoid" else 0.0)
+    c = slope * st["weight"] * (st["scale"] * st["beta"])
+    g = (of * (torch.cat([c, -c]) / n)[:, None]).sum(0)
+    g = torch.where(y >= 0, g, 0.0)
+    grad = _add_at_label(-g[:, None] * p, y, g)
+    return {"loss": (st["weight"] * loss).sum() * st["scale"], "pair_loss": loss, "rewards": reward, "logp": logp,
+            "grad": grad.to(st["z"].dtype)}
+
+
+PLAIN = {"logprob": _plain_logprob, "distill": _plain_distill, "policy": _plain_policy, "preference": _plain_preference}
+
+
+# ---- the definitions in 64 bits, row by row in pieces -------------------------------------------------------------------------
+
+
+def exact(case, seed):
+    st = prepare(case, seed)
+    return {"logprob": _exact_logprob, "distill": _exact_distill, "policy": _exact_policy, "preference": _exact_preference}[case["op"]](st, case)
+
+
+def _pieces(st, s):
+    for a in range(0, st["z"].shape[0], 512):
+        rows = slice(a, min(a + 512, st["z"].shape[0]))
+        yield rows, torch.log_softmax(st["z"][rows].double() * s, 1)
+
+
+def _join(parts):
+    return {k: None if parts[0][k] is None else torch.cat([p[k] for p in parts]) for k in parts[0]}
+
+
+def _pick(lp, y):
+    """log-probability at each label, zero where it is ignored"""
+    at = torch.arange(len(y), device=DEV)
+    return torch.where(y < 0, 0.0, lp[at, torch.where(y < 0, 0, y)])
+
+
+def _neg_entropy(lp):
+    return torch.xlogy(lp.exp(), lp.exp()).sum(1)
+
+
+def _exact_logprob(st, case):
+    s = 1.0 / case["temperature"]
+    parts = []
+    for rows, lp in _pieces(st, s):
+        y = st["y"][rows]
+        lse = torch.logsumexp(st["z"][rows].double() * s, 1)
+        parts.append({"logp": _pick(lp, y), "lse": torch.where(y < 0, 0.0, lse),
+                      "entropy": torch.where(y < 0, 0.0, -_neg_entropy(lp)) if case["entropy"] else None})
+    return _join(parts)
+
+
+def _exact_distill(st, case):
+    s = 1.0 / case["temperature"]
+    parts = []
+    for rows, lp in _pieces(st, s):
+        n = lp.shape[0]
+        index, a = st["index"][rows].long(), st["a"][rows].double() * s
+        spread = torch.zeros(n, case["vocab"] + 1, dtype=torch.float64, device=DEV)       # the teacher over the vocabulary; padding past its end
+        a = torch.where(index < 0, -math.inf, a)
+        norm = torch.logsumexp(a, 1) if st["lse_t"] is None else st["lse_t"][rows].double()
+        spread.scatter_(1, torch.where(index < 0, case["vocab"], index), torch.exp(a - norm[:, None]))
+        spread[:, case["vocab"]] = 0
+        q = spread[:, :-1]
+        member = q > 0
+        row = torch.where(member, torch.xlogy(q, q) - q * lp, 0.0).sum(1)
+        d = lp.exp() - q
+        if st["lse_t"] is not None:
+            r = (1 - q.sum(1)).clamp(min=0)
+            tail = torch.logsumexp(torch.where(member, -math.inf, lp), 1)
+            row = row + torch.xlogy(r, r) - r * tail
+            d = torch.where(member, d, lp.exp() - r[:, None] * torch.exp(lp - tail[:, None]))
+        parts.append({"row_loss": row, "grad": d * (st["weight"][rows].double() * st["scale"] * s)[:, None]})
+    got = _join(parts)
+    return {"loss": (got["row_loss"] * st["weight"].double()).sum() * st["scale"], **got}
+
+
+def _exact_policy(st, case):
+    s = 1.0 / case["temperature"]
+    parts = []
+    for rows, lp in _pieces(st, s):
+        y, w, adv = st["y"][rows], st["weight"][rows].double(), st["adv"][rows].double()
+        w = torch.where(y < 0, 0.0, w)
+        live = w != 0
+        logp = torch.where(live, _pick(lp, y), 0.0)
+        r = torch.exp(logp - st["old"][rows].double())
+        clipped = ((adv > 0) & (r > 1 + CLIP_HIGH)) | ((adv < 0) & (r < 1 - CLIP_LOW))
+        row = -adv * torch.where(clipped, torch.where(adv > 0, 1.0 + CLIP_HIGH, 1.0 - CLIP_LOW).double(), r)
+        g = torch.where(clipped, 0.0, -adv * r)
+        if case["kl"] != "none":
+            d = st["ref"][rows].double() - logp
+            if case["kl"] == "k1":
+                row, g = row - KL_COEF * d, g + KL_COEF
+            elif case["kl"] == "k2":
+                row, g = row + KL_COEF * d * d / 2, g - KL_COEF * d
+            else:
+                row, g = row + KL_COEF * (d.exp() - 1 - d), g + KL_COEF * (1 - d.exp())
+        p = lp.exp()
+        grad = -p * g[:, None]
+        grad[torch.arange(len(y), device=DEV), torch.where(y < 0, 0, y)] += g
+        if case["entropy"]:
+            minus_h = _neg_entropy(lp)
+            row = row + ENTROPY_COEF * minus_h
+            grad = grad + ENTROPY_COEF * (torch.xlogy(p, p) - p * minus_h[:, None])
+        grad = torch.where(live[:, None], grad * (w * (st["scale"] * s))[:, None], 0.0)
+        parts.append({"row_loss": torch.where(live, row, 0.0), "logp": logp, "grad": grad})
+    got = _join(parts)
+    return {"loss": (got["row_loss"] * st["weight"].double()).sum() * st["scale"], **got}
+
+
+def _exact_preference(st, case):
+    logp = torch.cat([_pick(lp, st["y"][rows]) for rows, lp in _pieces(st, 1.0)])
+    pairs, beta = case["pairs"], st["beta"]
+    off = st["off"].tolist()
+    reward, share = [], torch.zeros(case["rows"], dtype=torch.float64, device=DEV)
+    for k in range(2 * pairs):
+        span = slice(off[k], off[k + 1])
+        m = st["mask"][span].double()
+        n = m.sum().clamp(min=1) if case["normalised"] else 1.0
+        reward.append(beta * (m * (logp[span] - st["ref"][span].double())).sum() / n)
+        share[span] = m / n * (1.0 if k < pairs else -1.0) * beta
+    reward = torch.stack(reward)
+    delta = (reward[:pairs] - reward[pairs:]).clone().requires_grad_()
+    if case["loss"] == "sigmoid":
+        loss = -0.9 * torch.nn.functional.logsigmoid(delta) - 0.1 * torch.nn.functional.logsigmoid(-delta)
+    elif case["loss"] == "hinge":
+        loss = torch.relu(1 - delta)
+    else:
+        loss = (delta / beta - 1 / (2 * beta)) ** 2
+    slope = torch.autograd.grad(loss.sum(), delta)[0]
+    w = st["weight"].double()
+    seq = torch.searchsorted(st["off"][1:], torch.arange(case["rows"], device=DEV), right=True)
+    g = share * (slope * w * st["scale"])[seq % pairs]
+    g = torch.where(st["y"] < 0, 0.0, g)
+    grad = torch.empty(case["rows"], case["vocab"], dtype=torch.float64, device=DEV)
+    for rows, lp in _pieces(st, 1.0):
+        y = st["y"][rows]
+        grad[rows] = -g[rows, None] * lp.exp()
+        grad[rows][torch.arange(len(y), device=DEV), torch.where(y < 0, 0, y)] += g[rows]
+    return {"loss": (loss.detach() * w).sum() * st["scale"], "pair_loss": loss.detach(), "rewards": reward, "logp": logp, "grad": grad}

@@ -225,7 +225,7 @@ def _framework(st, case):
     r = L.preference_loss(t.logp, st["ref"], st["off"], mask=st["mask"], weight=st["weight"], beta=st["beta"], kind=case["loss"],
                           length_normalised=case["normalised"], label_smoothing=0.1 if case["loss"] == "sigmoid" else 0.0,
                           scale=st["scale"])
-    grad = L.token_logprob_grad(st["z"], st["y"], t.lse, r.grad)
+    grad = L.token_logprob_grad(st["z"], st["y"], t, r.grad)
     return {"loss": r.loss, "pair_loss": r.pair_loss, "rewards": r.rewards, "logp": t.logp, "grad": grad}
 
 

@@ -386,6 +386,121 @@ int lbfgsb_dbg_project_direction(lbfgsb_solver* s, const double* x, const double
  * the logistic function, for x in [0, 1], 2: 1 / (1 + x), 3: x / (1 + x).  Needs no solver; runs on the null stream. */
 int lbfgsb_dbg_elementary(int which, int64_t n, const double* x, double* y);
 
+/* ---- losses on the logits of a vocabulary ------------------------------------------------------
+ * What a model that answers with tokens is trained on, next to the objectives above (LBFGSB_OBJ_LOGISTIC_L2 over feature
+ * differences is the reward model that such training starts from): log-probabilities of given tokens, the loss on pairs
+ * of answers, the clipped policy loss and distillation from a teacher's top logits, each with its gradient with respect
+ * to the logits.
+ *
+ * A row of logits z belongs to one position.  With s = 1/temperature:
+ *     u = s z,   lse = log sum_j exp(u_j),   p_j = exp(u_j - lse),   H = lse - sum_j p_j u_j   (terms with p_j = 0 are 0).
+ * Logits of -infinity (entries masked out) and of the type's lowest value are ordinary values.  A row whose logits are
+ * all -infinity has no distribution: log-probabilities and lse -infinity, H = 0, gradient 0.  NaN or +infinity makes its
+ * own row's results NaN.  A row that does not count (negative label, weight 0) is not read, whatever it holds, and gets zeros.
+ * A label or teacher index past the vocabulary makes its row's results NaN; nothing outside the row is touched.
+ *
+ * Every total is  loss = scale * sum_n weight_n * loss_n  (weight NULL: ones); the gradients are that total's.  A mean over
+ * tokens or answers, and a mask, are weights.  Sums, maxima and statistics are held in 32 or 64 bits; a gradient is rounded
+ * once, to the type of the logits.  Results are the same bits from call to call.
+ *
+ * All calls only enqueue kernels on hip_stream (NULL = the default stream): no synchronisation, allocation, copy or memset,
+ * so they may be recorded into a HIP graph.  Pointers are device pointers unless the name ends in _host.  rows = 0 is
+ * allowed (the total is then 0).  Errors as above; the outputs are then untouched. */
+
+/* element types of logits and their gradients, beside LBFGSB_F32 (the solver's A takes F64 and F32 only) */
+enum { LBFGSB_BF16 = 2, LBFGSB_F16 = 3 };
+/* integer types of teacher indices */
+enum { LBFGSB_I32 = 0, LBFGSB_I64 = 1 };
+
+typedef struct {
+    int dtype;             /* LBFGSB_F32, LBFGSB_BF16 or LBFGSB_F16: element type of z and grad */
+    int64_t rows, vocab;   /* rows <= 2^31-1, 1 <= vocab <= 2^30 */
+    int64_t ld;            /* elements from one row of z to the next, >= vocab; rows may start on any element */
+    const void* z;         /* rows x vocab */
+    double temperature;    /* > 0 */
+    void* grad;            /* gradient with respect to z, rows x vocab; NULL: not wanted.  It may be z itself (with
+                              ld_grad == ld): the gradient then takes the logits' place.  It must not overlap z otherwise */
+    int64_t ld_grad;
+} lbfgsb_logits;
+
+/* Device workspace (256-byte aligned) of a call on rows x vocab logits; 0: none is needed, the pointer may be NULL.  Its contents
+ * need not be kept between calls; calls that may run at the same time need one each. */
+size_t lbfgsb_logits_workspace_bytes(const lbfgsb_logits* logits_host);
+
+/* Log-probability of each row's label, lse, and (where not NULL) what rounding took from lse and the entropy; rows entries
+ * each.  labels: rows entries.  logits_host->grad is not looked at. */
+int lbfgsb_token_logprob(const lbfgsb_logits* logits_host, const int64_t* labels, float* logp, float* lse, float* lse_rest,
+                         float* entropy, void* workspace, size_t workspace_bytes, void* hip_stream);
+/* The way back: with d_logp (and d_entropy or NULL) the gradient of something with respect to the outputs above,
+ *     dz_j = s * (d_logp * (1[j = label] - p_j) - d_entropy * p_j * (log p_j + H)).
+ * lse, lse_rest (or NULL = 0), entropy (needed with d_entropy only): the outputs of lbfgsb_token_logprob on the same logits.
+ * Without lse_rest, p_j is known to 2^-24 |lse| of itself: not at all in a row that is masked whole by the type's lowest value. */
+int lbfgsb_token_logprob_grad(const lbfgsb_logits* logits_host, const int64_t* labels, const float* lse, const float* lse_rest,
+                              const float* entropy, const float* d_logp, const float* d_entropy, void* hip_stream);
+
+/* A teacher's top logits for each row: index and logit hold `top` entries a row, `ld` elements apart.  An entry with a
+ * negative index, or a logit of -infinity, is padding. */
+typedef struct {
+    int index_type;        /* LBFGSB_I32 or LBFGSB_I64 */
+    int logit_type;        /* LBFGSB_F32, LBFGSB_BF16 or LBFGSB_F16 */
+    int64_t top, ld;       /* 1 <= top <= 1024, ld >= top */
+    const void* index;
+    const void* logit;
+    const float* lse;      /* rows entries: the teacher's own log sum_j exp(s a_j) over its whole vocabulary; or NULL */
+} lbfgsb_teacher;
+/* Distillation: Kullback-Leibler divergence of the student's distribution from the teacher's, over the teacher's entries.
+ *   lse NULL:  q = softmax of s a over the row's entries;  loss_n = sum_k q_k (log q_k - log p_k),  dz_j = s (p_j - q_j).
+ *   else:      q_k = exp(s a_k - lse), and the rest of the vocabulary is one more outcome, of mass r = max(0, 1 - sum q) for the
+ *              teacher and t (the student's p outside the entries):  loss_n = sum_k q_k (log q_k - log p_k) + r (log r - log t),
+ *              dz_j = s (p_j - q_j) for the entries, s p_j (1 - r/t) elsewhere.
+ * (q_j: zero off the entries; an index that comes twice adds up.)  A row without entries gives zeros.  vocab <= 2^19.
+ * weight: rows entries or NULL.  loss: one float; row_loss: rows entries (loss_n, unweighted). */
+int lbfgsb_distill_loss(const lbfgsb_logits* logits_host, const lbfgsb_teacher* teacher_host, const float* weight, double scale,
+                        float* loss, float* row_loss, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+enum { LBFGSB_KL_1 = 1, LBFGSB_KL_2 = 2, LBFGSB_KL_3 = 3 };
+typedef struct {           /* rows entries each */
+    const int64_t* labels;      /* the tokens taken; negative: not counted */
+    const float* old_logp;      /* their log-probabilities when they were drawn */
+    const float* advantage;
+    const float* ref_logp;      /* under the reference model; NULL allowed when kl_coef is 0 */
+    const float* weight;        /* or NULL = ones */
+} lbfgsb_rollout;
+typedef struct {
+    double clip_low, clip_high; /* the ratio is held in [1 - clip_low, 1 + clip_high]; 0 <= clip_low <= 1, clip_high >= 0 */
+    double kl_coef, entropy_coef;
+    int kl_kind;                /* with d = logp - ref_logp: KL_1: d, KL_2: d^2/2, KL_3: exp(-d) - 1 + d */
+} lbfgsb_policy_options;
+/* The clipped policy loss of each token, with r = exp(logp - old_logp) and A the advantage:
+ *     loss_n = -min(r A, min(max(r, 1 - clip_low), 1 + clip_high) A) + kl_coef KL(logp, ref_logp) - entropy_coef H.
+ * Its gradient with respect to logp is -r A where the first of the two is the smaller or equal, else 0, plus the KL term's.
+ * loss: one float; row_loss, logp, entropy (or NULL): rows entries. */
+int lbfgsb_policy_loss(const lbfgsb_logits* logits_host, const lbfgsb_rollout* rollout_host, const lbfgsb_policy_options* opt_host,
+                       double scale, float* loss, float* row_loss, float* logp, float* entropy, void* workspace,
+                       size_t workspace_bytes, void* hip_stream);
+
+enum { LBFGSB_PAIR_SIGMOID = 0, LBFGSB_PAIR_HINGE = 1, LBFGSB_PAIR_IPO = 2 };
+typedef struct {
+    int kind;                   /* LBFGSB_PAIR_* */
+    int length_normalised;      /* 1: an answer's log ratio is the mean over its tokens, 0: the sum */
+    double beta;                /* > 0 */
+    double label_smoothing;     /* SIGMOID only, in [0, 1) */
+    double margin;
+} lbfgsb_preference_options;
+/* The loss on pairs of answers, from the log-probabilities of their tokens (lbfgsb_token_logprob; the gradient goes back through
+ * lbfgsb_token_logprob_grad).  Answer i has the tokens offsets[i] <= t < offsets[i+1]; answers 0 .. pairs-1 are the chosen
+ * ones, pairs .. 2 pairs-1 the rejected ones of the same pairs.  offsets: 2 pairs + 1 ascending entries (taken into
+ * 0 .. tokens where they are not).  mask (or NULL): tokens entries, 0 = does not count.
+ *     R_i = sum (or mean) over the answer's tokens that count of logp - ref_logp  (ref_logp NULL: of logp; no token: 0),
+ *     delta = beta (R_chosen - R_rejected) - margin,
+ *     SIGMOID  -(1 - e) log sigmoid(delta) - e log sigmoid(-delta),  HINGE  max(0, 1 - delta),  IPO  ((delta - 1/2)/beta)^2.
+ * loss: one float; pair_loss: pairs entries; rewards: 2 pairs entries, beta R_i; grad (or NULL): d loss / d logp, tokens
+ * entries (0 for tokens that do not count or belong to no answer).  weight: pairs entries or NULL.
+ * R is summed in 64 bits. */
+int lbfgsb_preference_loss(int64_t tokens, int64_t pairs, const float* logp, const float* ref_logp, const int64_t* offsets,
+                           const uint8_t* mask, const float* weight, const lbfgsb_preference_options* opt_host, double scale,
+                           float* loss, float* pair_loss, float* rewards, float* grad, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -10,6 +10,10 @@ import ctypes as C
 import os
 from typing import Optional
 
+from . import losses
+from .losses import (DistillLoss, PolicyLoss, PreferenceLoss, TokenLogprob, distill_loss, policy_loss, preference_loss, token_logprob,
+                     token_logprob_grad)
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liblbfgsb.so")
 
@@ -29,6 +33,8 @@ EXPORTS = [
     "lbfgsb_auglag_get_x", "lbfgsb_auglag_get_lambda", "lbfgsb_auglag_inner", "lbfgsb_auglag_destroy",
     "lbfgsb_auglag_rows_workspace_bytes", "lbfgsb_auglag_create_rows",
     "lbfgsb_auglag_marginals_workspace_bytes", "lbfgsb_auglag_create_marginals",
+    "lbfgsb_logits_workspace_bytes", "lbfgsb_token_logprob", "lbfgsb_token_logprob_grad", "lbfgsb_distill_loss", "lbfgsb_policy_loss",
+    "lbfgsb_preference_loss",
 ]
 
 
@@ -169,6 +175,7 @@ def lib():
         L.lbfgsb_auglag_inner.argtypes = [vp]
         L.lbfgsb_auglag_destroy.restype = None
         L.lbfgsb_auglag_destroy.argtypes = [vp]
+        losses.declare(L)
         _lib = L
     return _lib
 

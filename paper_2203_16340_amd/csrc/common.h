@@ -12,6 +12,9 @@
 
 namespace lb {
 
+// Keeps the message of lbfgsb_last_error and returns `code`.
+int fail(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+
 constexpr int kMaxM = LBFGSB_MAX_M;
 constexpr int kMaxV = 64;          // 2*m + 1 <= 64 vectors enter the batched two-loop
 constexpr int kBlock = 256;        // threads per workgroup of every vector kernel (4 waves of 64)

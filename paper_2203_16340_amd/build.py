@@ -11,7 +11,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblbfgsb.so")
 SOURCES = ["fused.hip", "narrow.hip", "small.hip", "symmetric.hip", "gram.hip", "api.hip", "apass.hip", "resident.hip", "transport.hip", "vec.hip",
-           "logits.hip", "preference.hip", "losses_api.hip"]
+           "logits.hip", "logits_f32.hip", "logits_bf16.hip", "logits_f16.hip", "preference.hip", "losses_api.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
     # packed-fp32 instructions are kept out of the generated code on purpose

@@ -57,20 +57,20 @@ hipError_t launch_token_logprob_grad(const LogitsArgs& l, int dtype, const Token
 hipError_t launch_distill(const LogitsArgs& l, int dtype, const DistillArgs& a, float* loss, float* ws, hipStream_t st);
 hipError_t launch_policy(const LogitsArgs& l, int dtype, const PolicyArgs& a, float* loss, float* ws, hipStream_t st);
 hipError_t launch_preference(const PreferenceArgs& a, float* loss, hipStream_t st);
+// the same for one element type, rows > 0, without the totals (logits_rows.h)
+template <typename T>
+hipError_t token_logprob_rows(const LogitsArgs& l, const TokenArgs& a, float* ws, hipStream_t st);
+template <typename T>
+hipError_t token_grad_rows(const LogitsArgs& l, const TokenGradArgs& a, hipStream_t st);
+template <typename T>
+hipError_t policy_rows(const LogitsArgs& l, const PolicyArgs& a, float* ws, hipStream_t st);
+template <typename T>
+hipError_t distill_rows(const LogitsArgs& l, const DistillArgs& a, float* ws, hipStream_t st);
 // loss = scale * sum_n weight_n row_loss_n
 hipError_t launch_weighted_total(const float* row_loss, const float* weight, int64_t n, double scale, float* loss, hipStream_t st);
 size_t logits_workspace(int64_t rows, int64_t vocab, int dtype);
 
-// ---- element types: a chunk is 16 bytes of a row -------------------------------------------------------------------
-template <int DTYPE>
-struct Elem;
-template <>
-struct Elem<LBFGSB_F32> { typedef float type; };
-template <>
-struct Elem<LBFGSB_BF16> { typedef __bf16 type; };
-template <>
-struct Elem<LBFGSB_F16> { typedef _Float16 type; };
-
+// ---- a chunk is 16 bytes of a row ------------------------------------------------------------------------------------
 template <typename T>
 struct Chunk {
     static constexpr int E = 16 / (int)sizeof(T);
@@ -78,29 +78,6 @@ struct Chunk {
     typedef vec any __attribute__((aligned(sizeof(T))));           // a row may start on any element
     typedef float wide __attribute__((ext_vector_type(E)));
 };
-
-// elements [e, e + E) of a row; what lies past the vocabulary reads as -infinity, which no statistic notices
-template <typename T>
-__device__ __forceinline__ typename Chunk<T>::vec load_chunk(const T* row, int e, int vocab) {
-    constexpr int E = Chunk<T>::E;
-    if (e + E <= vocab) return *(const typename Chunk<T>::any*)(row + e);
-    typename Chunk<T>::vec v;
-#pragma unroll
-    for (int i = 0; i < E; ++i) v[i] = e + i < vocab ? row[e + i] : (T)(-INFINITY);
-    return v;
-}
-template <typename T>
-__device__ __forceinline__ void store_chunk(T* row, int e, int vocab, typename Chunk<T>::wide g) {
-    constexpr int E = Chunk<T>::E;
-    const typename Chunk<T>::vec v = __builtin_convertvector(g, typename Chunk<T>::vec);
-    if (e + E <= vocab) {
-        *(typename Chunk<T>::any*)(row + e) = v;
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < E; ++i)
-        if (e + i < vocab) row[e + i] = v[i];
-}
 
 // ---- statistics of a softmax -----------------------------------------------------------------------------------------
 // Over the entries seen so far, with a_j = (z_j - m) c: m = max z_j, s = sum 2^a_j, t = sum a_j 2^a_j (for the entropy).

@@ -1,0 +1,11 @@
+// The losses on rows of logits of type __bf16.
+#include "logits_rows.h"
+
+namespace lb {
+
+template hipError_t token_logprob_rows<__bf16>(const LogitsArgs&, const TokenArgs&, float*, hipStream_t);
+template hipError_t token_grad_rows<__bf16>(const LogitsArgs&, const TokenGradArgs&, hipStream_t);
+template hipError_t policy_rows<__bf16>(const LogitsArgs&, const PolicyArgs&, float*, hipStream_t);
+template hipError_t distill_rows<__bf16>(const LogitsArgs&, const DistillArgs&, float*, hipStream_t);
+
+}  // namespace lb

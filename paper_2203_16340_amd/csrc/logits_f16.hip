@@ -1,0 +1,11 @@
+// The losses on rows of logits of type _Float16.
+#include "logits_rows.h"
+
+namespace lb {
+
+template hipError_t token_logprob_rows<_Float16>(const LogitsArgs&, const TokenArgs&, float*, hipStream_t);
+template hipError_t token_grad_rows<_Float16>(const LogitsArgs&, const TokenGradArgs&, hipStream_t);
+template hipError_t policy_rows<_Float16>(const LogitsArgs&, const PolicyArgs&, float*, hipStream_t);
+template hipError_t distill_rows<_Float16>(const LogitsArgs&, const DistillArgs&, float*, hipStream_t);
+
+}  // namespace lb

@@ -10,10 +10,6 @@ import ctypes as C
 import os
 from typing import Optional
 
-from . import losses
-from .losses import (DistillLoss, PolicyLoss, PreferenceLoss, TokenLogprob, distill_loss, policy_loss, preference_loss, token_logprob,
-                     token_logprob_grad)
-
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liblbfgsb.so")
 
@@ -594,3 +590,9 @@ def solver_for_problem(prob, device="cuda:0", **option_overrides) -> Solver:
     s = Solver(prob.kind, A, b, l, u, prob.m, lam=prob.lam, mu=prob.mu, options=opts)
     s.set_x(torch.from_numpy(prob.x0).to(dev))
     return s
+
+
+from . import losses  # noqa: E402  (it uses what is above)
+from .losses import (  # noqa: E402
+    DistillLoss, PolicyLoss, PreferenceLoss, TokenLogprob, distill_loss, policy_loss, preference_loss, token_logprob,
+    token_logprob_grad)

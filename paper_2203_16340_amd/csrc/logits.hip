@@ -11,9 +11,17 @@ __global__ __launch_bounds__(kTotalBlock) void k_weighted_total(const float* row
                                                                 float* loss) {
     __shared__ double lds[kTotalBlock / 64];
     double sum = 0.0;
-    for (int64_t i = threadIdx.x; i < n; i += kTotalBlock) {
-        const float w = weight ? weight[i] : 1.0f;
-        if (w != 0.0f) sum += (double)w * (double)row_loss[i];   // (what does not count may be infinite)
+    for (int64_t i0 = threadIdx.x; i0 < n; i0 += 4 * kTotalBlock) {
+        float v[4], w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int64_t i = i0 + k * kTotalBlock;
+            v[k] = i < n ? row_loss[i] : 0.0f;
+            w[k] = i < n && weight ? weight[i] : 1.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (w[k] != 0.0f) sum += (double)w[k] * (double)v[k];   // (what does not count may be infinite)
     }
     sum = wave_sum(sum);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = sum;

@@ -52,11 +52,14 @@ struct Cut {
 };
 
 // A workgroup's hold on one row.  CH chunks a thread stay in registers between the statistics and the gradient; what a longer row has
-// before them is read a second time.  (CH = 0: all of it.)
+// before them is read a second time.  (CH = 0: no gradient, two loads in flight.)
+// Loads that are the last of their row go past the caches, unless a workgroup of 1024 makes them: us without / with, token
+// log-probabilities of 16400 x 131072 bf16 702 / 665, distillation 4096 x 65536 bf16 208 / 199, but policy 8192 x 131072 bf16 839 / 863.
 template <typename T, int BLOCK, int CH>
 struct Row {
     static constexpr int E = Chunk<T>::E;
-    static constexpr int kSlots = CH > 0 ? CH : 4;       // loads in flight
+    static constexpr int kSlots = CH > 0 ? CH : 2;
+    static constexpr bool NT_LOADS = BLOCK <= 512;
     typedef typename Chunk<T>::vec vec;
     typedef typename Chunk<T>::any any;
 
@@ -74,9 +77,13 @@ struct Row {
         if (j >= 0) alone = (float)row[j];
         start();
     }
-    __device__ __forceinline__ vec chunk(int i) const { return *(const any*)(base + (size_t)(unsigned)i * 16); }
+    __device__ __forceinline__ vec chunk(int i) const {
+        const any* p = (const any*)(base + (size_t)(unsigned)i * 16);
+        if constexpr (NT_LOADS) return __builtin_nontemporal_load(p);
+        else return *p;
+    }
     // Chunk of slot k in the round that begins at chunk `from`, of those before `end`; past the end it is the last one again, which
-    // is not looked at.
+    // is not looked at.  (No branch: with one around each load the compiler moves it to where its value is used.)
     __device__ __forceinline__ void fetch(int k, int from, int end) {
         const int i = from + k * BLOCK + (int)threadIdx.x;
         slot[k] = chunk(i < end ? i : end - 1);
@@ -156,19 +163,16 @@ struct Row {
                 for (int e = 0; e < E; ++e)
                     if (e == at) g[e] += mark;
             }
-            *(any*)(to + (size_t)(unsigned)i * 16) = __builtin_convertvector(g, vec);
+            __builtin_nontemporal_store(__builtin_convertvector(g, vec), (any*)(to + (size_t)(unsigned)i * 16));
         };
         const int j = cut.single((int)threadIdx.x);
         if (j >= 0) out[j] = (T)(slope_at<ENT>(alone, ref, c, A, B) + (j == y ? mark : 0.0f));
-        if constexpr (CH > 0) {
+        static_assert(CH > 0);
 #pragma unroll
-            for (int k = 0; k < CH; ++k) {
-                const int i = again + k * BLOCK + (int)threadIdx.x;
-                if (i < cut.whole) one(opaque(slot[k]), i);
-                if (again > 0) fetch(k, 0, again);
-            }
-        } else {
-            start();
+        for (int k = 0; k < CH; ++k) {
+            const int i = again + k * BLOCK + (int)threadIdx.x;
+            if (i < cut.whole) one(opaque(slot[k]), i);
+            if (again > 0) fetch(k, 0, again);
         }
         for (int from = 0; from < again; from += BLOCK * kSlots) {
             const int next = from + BLOCK * kSlots;
@@ -223,7 +227,7 @@ __global__ __launch_bounds__(BLOCK) void k_token_logprob(LogitsArgs l, TokenArgs
 }
 
 // The way back needs no sums: log p_j = z_j s - lse.  Workgroups take pieces of kGradChunks chunks a thread.
-constexpr int kGradBlock = 256, kGradChunks = 4;
+constexpr int kGradBlock = 512, kGradChunks = 2;
 
 template <typename T, bool ENT>
 __global__ __launch_bounds__(kGradBlock) void k_token_grad(LogitsArgs l, TokenGradArgs a, int pieces, int64_t first) {
@@ -258,7 +262,7 @@ __global__ __launch_bounds__(kGradBlock) void k_token_grad(LogitsArgs l, TokenGr
     vec slot[kGradChunks];
 #pragma unroll
     for (int k = 0; k < kGradChunks; ++k)
-        if (i0 + k * kGradBlock < cut.whole) slot[k] = *(const any*)(from + (size_t)(unsigned)(i0 + k * kGradBlock) * 16);
+        if (i0 + k * kGradBlock < cut.whole) slot[k] = __builtin_nontemporal_load((const any*)(from + (size_t)(unsigned)(i0 + k * kGradBlock) * 16));
     // p_j (-g - h (log p_j + H))
     const float A = -(g + h * entropy) * s, B = -h * s;
     auto at = [&](float z) {
@@ -280,7 +284,7 @@ __global__ __launch_bounds__(kGradBlock) void k_token_grad(LogitsArgs l, TokenGr
             for (int e = 0; e < E; ++e)
                 if (e == mark) o[e] = fmaf(g, s, o[e]);
         }
-        *(any*)(to + (size_t)(unsigned)i * 16) = __builtin_convertvector(o, vec);
+        __builtin_nontemporal_store(__builtin_convertvector(o, vec), (any*)(to + (size_t)(unsigned)i * 16));
     }
 }
 
@@ -544,9 +548,15 @@ void by_width(int vocab, F f) {
     constexpr int E = Chunk<T>::E;
     const int chunks = vocab / E;
     using std::integral_constant;
-    if (chunks <= 256 * 4) f(integral_constant<int, 256>{}, integral_constant<int, 4>{});
+    if (chunks <= 64 * 4) f(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+    else if (chunks <= 128 * 4) f(integral_constant<int, 128>{}, integral_constant<int, 4>{});
+    else if (chunks <= 256 * 4) f(integral_constant<int, 256>{}, integral_constant<int, 4>{});
+    else if (chunks <= 256 * 8) f(integral_constant<int, 256>{}, integral_constant<int, 8>{});
     else if (chunks <= 512 * 8) f(integral_constant<int, 512>{}, integral_constant<int, 8>{});
+    else if (chunks <= 512 * 10) f(integral_constant<int, 512>{}, integral_constant<int, 10>{});
+    else if (chunks <= 512 * 13) f(integral_constant<int, 512>{}, integral_constant<int, 13>{});
     else if (chunks <= 512 * 16) f(integral_constant<int, 512>{}, integral_constant<int, 16>{});
+    else if (chunks <= 1024 * 13) f(integral_constant<int, 1024>{}, integral_constant<int, 13>{});
     else f(integral_constant<int, 1024>{}, integral_constant<int, 16>{});
 }
 
@@ -554,10 +564,15 @@ void by_width(int vocab, F f) {
 
 template <typename T>
 hipError_t token_logprob_rows(const LogitsArgs& l, const TokenArgs& a, float*, hipStream_t st) {
-    by_rows(l.rows, [&](int64_t first, dim3 grid) {
-        if (a.entropy) hipLaunchKernelGGL((k_token_logprob<T, true, 512>), grid, dim3(512), 0, st, l, a, first);
-        else hipLaunchKernelGGL((k_token_logprob<T, false, 512>), grid, dim3(512), 0, st, l, a, first);
-    });
+    const int chunks = l.vocab / Chunk<T>::E;
+    auto launch = [&](auto block) {
+        constexpr int BLOCK = decltype(block)::value;
+        const auto kernel = a.entropy ? k_token_logprob<T, true, BLOCK> : k_token_logprob<T, false, BLOCK>;
+        by_rows(l.rows, [&](int64_t first, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(BLOCK), 0, st, l, a, first); });
+    };
+    if (chunks <= 1024) launch(std::integral_constant<int, 64>{});
+    else if (chunks <= 4096) launch(std::integral_constant<int, 256>{});
+    else launch(std::integral_constant<int, 512>{});
     return hipGetLastError();
 }
 

@@ -423,8 +423,9 @@ typedef struct {
     int64_t ld_grad;
 } lbfgsb_logits;
 
-/* Device workspace (256-byte aligned) of a call on rows x vocab logits; 0: none is needed, the pointer may be NULL.  Its contents
- * need not be kept between calls; calls that may run at the same time need one each. */
+/* Device workspace (256-byte aligned) of a call on these logits (dtype, rows, vocab and whether grad is NULL are read; a call without a
+ * gradient needs no more than one with).  0: none is needed, the pointer may be NULL.  Its contents need not be kept between
+ * calls; calls that may run at the same time need one each. */
 size_t lbfgsb_logits_workspace_bytes(const lbfgsb_logits* logits_host);
 
 /* Log-probability of each row's label, lse, and (where not NULL) what rounding took from lse and the entropy; rows entries

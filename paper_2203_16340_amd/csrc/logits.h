@@ -9,6 +9,34 @@ namespace lb {
 constexpr int kMaxTop = 1024;                  // teacher entries of a row, at most
 constexpr int64_t kMaxDistillVocab = 1 << 19;  // one bit for each entry of the vocabulary is kept in LDS
 
+// Statistics of a softmax over the entries seen so far, with a_j = (z_j - m) c: m = max z_j, s = sum 2^a_j, t = sum a_j 2^a_j (for
+// the entropy).  The difference is taken before the scale, so that a maximum near the type's largest or lowest value overflows
+// nothing.
+struct Stat {
+    float m, s, t;
+};
+
+// What a row's entries of the teacher come to.
+struct Teacher {
+    double cross;       // sum_k q_k (log q_k - s z_k)
+    double sum;         // sum_k q_k
+    Stat top;           // the student's statistics over the entries, each once
+    int entries;        // how many there are, each once
+    int lost;           // one of them lies past the vocabulary
+};
+
+// A few long rows are split: workgroups of a first launch take the statistics of pieces, those of a second join them and write the
+// gradient.  What the first leaves for the second, a row each, in the caller's workspace.
+constexpr int kSplitRows = 64;      // rows, at most (a wave looks after their total)
+constexpr int kSplits = 64;         // pieces of a row, at most (a wave joins them)
+struct SplitRow {
+    Stat part[kSplits];
+    Teacher teacher;
+    float zy;                       // the label's logit
+    int at[kMaxTop];                // the teacher's entries, as in TopLds
+    float q[kMaxTop], z[kMaxTop];
+};
+
 struct LogitsArgs {
     const void* z;
     void* dz;               // null: no gradient
@@ -52,23 +80,24 @@ struct PreferenceArgs {
     int kind, normalised;
 };
 
-hipError_t launch_token_logprob(const LogitsArgs& l, int dtype, const TokenArgs& a, float* ws, hipStream_t st);
+hipError_t launch_token_logprob(const LogitsArgs& l, int dtype, const TokenArgs& a, SplitRow* ws, hipStream_t st);
 hipError_t launch_token_logprob_grad(const LogitsArgs& l, int dtype, const TokenGradArgs& a, hipStream_t st);
-hipError_t launch_distill(const LogitsArgs& l, int dtype, const DistillArgs& a, float* loss, float* ws, hipStream_t st);
-hipError_t launch_policy(const LogitsArgs& l, int dtype, const PolicyArgs& a, float* loss, float* ws, hipStream_t st);
+hipError_t launch_distill(const LogitsArgs& l, int dtype, const DistillArgs& a, float* loss, SplitRow* ws, hipStream_t st);
+hipError_t launch_policy(const LogitsArgs& l, int dtype, const PolicyArgs& a, float* loss, SplitRow* ws, hipStream_t st);
 hipError_t launch_preference(const PreferenceArgs& a, float* loss, hipStream_t st);
-// the same for one element type, rows > 0, without the totals (logits_rows.h)
+// the same for one element type, rows > 0 (logits_rows.h)
 template <typename T>
-hipError_t token_logprob_rows(const LogitsArgs& l, const TokenArgs& a, float* ws, hipStream_t st);
+hipError_t token_logprob_rows(const LogitsArgs& l, const TokenArgs& a, SplitRow* ws, hipStream_t st);
 template <typename T>
 hipError_t token_grad_rows(const LogitsArgs& l, const TokenGradArgs& a, hipStream_t st);
 template <typename T>
-hipError_t policy_rows(const LogitsArgs& l, const PolicyArgs& a, float* ws, hipStream_t st);
+hipError_t policy_rows(const LogitsArgs& l, const PolicyArgs& a, float* loss, SplitRow* ws, hipStream_t st);
 template <typename T>
-hipError_t distill_rows(const LogitsArgs& l, const DistillArgs& a, float* ws, hipStream_t st);
+hipError_t distill_rows(const LogitsArgs& l, const DistillArgs& a, float* loss, SplitRow* ws, hipStream_t st);
 // loss = scale * sum_n weight_n row_loss_n
 hipError_t launch_weighted_total(const float* row_loss, const float* weight, int64_t n, double scale, float* loss, hipStream_t st);
-size_t logits_workspace(int64_t rows, int64_t vocab, int dtype);
+// Pieces that each of a call's rows is split into; 1: none is.
+int row_splits(int64_t rows, int64_t vocab, int size, bool grad);   // size: bytes of a logit; grad: a gradient is wanted
 
 // ---- a chunk is 16 bytes of a row ------------------------------------------------------------------------------------
 template <typename T>
@@ -80,11 +109,6 @@ struct Chunk {
 };
 
 // ---- statistics of a softmax -----------------------------------------------------------------------------------------
-// Over the entries seen so far, with a_j = (z_j - m) c: m = max z_j, s = sum 2^a_j, t = sum a_j 2^a_j (for the entropy).
-// The difference is taken before the scale, so that a maximum near the type's largest or lowest value overflows nothing.
-struct Stat {
-    float m, s, t;
-};
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 // (how far below the maximum, in powers of two: no further than counts, so that 0 times it is 0; -infinity - -infinity, which is
 // no number, ends here as well)
@@ -131,7 +155,10 @@ __device__ __forceinline__ Stat wave_stat(Stat a, float c) {
 template <bool ENT, int NW>
 __device__ __forceinline__ Stat block_stat(Stat a, float c, Stat* lds) {
     a = wave_stat<ENT>(a, c);
-    if constexpr (NW == 1) return a;
+    if constexpr (NW == 1) {
+        __syncthreads();            // (callers count on the barrier)
+        return a;
+    }
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = a;
     __syncthreads();
     float top = lds[0].m;

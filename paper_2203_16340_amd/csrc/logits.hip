@@ -41,14 +41,23 @@ hipError_t by_type(int dtype, F f) {
 
 }  // namespace
 
-size_t logits_workspace(int64_t, int64_t, int) { return 0; }
+int row_splits(int64_t rows, int64_t vocab, int size, bool grad) {
+    // Calls in a row on R rows of V bf16 logits, us, whole / in pieces: policy loss with gradient 1 x 16384 7.4 / 6.2, 64 x 16384
+    // 8.4 / 7.1, 1 x 32768 9.0 / 8.0, 64 x 32768 9.9 / 8.3, 1 x 131072 19.3 / 7.4, 64 x 131072 20.0 / 10.8; but 64 x 8192 6.5 / 6.9.  Log-probabilities
+    // (one launch against two, and less to do in them) 8 x 32768 4.7 / 6.4, 1 x 131072 9.7 / 6.9, 64 x 131072 22 / 8.
+    const int64_t chunks = vocab * size / 16;
+    if (rows > kSplitRows || chunks < (grad ? 4096 : 8192)) return 1;
+    // about two workgroups a compute unit, with two chunks a thread or more
+    const int64_t most = chunks / 1024, want = 512 / rows, splits = want < most ? want : most;
+    return (int)(splits < kSplits ? splits : kSplits);
+}
 
 hipError_t launch_weighted_total(const float* row_loss, const float* weight, int64_t n, double scale, float* loss, hipStream_t st) {
     hipLaunchKernelGGL(k_weighted_total, dim3(1), dim3(kTotalBlock), 0, st, row_loss, weight, n, scale, loss);
     return hipGetLastError();
 }
 
-hipError_t launch_token_logprob(const LogitsArgs& l, int dtype, const TokenArgs& a, float* ws, hipStream_t st) {
+hipError_t launch_token_logprob(const LogitsArgs& l, int dtype, const TokenArgs& a, SplitRow* ws, hipStream_t st) {
     if (l.rows == 0) return hipSuccess;
     return by_type(dtype, [&](auto e) { return token_logprob_rows<decltype(e)>(l, a, ws, st); });
 }
@@ -58,16 +67,14 @@ hipError_t launch_token_logprob_grad(const LogitsArgs& l, int dtype, const Token
     return by_type(dtype, [&](auto e) { return token_grad_rows<decltype(e)>(l, a, st); });
 }
 
-hipError_t launch_policy(const LogitsArgs& l, int dtype, const PolicyArgs& a, float* loss, float* ws, hipStream_t st) {
-    if (l.rows > 0)
-        if (hipError_t err = by_type(dtype, [&](auto e) { return policy_rows<decltype(e)>(l, a, ws, st); }); err != hipSuccess) return err;
-    return launch_weighted_total(a.row_loss, a.weight, l.rows, a.scale, loss, st);
+hipError_t launch_policy(const LogitsArgs& l, int dtype, const PolicyArgs& a, float* loss, SplitRow* ws, hipStream_t st) {
+    if (l.rows == 0) return launch_weighted_total(nullptr, nullptr, 0, a.scale, loss, st);
+    return by_type(dtype, [&](auto e) { return policy_rows<decltype(e)>(l, a, loss, ws, st); });
 }
 
-hipError_t launch_distill(const LogitsArgs& l, int dtype, const DistillArgs& a, float* loss, float* ws, hipStream_t st) {
-    if (l.rows > 0)
-        if (hipError_t err = by_type(dtype, [&](auto e) { return distill_rows<decltype(e)>(l, a, ws, st); }); err != hipSuccess) return err;
-    return launch_weighted_total(a.row_loss, a.weight, l.rows, a.scale, loss, st);
+hipError_t launch_distill(const LogitsArgs& l, int dtype, const DistillArgs& a, float* loss, SplitRow* ws, hipStream_t st) {
+    if (l.rows == 0) return launch_weighted_total(nullptr, nullptr, 0, a.scale, loss, st);
+    return by_type(dtype, [&](auto e) { return distill_rows<decltype(e)>(l, a, loss, ws, st); });
 }
 
 }  // namespace lb

@@ -51,48 +51,57 @@ struct Cut {
     __device__ __forceinline__ int shift() const { return (E - head) & (E - 1); }
 };
 
-// A workgroup's hold on one row.  CH chunks a thread stay in registers between the statistics and the gradient; what a longer row has
-// before them is read a second time.  (CH = 0: no gradient, two loads in flight.)
+// A workgroup's hold on one row, or on piece `piece` of `pieces` of it.  CH chunks a thread stay in registers between the statistics and the gradient; what a longer row has
+// before them is read a second time.  (CH = 0: no gradient, SLOTS loads in flight.)
 // Loads that are the last of their row go past the caches, unless a workgroup of 1024 makes them: us without / with, token
 // log-probabilities of 16400 x 131072 bf16 702 / 665, distillation 4096 x 65536 bf16 208 / 199, but policy 8192 x 131072 bf16 839 / 863.
-template <typename T, int BLOCK, int CH>
+template <typename T, int BLOCK, int CH, bool NT_LOADS = (BLOCK <= 512), int SLOTS = 2>
 struct Row {
     static constexpr int E = Chunk<T>::E;
-    static constexpr int kSlots = CH > 0 ? CH : 2;
-    static constexpr bool NT_LOADS = BLOCK <= 512;
+    static constexpr int kSlots = CH > 0 ? CH : SLOTS;
     typedef typename Chunk<T>::vec vec;
     typedef typename Chunk<T>::any any;
 
     vec slot[kSlots];
     float alone;                         // the single element of this thread, if any
-    const char* base;                    // the first chunk
+    const char* base;                    // the row's first chunk
     Cut<T> cut;
-    int again;                           // chunks that are read twice
+    int begin, end;                      // the chunks of this piece
+    int again;                           // up to here they are read twice
+    int j;                               // where `alone` stands, or -1 (the single elements go with the first piece)
 
-    __device__ __forceinline__ Row(const T* row, int vocab) : cut(row, vocab) {
+    __device__ __forceinline__ Row(const T* row, int vocab, int piece = 0, int pieces = 1) : cut(row, vocab) {
         base = (const char*)(row + cut.head);
-        again = CH > 0 ? (cut.whole > BLOCK * CH ? cut.whole - BLOCK * CH : 0) : cut.whole;
+        const int each = (cut.whole + pieces - 1) / pieces;
+        begin = pieces == 1 ? 0 : (piece * each < cut.whole ? piece * each : cut.whole);
+        end = pieces == 1 ? cut.whole : (begin + each < cut.whole ? begin + each : cut.whole);
+        again = CH > 0 ? (end - begin > BLOCK * CH ? end - BLOCK * CH : begin) : end;
         alone = 0.0f;
-        const int j = cut.single((int)threadIdx.x);
+        j = piece == 0 ? cut.single((int)threadIdx.x) : -1;
         if (j >= 0) alone = (float)row[j];
         start();
+    }
+    // whether element e is one of this piece's
+    __device__ __forceinline__ bool has(int e) const {
+        const int i = e - cut.head;
+        return i < 0 || i >= cut.whole * E ? begin == 0 : i >= begin * E && i < end * E;
     }
     __device__ __forceinline__ vec chunk(int i) const {
         const any* p = (const any*)(base + (size_t)(unsigned)i * 16);
         if constexpr (NT_LOADS) return __builtin_nontemporal_load(p);
         else return *p;
     }
-    // Chunk of slot k in the round that begins at chunk `from`, of those before `end`; past the end it is the last one again, which
+    // Chunk of slot k in the round that begins at chunk `from`, of those before `to`; past them it is the last one again, which
     // is not looked at.  (No branch: with one around each load the compiler moves it to where its value is used.)
-    __device__ __forceinline__ void fetch(int k, int from, int end) {
+    __device__ __forceinline__ void fetch(int k, int from, int to) {
         const int i = from + k * BLOCK + (int)threadIdx.x;
-        slot[k] = chunk(i < end ? i : end - 1);
+        slot[k] = chunk(i < to ? i : to - 1);
     }
     __device__ __forceinline__ void start() {
-        const int end = again > 0 ? again : cut.whole;
-        if (end > 0) {
+        const int to = again > begin ? again : end;
+        if (to > begin) {
 #pragma unroll
-            for (int k = 0; k < kSlots; ++k) fetch(k, 0, end);
+            for (int k = 0; k < kSlots; ++k) fetch(k, begin, to);
         }
     }
     // (the same bits, but to the compiler a new value: else it keeps the 32-bit values of a 16-bit row as well, twice the registers)
@@ -122,22 +131,21 @@ struct Row {
             }
             take<ENT>(a, z, c);
         };
-        const int j = cut.single((int)threadIdx.x);
-        for (int from = 0; from < again; from += BLOCK * kSlots) {
+        for (int from = begin; from < again; from += BLOCK * kSlots) {
             const int next = from + BLOCK * kSlots;
 #pragma unroll
             for (int k = 0; k < kSlots; ++k) {
                 const int i = from + k * BLOCK + (int)threadIdx.x;
                 if (i < again) one(slot[k], i);
                 if (next < again) fetch(k, next, again);
-                else if (CH > 0) fetch(k, again, cut.whole);
+                else if (CH > 0) fetch(k, again, end);
             }
         }
         if constexpr (CH > 0) {
 #pragma unroll
             for (int k = 0; k < CH; ++k) {
                 const int i = again + k * BLOCK + (int)threadIdx.x;
-                if (i < cut.whole) one(slot[k], i);
+                if (i < end) one(slot[k], i);
             }
         }
         if (j >= 0) {
@@ -165,16 +173,15 @@ struct Row {
             }
             __builtin_nontemporal_store(__builtin_convertvector(g, vec), (any*)(to + (size_t)(unsigned)i * 16));
         };
-        const int j = cut.single((int)threadIdx.x);
         if (j >= 0) out[j] = (T)(slope_at<ENT>(alone, ref, c, A, B) + (j == y ? mark : 0.0f));
         static_assert(CH > 0);
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
             const int i = again + k * BLOCK + (int)threadIdx.x;
-            if (i < cut.whole) one(opaque(slot[k]), i);
-            if (again > 0) fetch(k, 0, again);
+            if (i < end) one(opaque(slot[k]), i);
+            if (again > begin) fetch(k, begin, again);
         }
-        for (int from = 0; from < again; from += BLOCK * kSlots) {
+        for (int from = begin; from < again; from += BLOCK * kSlots) {
             const int next = from + BLOCK * kSlots;
 #pragma unroll
             for (int k = 0; k < kSlots; ++k) {
@@ -185,45 +192,59 @@ struct Row {
         }
     }
 
-    static __device__ __forceinline__ void fill(T* out, int vocab, float value) {
+    // zeros in a row, or piece `piece` of `pieces` of it
+    static __device__ __forceinline__ void clear(T* out, int vocab, int piece = 0, int pieces = 1) {
         const Cut<T> cut(out, vocab);
         vec v;
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = (T)value;
-        for (int i = threadIdx.x; i < cut.whole; i += BLOCK) *(any*)((char*)(out + cut.head) + (size_t)(unsigned)i * 16) = v;
-        const int j = cut.single((int)threadIdx.x);
-        if (j >= 0) out[j] = (T)value;
+        for (int e = 0; e < E; ++e) v[e] = (T)0.0f;
+        for (int i = piece * BLOCK + (int)threadIdx.x; i < cut.whole; i += pieces * BLOCK)
+            __builtin_nontemporal_store(v, (any*)((char*)(out + cut.head) + (size_t)(unsigned)i * 16));
+        const int j = piece == 0 ? cut.single((int)threadIdx.x) : -1;
+        if (j >= 0) out[j] = (T)0.0f;
     }
 };
 
 // ---- token log-probabilities -------------------------------------------------------------------------------------------
 
-template <typename T, bool ENT, int BLOCK>
+__device__ __forceinline__ float logp_of(Stat st, const RowLog& g, double s, float zy) {
+    // (zy is no number where the label is past the vocabulary)
+    return st.s == 0.0f ? (zy == zy ? -INFINITY : zy) : (float)(((double)zy - (double)st.m) * s - g.log_s);
+}
+template <typename T>
+__device__ __forceinline__ float label_logit(const T* row, int64_t y, int vocab) {
+    return y < vocab ? (float)row[y] : NAN;
+}
+
+__device__ __forceinline__ void put_token(const LogitsArgs& l, const TokenArgs& a, int64_t r, Stat st, float zy) {
+    const RowLog g = row_log(st, l.s);
+    const float lse = (float)g.lse;
+    a.logp[r] = logp_of(st, g, l.s, zy);
+    a.lse[r] = lse;
+    if (a.lse_rest) a.lse_rest[r] = fabsf(lse) < INFINITY ? (float)(((double)st.m * l.s - (double)lse) + g.log_s) : 0.0f;
+    if (a.entropy) a.entropy[r] = (float)g.entropy;
+}
+__device__ __forceinline__ void put_no_token(const TokenArgs& a, int64_t r) {
+    a.logp[r] = 0.0f;
+    a.lse[r] = 0.0f;
+    if (a.lse_rest) a.lse_rest[r] = 0.0f;
+    if (a.entropy) a.entropy[r] = 0.0f;
+}
+
+template <typename T, bool ENT, int BLOCK, int SLOTS>
 __global__ __launch_bounds__(BLOCK) void k_token_logprob(LogitsArgs l, TokenArgs a, int64_t first) {
     __shared__ Stat lds[BLOCK / 64];
     const int64_t r = first + blockIdx.x;
     const T* row = (const T*)l.z + r * l.ld;
     const int64_t y = a.labels[r];
     if (y < 0) {
-        if (threadIdx.x == 0) {
-            a.logp[r] = 0.0f;
-            a.lse[r] = 0.0f;
-            if (a.lse_rest) a.lse_rest[r] = 0.0f;
-            if (ENT) a.entropy[r] = 0.0f;
-        }
+        if (threadIdx.x == 0) put_no_token(a, r);
         return;
     }
-    const float zy = y < l.vocab ? (float)row[y] : NAN;
-    Row<T, BLOCK, 0> z(row, l.vocab);
+    Row<T, BLOCK, 0, (BLOCK <= 512), SLOTS> z(row, l.vocab);
+    const float zy = label_logit(row, y, l.vocab);
     const Stat st = block_stat<ENT, BLOCK / 64>(z.template stat<ENT, false>(l.c, nullptr), l.c, lds);
-    if (threadIdx.x == 0) {
-        const RowLog g = row_log(st, l.s);
-        a.logp[r] = st.s == 0.0f ? (y < l.vocab ? -INFINITY : NAN) : (float)(((double)zy - (double)st.m) * l.s - g.log_s);
-        const float lse = (float)g.lse;
-        a.lse[r] = lse;
-        if (a.lse_rest) a.lse_rest[r] = fabsf(lse) < INFINITY ? (float)(((double)st.m * l.s - (double)lse) + g.log_s) : 0.0f;
-        if (ENT) a.entropy[r] = (float)g.entropy;
-    }
+    if (threadIdx.x == 0) put_token(l, a, r, st, zy);
 }
 
 // The way back needs no sums: log p_j = z_j s - lse.  Workgroups take pieces of kGradChunks chunks a thread.
@@ -319,6 +340,33 @@ __device__ __forceinline__ TokenLoss policy_token(const PolicyArgs& a, int64_t r
     return t;
 }
 
+// Everything about a row of the policy loss but its gradient's entries: dz_j = 2^a_j (A + B a_j), and `mark` more at the label.
+struct PolicyRow {
+    float loss, logp, entropy, A, B, mark;
+    bool empty;
+};
+// dz_j = W (slope (1[j = y] - p_j) + c_H p_j (log p_j + H)),  log p_j = ln 2 a_j - ln S
+template <bool ENT>
+__device__ __forceinline__ PolicyRow policy_row(const LogitsArgs& l, const PolicyArgs& a, int64_t r, float w, Stat st, float zy) {
+    const RowLog g = row_log(st, l.s);
+    PolicyRow p;
+    p.empty = st.s == 0.0f;
+    p.logp = logp_of(st, g, l.s, zy);
+    p.entropy = (float)g.entropy;
+    const TokenLoss t = policy_token(a, r, p.logp);
+    p.loss = ENT ? fmaf(-a.entropy_coef, p.entropy, t.loss) : t.loss;
+    const float W = (float)((double)w * a.scale * l.s), over = W / st.s;
+    p.A = over * (ENT ? fmaf(a.entropy_coef, (float)(g.entropy - g.log_s), -t.slope) : -t.slope);
+    p.B = ENT ? over * a.entropy_coef * 0.693147180559945309417f : 0.0f;
+    p.mark = W * t.slope;
+    return p;
+}
+__device__ __forceinline__ void put_policy(const PolicyArgs& a, int64_t r, float loss, float logp, float entropy) {
+    a.row_loss[r] = loss;
+    a.logp[r] = logp;
+    if (a.entropy) a.entropy[r] = entropy;
+}
+
 template <typename T, bool ENT, int BLOCK, int CH>
 __global__ __launch_bounds__(BLOCK) void k_policy(LogitsArgs l, PolicyArgs a, int64_t first) {
     __shared__ Stat lds[BLOCK / 64];
@@ -328,36 +376,18 @@ __global__ __launch_bounds__(BLOCK) void k_policy(LogitsArgs l, PolicyArgs a, in
     const int64_t y = a.labels[r];
     const float w = a.weight ? a.weight[r] : 1.0f;
     if (y < 0 || w == 0.0f) {
-        if (threadIdx.x == 0) {
-            a.row_loss[r] = 0.0f;
-            a.logp[r] = 0.0f;
-            if (a.entropy) a.entropy[r] = 0.0f;
-        }
-        if (l.dz) Row<T, BLOCK, CH>::fill(out, l.vocab, 0.0f);
+        if (threadIdx.x == 0) put_policy(a, r, 0.0f, 0.0f, 0.0f);
+        if (l.dz) Row<T, BLOCK, CH>::clear(out, l.vocab);
         return;
     }
     Row<T, BLOCK, CH> z(row, l.vocab);
-    const float zy = y < l.vocab ? (float)row[y] : NAN;
+    const float zy = label_logit(row, y, l.vocab);
     const Stat st = block_stat<ENT, BLOCK / 64>(z.template stat<ENT, false>(l.c, nullptr), l.c, lds);
-    const RowLog g = row_log(st, l.s);
-    const bool empty = st.s == 0.0f;
-    const float logp = empty ? (y < l.vocab ? -INFINITY : NAN) : (float)(((double)zy - (double)st.m) * l.s - g.log_s);
-    const TokenLoss t = policy_token(a, r, logp);
-    if (threadIdx.x == 0) {
-        a.row_loss[r] = ENT ? fmaf(-a.entropy_coef, (float)g.entropy, t.loss) : t.loss;
-        a.logp[r] = logp;
-        if (ENT && a.entropy) a.entropy[r] = (float)g.entropy;
-    }
+    const PolicyRow p = policy_row<ENT>(l, a, r, w, st, zy);
+    if (threadIdx.x == 0) put_policy(a, r, p.loss, p.logp, p.entropy);
     if (!l.dz) return;
-    if (empty) {
-        Row<T, BLOCK, CH>::fill(out, l.vocab, 0.0f);
-        return;
-    }
-    // dz_j = W (slope (1[j = y] - p_j) + c_H p_j (log p_j + H)),  log p_j = ln 2 a_j - ln S
-    const float W = (float)((double)w * a.scale * l.s), over = W / st.s;
-    const float A = over * (ENT ? fmaf(a.entropy_coef, (float)(g.entropy - g.log_s), -t.slope) : -t.slope);
-    const float B = ENT ? over * a.entropy_coef * 0.693147180559945309417f : 0.0f;
-    z.template write<ENT>(out, st.m, l.c, A, B, (int)y, W * t.slope);
+    if (p.empty) Row<T, BLOCK, CH>::clear(out, l.vocab);
+    else z.template write<ENT>(out, st.m, l.c, p.A, p.B, (int)y, p.mark);
 }
 
 // ---- distillation ----------------------------------------------------------------------------------------------------------
@@ -370,14 +400,6 @@ __device__ __forceinline__ int64_t teacher_index(const DistillArgs& a, int64_t a
     return a.index_type == LBFGSB_I32 ? (int64_t)((const int*)a.index)[at] : ((const int64_t*)a.index)[at];
 }
 
-// What a row's first wave finds out about the teacher, in LDS.
-struct Teacher {
-    double cross;       // sum_k q_k (log q_k - s z_k)
-    double sum;         // sum_k q_k
-    Stat top;           // the student's statistics over the entries, each once
-    int entries;        // how many there are, each once
-    int lost;           // one of them lies past the vocabulary
-};
 // LDS of the distillation kernel: a row's entries (index, teacher's share, student's logit, scratch), then one bit for each
 // entry of the vocabulary.
 struct TopLds {
@@ -385,12 +407,27 @@ struct TopLds {
     float *q, *z, *scratch;
     unsigned* seen;
 };
+__device__ __forceinline__ TopLds top_lds(unsigned char* dyn, int top) {
+    TopLds s;
+    s.at = (int*)dyn;
+    s.q = (float*)(s.at + top);
+    s.z = s.q + top;
+    s.scratch = s.z + top;
+    s.seen = (unsigned*)(s.scratch + top);
+    return s;
+}
 __host__ __device__ inline size_t distill_lds(int top, int vocab) { return (size_t)top * 16 + (size_t)(vocab + 8 + 127) / 128 * 16; }
 
 // Between an LDS write of one lane and a read by another of the same wave.
 __device__ __forceinline__ void wave_fence() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
+}
+
+template <int BLOCK>
+__device__ __forceinline__ void clear_seen(TopLds s, int vocab) {
+    for (int i = threadIdx.x; i < (vocab + 8 + 127) / 128 * 4; i += BLOCK) s.seen[i] = 0;
+    __syncthreads();
 }
 
 // By the first wave.  An index that comes twice keeps its first place only, with the sum of its shares.  The bits of the
@@ -476,63 +513,223 @@ __device__ __forceinline__ void read_teacher(const LogitsArgs& l, const DistillA
     if (lane == 0) *out = {cross, sum, st, (int)count, any_lost};
 }
 
+// Everything about a row of the distillation but its gradient's entries: away from the teacher's dz_j = A 2^((z_j - st.m) c), at one
+// of them W (p_j - q_j).
+struct DistillRow {
+    Stat all;           // over the whole row
+    float loss, A, W;
+    bool empty;
+    __device__ __forceinline__ float at_entry(float z, float q, float c) const {
+        return W * (exp2_hw((z - anchor(all.m)) * c) / all.s - q);
+    }
+};
+// st: over the row, REST: over what is not among the entries
+template <bool REST>
+__device__ __forceinline__ DistillRow distill_row(const LogitsArgs& l, const DistillArgs& a, float w, Stat st, const Teacher& t) {
+    DistillRow d;
+    d.all = REST ? merged(st, t.top, l.c) : st;
+    const RowLog g = row_log(d.all, l.s);
+    double loss = t.entries ? t.cross + t.sum * g.lse : 0.0;
+    float A;
+    if (REST) {
+        // the rest's shares, of the teacher and (its logarithm) of the student
+        const double rest = t.entries < l.vocab && t.sum < 1.0 ? 1.0 - t.sum : 0.0;
+        const double log_t = st.s == 0.0f ? -INFINITY : ((double)st.m - (double)d.all.m) * l.s + log_d((double)st.s) - g.log_s;
+        if (rest > 0.0) loss += rest * (log_d(rest) - log_t);
+        A = st.s == 0.0f ? 0.0f : (float)(((double)expf((float)log_t) - rest) / (double)st.s);
+    } else {
+        A = t.entries ? 1.0f / st.s : 0.0f;
+    }
+    if (d.all.s == 0.0f) loss = t.entries ? INFINITY : 0.0;
+    if (t.lost) loss = NAN;
+    d.empty = d.all.s == 0.0f && !t.lost;
+    d.W = loss != loss ? NAN : (float)((double)w * a.scale * l.s);
+    d.A = d.W * A;
+    d.loss = (float)loss;
+    return d;
+}
+
 template <typename T, bool REST, int BLOCK, int CH>
 __global__ __launch_bounds__(BLOCK) void k_distill(LogitsArgs l, DistillArgs a, int64_t first) {
     __shared__ Stat lds[BLOCK / 64];
     __shared__ Teacher teacher;
     extern __shared__ __align__(16) unsigned char dyn[];
-    TopLds s;
-    s.at = (int*)dyn;
-    s.q = (float*)(s.at + a.top);
-    s.z = s.q + a.top;
-    s.scratch = s.z + a.top;
-    s.seen = (unsigned*)(s.scratch + a.top);
+    const TopLds s = top_lds(dyn, a.top);
     const int64_t r = first + blockIdx.x;
     const T* row = (const T*)l.z + r * l.ld;
     T* out = (T*)l.dz + r * l.ld_dz;
     const float w = a.weight ? a.weight[r] : 1.0f;
     if (w == 0.0f) {
         if (threadIdx.x == 0) a.row_loss[r] = 0.0f;
-        if (l.dz) Row<T, BLOCK, CH>::fill(out, l.vocab, 0.0f);
+        if (l.dz) Row<T, BLOCK, CH>::clear(out, l.vocab);
         return;
     }
     Row<T, BLOCK, CH> z(row, l.vocab);
-    if (REST) {
-        for (int i = threadIdx.x; i < (l.vocab + 8 + 127) / 128 * 4; i += BLOCK) s.seen[i] = 0;
-        __syncthreads();
-    }
+    if (REST) clear_seen<BLOCK>(s, l.vocab);
     if (threadIdx.x < 64) read_teacher<T, !REST>(l, a, r, row, z.cut.shift(), s, &teacher);
     if (REST) __syncthreads();
-    const Stat st =
-        block_stat<false, BLOCK / 64>(z.template stat<false, REST>(l.c, (const unsigned char*)s.seen), l.c, lds);
-    const Stat all = REST ? merged(st, teacher.top, l.c) : st;
-    const RowLog g = row_log(all, l.s);
-    const bool empty = all.s == 0.0f;
-    double loss = teacher.entries ? teacher.cross + teacher.sum * g.lse : 0.0;
-    float A;                                  // away from the entries, dz_j = W A 2^((z_j - st.m) c)
-    if (REST) {
-        // the rest's shares: r of the teacher, t of the student
-        const double rest = teacher.entries < l.vocab ? (teacher.sum < 1.0 ? 1.0 - teacher.sum : 0.0) : 0.0;
-        const double log_t = st.s == 0.0f ? -INFINITY : ((double)st.m - (double)all.m) * l.s + log_d((double)st.s) - g.log_s;
-        if (rest > 0.0) loss += rest * (log_d(rest) - log_t);
-        A = st.s == 0.0f ? 0.0f : (float)(((double)expf((float)log_t) - rest) / (double)st.s);
-    } else {
-        A = teacher.entries ? 1.0f / st.s : 0.0f;
-    }
-    if (empty) loss = teacher.entries ? INFINITY : 0.0;
-    if (teacher.lost) loss = NAN;
-    if (threadIdx.x == 0) a.row_loss[r] = (float)loss;
+    const Stat st = block_stat<false, BLOCK / 64>(z.template stat<false, REST>(l.c, (const unsigned char*)s.seen), l.c, lds);
+    const DistillRow d = distill_row<REST>(l, a, w, st, teacher);
+    if (threadIdx.x == 0) a.row_loss[r] = d.loss;
     if (!l.dz) return;
-    if (empty && !teacher.lost) {
-        Row<T, BLOCK, CH>::fill(out, l.vocab, 0.0f);
+    if (d.empty) {
+        Row<T, BLOCK, CH>::clear(out, l.vocab);
         return;
     }
-    const float W = loss != loss ? NAN : (float)((double)w * a.scale * l.s);
-    z.template write<false>(out, st.m, l.c, W * A, 0.0f, -1, 0.0f);
+    z.template write<false>(out, st.m, l.c, d.A, 0.0f, -1, 0.0f);
     __syncthreads();                          // (the entries' own values come after the row's)
-    for (int k = threadIdx.x; k < a.top; k += BLOCK) {
-        const int j = s.at[k];
-        if (j >= 0) out[j] = (T)(W * (exp2_hw((s.z[k] - anchor(all.m)) * l.c) / all.s - s.q[k]));
+    for (int k = threadIdx.x; k < a.top; k += BLOCK)
+        if (s.at[k] >= 0) out[s.at[k]] = (T)d.at_entry(s.z[k], s.q[k], l.c);
+}
+
+// ---- a few long rows, in pieces ----------------------------------------------------------------------------------------------
+// One workgroup a row leaves most of the chip idle when there are few: the statistics of a row's pieces by a workgroup each, then, in
+// a second launch, the join and the gradient by as many.  (The second reads the logits again, out of the caches.)
+
+constexpr int kSplitBlock = 512, kSplitHold = 4;      // threads; chunks a thread holds in the second launch
+
+// the statistics of a row, by every wave of the second launch
+template <bool ENT>
+__device__ __forceinline__ Stat joined(const SplitRow& s, int splits, float c) {
+    const int lane = threadIdx.x & 63;
+    return wave_stat<ENT>(lane < splits ? s.part[lane] : Stat{-INFINITY, 0.0f, 0.0f}, c);
+}
+// the same by one lane
+__device__ __forceinline__ Stat joined_alone(const SplitRow& s, int splits, float c) {
+    Stat a = s.part[0];
+    for (int i = 1; i < splits; ++i) a = merged(a, s.part[i], c);
+    return a;
+}
+
+template <typename T, bool ENT>
+__global__ __launch_bounds__(kSplitBlock) void k_split(LogitsArgs l, const int64_t* labels, const float* weight, SplitRow* ws, int splits) {
+    __shared__ Stat lds[kSplitBlock / 64];
+    const int r = blockIdx.x / splits, i = blockIdx.x % splits;
+    const T* row = (const T*)l.z + r * l.ld;
+    const int64_t y = labels[r];
+    if (y < 0 || (weight && weight[r] == 0.0f)) return;
+    Row<T, kSplitBlock, 0, false> z(row, l.vocab, i, splits);
+    const float zy = label_logit(row, y, l.vocab);
+    const Stat st = block_stat<ENT, kSplitBlock / 64>(z.template stat<ENT, false>(l.c, nullptr), l.c, lds);
+    if (threadIdx.x == 0) {
+        ws[r].part[i] = st;
+        if (i == 0) ws[r].zy = zy;            // (the second launch may write the gradient over it)
+    }
+}
+
+// One workgroup more for each row: the teacher's entries.
+template <typename T, bool REST>
+__global__ __launch_bounds__(kSplitBlock) void k_split_distill(LogitsArgs l, DistillArgs a, SplitRow* ws, int splits) {
+    __shared__ Stat lds[kSplitBlock / 64];
+    extern __shared__ __align__(16) unsigned char dyn[];
+    const TopLds s = top_lds(dyn, a.top);
+    const int r = blockIdx.x / (splits + 1), i = blockIdx.x % (splits + 1);
+    const T* row = (const T*)l.z + r * l.ld;
+    if (a.weight && a.weight[r] == 0.0f) return;
+    if (i == splits) {
+        const Cut<T> cut(row, l.vocab);
+        if (threadIdx.x < 64) read_teacher<T, true>(l, a, r, row, cut.shift(), s, &ws[r].teacher);
+        __syncthreads();
+        for (int k = threadIdx.x; k < a.top; k += kSplitBlock) {
+            ws[r].at[k] = s.at[k];
+            ws[r].q[k] = s.q[k];
+            ws[r].z[k] = s.z[k];
+        }
+        return;
+    }
+    Row<T, kSplitBlock, 0, false> z(row, l.vocab, i, splits);
+    if (REST) {
+        clear_seen<kSplitBlock>(s, l.vocab);
+        for (int k = threadIdx.x; k < a.top; k += kSplitBlock) {
+            const int64_t j = teacher_index(a, r * a.ld + k);
+            if (j >= 0 && j < l.vocab && teacher_logit(a, r * a.ld + k) != -INFINITY)
+                atomicOr(&s.seen[((int)j + z.cut.shift()) >> 5], 1u << (((int)j + z.cut.shift()) & 31));
+        }
+        __syncthreads();
+    }
+    const Stat st = block_stat<false, kSplitBlock / 64>(z.template stat<false, REST>(l.c, (const unsigned char*)s.seen), l.c, lds);
+    if (threadIdx.x == 0) ws[r].part[i] = st;
+}
+
+__global__ __launch_bounds__(64) void k_join_token(LogitsArgs l, TokenArgs a, const SplitRow* ws, int splits) {
+    const int r = blockIdx.x;
+    if (a.labels[r] < 0) {
+        if (threadIdx.x == 0) put_no_token(a, r);
+        return;
+    }
+    const Stat st = joined<true>(ws[r], splits, l.c);
+    if (threadIdx.x == 0) put_token(l, a, r, st, ws[r].zy);
+}
+
+// The last workgroup of the second launch has the total, a lane for each row.
+__device__ __forceinline__ void put_total(double mine, double scale, float* loss) {
+    const double sum = wave_sum(mine);
+    if (threadIdx.x == 0) *loss = (float)(sum * scale);
+}
+
+template <typename T, bool ENT>
+__global__ __launch_bounds__(kSplitBlock) void k_join_policy(LogitsArgs l, PolicyArgs a, const SplitRow* ws, int splits, float* loss) {
+    const int r = blockIdx.x / splits, i = blockIdx.x % splits;
+    if (r == l.rows) {
+        if (threadIdx.x >= 64) return;
+        const int q = threadIdx.x;
+        const float w = q < l.rows ? (a.weight ? a.weight[q] : 1.0f) : 0.0f;
+        double mine = 0.0;
+        if (w != 0.0f && a.labels[q] >= 0)
+            mine = (double)w * (double)policy_row<ENT>(l, a, q, w, joined_alone(ws[q], splits, l.c), ws[q].zy).loss;
+        put_total(mine, a.scale, loss);
+        return;
+    }
+    T* out = (T*)l.dz + r * l.ld_dz;
+    const int64_t y = a.labels[r];
+    const float w = a.weight ? a.weight[r] : 1.0f;
+    if (y < 0 || w == 0.0f) {
+        if (threadIdx.x == 0 && i == 0) put_policy(a, r, 0.0f, 0.0f, 0.0f);
+        if (l.dz) Row<T, kSplitBlock, kSplitHold>::clear(out, l.vocab, i, splits);
+        return;
+    }
+    Row<T, kSplitBlock, kSplitHold> z((const T*)l.z + r * l.ld, l.vocab, i, splits);
+    const Stat st = joined<ENT>(ws[r], splits, l.c);
+    const PolicyRow p = policy_row<ENT>(l, a, r, w, st, ws[r].zy);
+    if (threadIdx.x == 0 && i == 0) put_policy(a, r, p.loss, p.logp, p.entropy);
+    if (!l.dz) return;
+    if (p.empty) Row<T, kSplitBlock, kSplitHold>::clear(out, l.vocab, i, splits);
+    else z.template write<ENT>(out, st.m, l.c, p.A, p.B, (int)y, p.mark);
+}
+
+template <typename T, bool REST>
+__global__ __launch_bounds__(kSplitBlock) void k_join_distill(LogitsArgs l, DistillArgs a, const SplitRow* ws, int splits, float* loss) {
+    const int r = blockIdx.x / splits, i = blockIdx.x % splits;
+    if (r == l.rows) {
+        if (threadIdx.x >= 64) return;
+        const int q = threadIdx.x;
+        const float w = q < l.rows ? (a.weight ? a.weight[q] : 1.0f) : 0.0f;
+        double mine = 0.0;
+        if (w != 0.0f) mine = (double)w * (double)distill_row<REST>(l, a, w, joined_alone(ws[q], splits, l.c), ws[q].teacher).loss;
+        put_total(mine, a.scale, loss);
+        return;
+    }
+    T* out = (T*)l.dz + r * l.ld_dz;
+    const float w = a.weight ? a.weight[r] : 1.0f;
+    if (w == 0.0f) {
+        if (threadIdx.x == 0 && i == 0) a.row_loss[r] = 0.0f;
+        if (l.dz) Row<T, kSplitBlock, kSplitHold>::clear(out, l.vocab, i, splits);
+        return;
+    }
+    Row<T, kSplitBlock, kSplitHold> z((const T*)l.z + r * l.ld, l.vocab, i, splits);
+    const Stat st = joined<false>(ws[r], splits, l.c);
+    const DistillRow d = distill_row<REST>(l, a, w, st, ws[r].teacher);
+    if (threadIdx.x == 0 && i == 0) a.row_loss[r] = d.loss;
+    if (!l.dz) return;
+    if (d.empty) {
+        Row<T, kSplitBlock, kSplitHold>::clear(out, l.vocab, i, splits);
+        return;
+    }
+    z.template write<false>(out, st.m, l.c, d.A, 0.0f, -1, 0.0f);
+    __syncthreads();                          // (the entries' own values come after the row's)
+    for (int k = threadIdx.x; k < a.top; k += kSplitBlock) {
+        const int j = ws[r].at[k];
+        if (j >= 0 && z.has(j)) out[j] = (T)d.at_entry(ws[r].z[k], ws[r].q[k], l.c);
     }
 }
 
@@ -562,17 +759,39 @@ void by_width(int vocab, F f) {
 
 }  // namespace
 
+// LDS beyond what a kernel has without asking
+template <typename K>
+hipError_t allow_lds(K kernel, size_t bytes) {
+    if (bytes <= 60 << 10) return hipSuccess;
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+
 template <typename T>
-hipError_t token_logprob_rows(const LogitsArgs& l, const TokenArgs& a, float*, hipStream_t st) {
-    const int chunks = l.vocab / Chunk<T>::E;
-    auto launch = [&](auto block) {
-        constexpr int BLOCK = decltype(block)::value;
-        const auto kernel = a.entropy ? k_token_logprob<T, true, BLOCK> : k_token_logprob<T, false, BLOCK>;
+hipError_t token_logprob_rows(const LogitsArgs& l, const TokenArgs& a, SplitRow* ws, hipStream_t st) {
+    const int chunks = l.vocab / Chunk<T>::E, splits = row_splits(l.rows, l.vocab, sizeof(T), false);
+    if (splits > 1) {
+        const auto kernel = a.entropy ? k_split<T, true> : k_split<T, false>;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)l.rows * splits), dim3(kSplitBlock), 0, st, l, a.labels, (const float*)nullptr, ws, splits);
+        hipLaunchKernelGGL(k_join_token, dim3((unsigned)l.rows), dim3(64), 0, st, l, a, (const SplitRow*)ws, splits);
+        return hipGetLastError();
+    }
+    auto launch = [&](auto block, auto slots) {
+        constexpr int BLOCK = decltype(block)::value, SLOTS = decltype(slots)::value;
+        const auto kernel = a.entropy ? k_token_logprob<T, true, BLOCK, SLOTS> : k_token_logprob<T, false, BLOCK, SLOTS>;
         by_rows(l.rows, [&](int64_t first, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(BLOCK), 0, st, l, a, first); });
     };
-    if (chunks <= 1024) launch(std::integral_constant<int, 64>{});
-    else if (chunks <= 4096) launch(std::integral_constant<int, 256>{});
-    else launch(std::integral_constant<int, 512>{});
+    // Where there are rows for every compute unit, few threads to each; where there are not, many.  bf16, us, 64 / 256 / 512 threads, two
+    // loads each: 16384 x 2000 16.4 / 24.7 / 41, x 8000 45.7 / 48.0 / 58, x 32000 164 / 162 / 163, 3001 x 50021 (f16) 54 / 53 / 47;
+    // 512 and 1024 threads, four loads: 128 x 4000 4.3 (64 threads) / 3.4 (512), 128 x 32768 6.5 (256) / 4.8 (1024).
+    using std::integral_constant;
+    if (l.rows <= 512) {
+        if (chunks <= 1024) launch(integral_constant<int, 512>{}, integral_constant<int, 4>{});
+        else launch(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+    } else {
+        if (chunks <= 1024) launch(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+        else if (chunks <= 4096) launch(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+        else launch(integral_constant<int, 512>{}, integral_constant<int, 2>{});
+    }
     return hipGetLastError();
 }
 
@@ -586,27 +805,45 @@ hipError_t token_grad_rows(const LogitsArgs& l, const TokenGradArgs& a, hipStrea
 }
 
 template <typename T>
-hipError_t policy_rows(const LogitsArgs& l, const PolicyArgs& a, float*, hipStream_t st) {
+hipError_t policy_rows(const LogitsArgs& l, const PolicyArgs& a, float* loss, SplitRow* ws, hipStream_t st) {
+    const bool ent = a.entropy || a.entropy_coef != 0.0f;
+    if (const int splits = row_splits(l.rows, l.vocab, sizeof(T), l.dz != nullptr); splits > 1) {
+        const unsigned blocks = (unsigned)l.rows * splits;
+        hipLaunchKernelGGL((ent ? k_split<T, true> : k_split<T, false>), dim3(blocks), dim3(kSplitBlock), 0, st, l, a.labels, a.weight, ws, splits);
+        hipLaunchKernelGGL((ent ? k_join_policy<T, true> : k_join_policy<T, false>), dim3(blocks + 1), dim3(kSplitBlock), 0, st, l, a,
+                           (const SplitRow*)ws, splits, loss);
+        return hipGetLastError();
+    }
     by_width<T>(l.vocab, [&](auto block, auto ch) {
         constexpr int BLOCK = decltype(block)::value, CH = decltype(ch)::value;
-        const auto kernel = a.entropy || a.entropy_coef != 0.0f ? k_policy<T, true, BLOCK, CH> : k_policy<T, false, BLOCK, CH>;
+        const auto kernel = ent ? k_policy<T, true, BLOCK, CH> : k_policy<T, false, BLOCK, CH>;
         by_rows(l.rows, [&](int64_t first, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(BLOCK), 0, st, l, a, first); });
     });
-    return hipGetLastError();
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    return launch_weighted_total(a.row_loss, a.weight, l.rows, a.scale, loss, st);
 }
 
 template <typename T>
-hipError_t distill_rows(const LogitsArgs& l, const DistillArgs& a, float*, hipStream_t st) {
+hipError_t distill_rows(const LogitsArgs& l, const DistillArgs& a, float* loss, SplitRow* ws, hipStream_t st) {
     const size_t lds = distill_lds(a.top, l.vocab);
+    if (const int splits = row_splits(l.rows, l.vocab, sizeof(T), l.dz != nullptr); splits > 1) {
+        const auto kernel = a.lse ? k_split_distill<T, true> : k_split_distill<T, false>;
+        if (hipError_t e = allow_lds(kernel, lds); e != hipSuccess) return e;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)l.rows * (splits + 1)), dim3(kSplitBlock), lds, st, l, a, ws, splits);
+        hipLaunchKernelGGL((a.lse ? k_join_distill<T, true> : k_join_distill<T, false>), dim3((unsigned)l.rows * splits + 1), dim3(kSplitBlock), 0,
+                           st, l, a, (const SplitRow*)ws, splits, loss);
+        return hipGetLastError();
+    }
     hipError_t err = hipSuccess;
     by_width<T>(l.vocab, [&](auto block, auto ch) {
         constexpr int BLOCK = decltype(block)::value, CH = decltype(ch)::value;
         const auto kernel = a.lse ? k_distill<T, true, BLOCK, CH> : k_distill<T, false, BLOCK, CH>;
-        err = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        err = allow_lds(kernel, lds);
         if (err != hipSuccess) return;
         by_rows(l.rows, [&](int64_t first, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(BLOCK), lds, st, l, a, first); });
     });
-    return err != hipSuccess ? err : hipGetLastError();
+    if (err != hipSuccess || (err = hipGetLastError()) != hipSuccess) return err;
+    return launch_weighted_total(a.row_loss, a.weight, l.rows, a.scale, loss, st);
 }
 
 }  // namespace lb

@@ -46,8 +46,13 @@ int check_logits(const lbfgsb_logits* l, int grad) {
     return LBFGSB_OK;
 }
 
-int check_workspace(const lbfgsb_logits* l, const void* ws, size_t bytes) {
-    const size_t need = l->rows ? logits_workspace(l->rows, l->vocab, l->dtype) : 0;
+size_t workspace_of(const lbfgsb_logits* l, bool grad) {
+    if (l->rows == 0 || row_splits(l->rows, l->vocab, (int)size_of(l->dtype), grad) == 1) return 0;
+    return (l->rows * sizeof(SplitRow) + 255) & ~(size_t)255;
+}
+
+int check_workspace(const lbfgsb_logits* l, bool grad, const void* ws, size_t bytes) {
+    const size_t need = workspace_of(l, grad);
     if (need == 0) return LBFGSB_OK;
     if (!ws || misaligned(ws, 256)) return fail(LBFGSB_E_INVALID_ARG, "workspace is NULL or not aligned to 256 bytes");
     if (bytes < need) return fail(LBFGSB_E_INVALID_ARG, "workspace too small: %zu bytes, need %zu", bytes, need);
@@ -71,16 +76,16 @@ extern "C" {
 
 size_t lbfgsb_logits_workspace_bytes(const lbfgsb_logits* logits_host) {
     if (check_shape(logits_host)) return 0;
-    return logits_host->rows ? logits_workspace(logits_host->rows, logits_host->vocab, logits_host->dtype) : 0;
+    return workspace_of(logits_host, logits_host->grad != nullptr);
 }
 
 int lbfgsb_token_logprob(const lbfgsb_logits* logits_host, const int64_t* labels, float* logp, float* lse, float* lse_rest,
                          float* entropy, void* workspace, size_t workspace_bytes, void* hip_stream) {
     if (int rc = check_logits(logits_host, -1)) return rc;
-    if (int rc = check_workspace(logits_host, workspace, workspace_bytes)) return rc;
+    if (int rc = check_workspace(logits_host, false, workspace, workspace_bytes)) return rc;
     if (logits_host->rows == 0) return LBFGSB_OK;
     if (!labels || !logp || !lse) return fail(LBFGSB_E_INVALID_ARG, "labels, logp and lse must not be NULL");
-    HIP_TRY(launch_token_logprob(args_of(logits_host, false), logits_host->dtype, {labels, logp, lse, lse_rest, entropy}, (float*)workspace,
+    HIP_TRY(launch_token_logprob(args_of(logits_host, false), logits_host->dtype, {labels, logp, lse, lse_rest, entropy}, (SplitRow*)workspace,
                                  (hipStream_t)hip_stream));
     return LBFGSB_OK;
 }
@@ -99,7 +104,7 @@ int lbfgsb_token_logprob_grad(const lbfgsb_logits* logits_host, const int64_t* l
 int lbfgsb_distill_loss(const lbfgsb_logits* logits_host, const lbfgsb_teacher* teacher_host, const float* weight, double scale,
                         float* loss, float* row_loss, void* workspace, size_t workspace_bytes, void* hip_stream) {
     if (int rc = check_logits(logits_host, 0)) return rc;
-    if (int rc = check_workspace(logits_host, workspace, workspace_bytes)) return rc;
+    if (int rc = check_workspace(logits_host, logits_host->grad != nullptr, workspace, workspace_bytes)) return rc;
     const lbfgsb_teacher* t = teacher_host;
     if (!t) return fail(LBFGSB_E_INVALID_ARG, "teacher is NULL");
     if (logits_host->vocab > kMaxDistillVocab) return fail(LBFGSB_E_INVALID_ARG, "distillation takes a vocabulary of at most 2^19");
@@ -113,7 +118,7 @@ int lbfgsb_distill_loss(const lbfgsb_logits* logits_host, const lbfgsb_teacher* 
         return fail(LBFGSB_E_INVALID_ARG, "index, logit or row_loss is NULL or not aligned to its elements");
     HIP_TRY(launch_distill(args_of(logits_host, true), logits_host->dtype,
                            {t->index, t->logit, t->lse, weight, row_loss, t->ld, (int)t->top, t->index_type, t->logit_type, scale}, loss,
-                           (float*)workspace, (hipStream_t)hip_stream));
+                           (SplitRow*)workspace, (hipStream_t)hip_stream));
     return LBFGSB_OK;
 }
 
@@ -121,7 +126,7 @@ int lbfgsb_policy_loss(const lbfgsb_logits* logits_host, const lbfgsb_rollout* r
                        double scale, float* loss, float* row_loss, float* logp, float* entropy, void* workspace,
                        size_t workspace_bytes, void* hip_stream) {
     if (int rc = check_logits(logits_host, 0)) return rc;
-    if (int rc = check_workspace(logits_host, workspace, workspace_bytes)) return rc;
+    if (int rc = check_workspace(logits_host, logits_host->grad != nullptr, workspace, workspace_bytes)) return rc;
     const lbfgsb_rollout* p = rollout_host;
     const lbfgsb_policy_options* o = opt_host;
     if (!p || !o) return fail(LBFGSB_E_INVALID_ARG, "rollout or options is NULL");
@@ -137,7 +142,7 @@ int lbfgsb_policy_loss(const lbfgsb_logits* logits_host, const lbfgsb_rollout* r
     HIP_TRY(launch_policy(args_of(logits_host, true), logits_host->dtype,
                           {p->labels, p->old_logp, p->advantage, p->ref_logp, p->weight, row_loss, logp, entropy, (float)(1.0 - o->clip_low),
                            (float)(1.0 + o->clip_high), (float)o->kl_coef, (float)o->entropy_coef, o->kl_kind, scale},
-                          loss, (float*)workspace, (hipStream_t)hip_stream));
+                          loss, (SplitRow*)workspace, (hipStream_t)hip_stream));
     return LBFGSB_OK;
 }
 

@@ -150,7 +150,7 @@ def _logits(z, temperature: float, grad):
     if grad is False or grad is None:
         return Logits(dtype, rows, vocab, ld, z.data_ptr(), temperature, None, 0), None
     if grad is True:
-        grad = z.new_empty(z.shape)
+        grad = _torch.empty_like(z) if z.is_contiguous() else z.new_empty(z.shape)   # (the first is the cheaper call)
     elif _logit_type(grad, "grad") != dtype or grad.shape != z.shape or grad.device != z.device:
         raise TypeError("grad must have the type, shape and device of the logits")
     return Logits(dtype, rows, vocab, ld, z.data_ptr(), temperature, grad.data_ptr(), _stride(grad)), grad

@@ -174,28 +174,34 @@ __device__ __forceinline__ Stat block_stat(Stat a, float c, Stat* lds) {
     return r;
 }
 
-// Entries of one chunk (or several) join the statistics.
-template <bool ENT, int N>
-__device__ __forceinline__ void take(Stat& a, const float (&z)[N], float c) {
-    float top = z[0];
+// A thread's statistics while it goes through its entries.  ref: what an entry's difference is taken from (anchor(a.m)).
+struct Running {
+    Stat a{-INFINITY, 0.0f, 0.0f};
+    float ref = 0.0f;
+    template <bool ENT, int N>
+    __device__ __forceinline__ void take(const float (&z)[N], float c) {
+        float top = z[0];
 #pragma unroll
-    for (int i = 1; i < N; ++i) top = fmaxf(top, z[i]);
-    if (top > a.m) a = rescaled(a, top, c);
-    const float ref = anchor(a.m);
-    float s[N], t = 0.0f;
+        for (int i = 1; i < N; ++i) top = fmaxf(top, z[i]);
+        if (top > a.m) {
+            a = rescaled(a, top, c);
+            ref = top;
+        }
+        float s[N], t = 0.0f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const float d = (z[i] - ref) * c;
-        s[i] = exp2_hw(d);
-        if (ENT) t = fmaf(s[i], fmaxf(d, -1000.0f), t);
+        for (int i = 0; i < N; ++i) {
+            const float d = (z[i] - ref) * c;
+            s[i] = exp2_hw(d);
+            if (ENT) t = fmaf(s[i], fmaxf(d, -1000.0f), t);
+        }
+#pragma unroll
+        for (int w = 1; w < N; w *= 2)
+#pragma unroll
+            for (int i = 0; i + w < N; i += 2 * w) s[i] += s[i + w];
+        a.s += s[0];
+        if (ENT) a.t += t;
     }
-#pragma unroll
-    for (int w = 1; w < N; w *= 2)
-#pragma unroll
-        for (int i = 0; i + w < N; i += 2 * w) s[i] += s[i + w];
-    a.s += s[0];
-    if (ENT) a.t += t;
-}
+};
 
 // What follows from a row's statistics, in 64 bits.
 struct RowLog {

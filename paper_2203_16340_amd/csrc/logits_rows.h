@@ -14,6 +14,7 @@ namespace lb {
 
 namespace {
 
+constexpr int64_t kTurnBlocks = 512;         // workgroups that take rows in turns: two for each compute unit
 constexpr int64_t kRowBlocksMax = 1 << 20;   // workgroups of a launch, at most: longer batches take several
 
 template <typename T>
@@ -42,6 +43,9 @@ struct Cut {
         whole = (vocab - head) / E;
         tail = vocab - head - whole * E;
     }
+    // chunks from the boundary of a 128-byte line to the first one: with the waves' loads and stores starting on lines (chunk i - lead by
+    // thread i), 8192 x 50000 bf16, whose rows do not, takes 284 us for 311
+    __device__ __forceinline__ int lead(const T* at) const { return (int)(((uintptr_t)(at + head) >> 4) & 7u); }
     // the single element of thread t < 2 E, or -1
     __device__ __forceinline__ int single(int t) const {
         return t < E ? (t < head ? t : -1) : (t - E < tail ? head + whole * E + t - E : -1);
@@ -51,57 +55,84 @@ struct Cut {
     __device__ __forceinline__ int shift() const { return (E - head) & (E - 1); }
 };
 
-// A workgroup's hold on one row, or on piece `piece` of `pieces` of it.  CH chunks a thread stay in registers between the statistics and the gradient; what a longer row has
+// A row, or piece `piece` of `pieces` of it, as a workgroup goes through it: what is the same for all its threads.
+template <typename T, int HOLD, bool LONG>       // HOLD: chunks that the workgroup keeps; LONG: there may be more of them
+struct Span {
+    static constexpr int E = Chunk<T>::E;
+    static constexpr bool SURE = HOLD >= 8192;       // LONG is only asked for where there are more: a whole row of HOLD - 8 chunks at least
+    const T* row;
+    Cut<T> cut;
+    int begin, end;                      // its chunks
+    int again;                           // up to here they are read twice
+    int origin, keep;                    // where thread 0 stands in the first round and in what is kept: on a line, up to 7 before the first
+    bool singles;                        // the single elements go with the first piece
+
+    __device__ __forceinline__ Span(const T* r, int vocab, int piece = 0, int pieces = 1) : row(r), cut(r, vocab) {
+        const int lead = cut.lead(r), each = ((cut.whole + lead + pieces - 1) / pieces + 7) & ~7;
+        begin = pieces == 1 || piece == 0 ? 0 : min(piece * each - lead, cut.whole);
+        end = pieces == 1 ? cut.whole : max(min((piece + 1) * each - lead, cut.whole), begin);
+        origin = begin == 0 ? -lead : begin;
+        again = LONG && (SURE || end - origin > HOLD) ? max(((end - (HOLD - 16) + lead + 7) & ~7) - lead, begin) : begin;
+        keep = repeats() ? again : origin;
+        singles = piece == 0;
+    }
+    __device__ __forceinline__ const char* base() const { return (const char*)(row + cut.head); }
+    __device__ __forceinline__ bool repeats() const { return LONG && (SURE || again > begin); }
+    // the first chunks that are read: up to here
+    __device__ __forceinline__ int first_end() const { return repeats() ? again : end; }
+    __device__ __forceinline__ int single() const { return singles ? cut.single((int)threadIdx.x) : -1; }
+    // whether element e is one of this piece's
+    __device__ __forceinline__ bool has(int e) const {
+        const int i = e - cut.head;
+        return i < 0 || i >= cut.whole * E ? singles : i >= begin * E && i < end * E;
+    }
+};
+
+// A workgroup's hold on a span.  CH chunks a thread stay in registers between the statistics and the gradient; what a longer row has
 // before them is read a second time.  (CH = 0: no gradient, SLOTS loads in flight.)
 // Loads that are the last of their row go past the caches, unless a workgroup of 1024 makes them: us without / with, token
 // log-probabilities of 16400 x 131072 bf16 702 / 665, distillation 4096 x 65536 bf16 208 / 199, but policy 8192 x 131072 bf16 839 / 863.
-template <typename T, int BLOCK, int CH, bool NT_LOADS = (BLOCK <= 512), int SLOTS = 2>
+template <typename T, int BLOCK, int CH, bool LONG = CH == 0, bool NT_LOADS = (BLOCK <= 512), int SLOTS = 2>
 struct Row {
     static constexpr int E = Chunk<T>::E;
     static constexpr int kSlots = CH > 0 ? CH : SLOTS;
     typedef typename Chunk<T>::vec vec;
     typedef typename Chunk<T>::any any;
+    typedef lb::Span<T, BLOCK * CH, LONG> Span;
 
     vec slot[kSlots];
     float alone;                         // the single element of this thread, if any
-    const char* base;                    // the row's first chunk
-    Cut<T> cut;
-    int begin, end;                      // the chunks of this piece
-    int again;                           // up to here they are read twice
-    int j;                               // where `alone` stands, or -1 (the single elements go with the first piece)
 
-    __device__ __forceinline__ Row(const T* row, int vocab, int piece = 0, int pieces = 1) : cut(row, vocab) {
-        base = (const char*)(row + cut.head);
-        const int each = (cut.whole + pieces - 1) / pieces;
-        begin = pieces == 1 ? 0 : (piece * each < cut.whole ? piece * each : cut.whole);
-        end = pieces == 1 ? cut.whole : (begin + each < cut.whole ? begin + each : cut.whole);
-        again = CH > 0 ? (end - begin > BLOCK * CH ? end - BLOCK * CH : begin) : end;
-        alone = 0.0f;
-        j = piece == 0 ? cut.single((int)threadIdx.x) : -1;
-        if (j >= 0) alone = (float)row[j];
-        start();
+    // The thread's index, to the compiler a new value each time: else it keeps every slot's place, several registers a slot, from one row
+    // to the next.
+    static __device__ __forceinline__ int thread() {
+        int t = (int)threadIdx.x;
+        asm volatile("" : "+v"(t));
+        return t;
     }
-    // whether element e is one of this piece's
-    __device__ __forceinline__ bool has(int e) const {
-        const int i = e - cut.head;
-        return i < 0 || i >= cut.whole * E ? begin == 0 : i >= begin * E && i < end * E;
-    }
-    __device__ __forceinline__ vec chunk(int i) const {
-        const any* p = (const any*)(base + (size_t)(unsigned)i * 16);
+    static __device__ __forceinline__ vec chunk(const Span& sp, int i) {
+        const any* p = (const any*)(sp.base() + (size_t)(unsigned)i * 16);
         if constexpr (NT_LOADS) return __builtin_nontemporal_load(p);
         else return *p;
     }
-    // Chunk of slot k in the round that begins at chunk `from`, of those before `to`; past them it is the last one again, which
-    // is not looked at.  (No branch: with one around each load the compiler moves it to where its value is used.)
-    __device__ __forceinline__ void fetch(int k, int from, int to) {
-        const int i = from + k * BLOCK + (int)threadIdx.x;
-        slot[k] = chunk(i < to ? i : to - 1);
+    // Chunk of slot k in the round that thread 0 begins at `from`, of those from `at` on and before `to`; outside it is the first or last
+    // one again, which is not looked at.  (No branch: with one around each load the compiler moves it to where its value is used.)
+    __device__ __forceinline__ void fetch(const Span& sp, int k, int from, int at, int to, int t) {
+        const int i = from + k * BLOCK + t;
+        slot[k] = chunk(sp, min(k == 0 ? max(i, at) : i, to - 1));
     }
-    __device__ __forceinline__ void start() {
-        const int to = again > begin ? again : end;
-        if (to > begin) {
+    static __device__ __forceinline__ bool in(int k, int i, int at, int to) { return (k > 0 || i >= at) && i < to; }
+    __device__ __forceinline__ void open_single(const Span& sp) {
+        alone = 0.0f;
+        const int j = sp.single();
+        if (j >= 0) alone = (float)sp.row[j];
+    }
+    __device__ __forceinline__ void open(const Span& sp) {
+        open_single(sp);
+        const int to = sp.first_end(), t = thread();
+        if (to > sp.begin) {
 #pragma unroll
-            for (int k = 0; k < kSlots; ++k) fetch(k, begin, to);
+            for (int k = 0; k < kSlots; ++k) fetch(sp, k, sp.origin, sp.begin, to, t);
         }
     }
     // (the same bits, but to the compiler a new value: else it keeps the 32-bit values of a 16-bit row as well, twice the registers)
@@ -110,18 +141,18 @@ struct Row {
         return v;
     }
 
-    // Statistics of the row; ends with the last CH chunks a thread in the slots.  skip (where SKIP): a bit for each entry that stays out
-    // (Cut::shift).
+    // Statistics of an open span; ends with the last CH chunks a thread in the slots.  skip (where SKIP): a bit for each entry that stays
+    // out (Cut::shift).
     template <bool ENT, bool SKIP>
-    __device__ __forceinline__ Stat stat(float c, const unsigned char* skip) {
-        Stat a{-INFINITY, 0.0f, 0.0f};
+    __device__ __forceinline__ Stat stat(const Span& sp, float c, const unsigned char* skip) {
+        Running a;
         auto one = [&](vec raw, int i) {
             const auto v = widened<T>(raw);
             float z[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) z[e] = v[e];
             if constexpr (SKIP) {
-                const int at = cut.first(i) + cut.shift();
+                const int at = sp.cut.first(i) + sp.cut.shift();
                 const unsigned bits = E == 8 ? skip[at >> 3] : (skip[at >> 3] >> (at & 4)) & 15u;
                 if (bits) {
 #pragma unroll
@@ -129,67 +160,76 @@ struct Row {
                         if (bits >> e & 1) z[e] = -INFINITY;
                 }
             }
-            take<ENT>(a, z, c);
+            a.take<ENT>(z, c);
         };
-        for (int from = begin; from < again; from += BLOCK * kSlots) {
+        const int t = thread();
+        const int first = CH > 0 ? sp.again : sp.end;
+        if (CH == 0 || sp.repeats()) for (int from = sp.origin; from < first; from += BLOCK * kSlots) {
             const int next = from + BLOCK * kSlots;
 #pragma unroll
             for (int k = 0; k < kSlots; ++k) {
-                const int i = from + k * BLOCK + (int)threadIdx.x;
-                if (i < again) one(slot[k], i);
-                if (next < again) fetch(k, next, again);
-                else if (CH > 0) fetch(k, again, end);
+                const int i = from + k * BLOCK + t;
+                if (in(k, i, sp.begin, first)) one(slot[k], i);
+                if (next < first) fetch(sp, k, next, sp.begin, first, t);
+                else if (CH > 0) fetch(sp, k, sp.keep, sp.again, sp.end, t);
             }
         }
         if constexpr (CH > 0) {
 #pragma unroll
             for (int k = 0; k < CH; ++k) {
-                const int i = again + k * BLOCK + (int)threadIdx.x;
-                if (i < end) one(slot[k], i);
+                const int i = sp.keep + k * BLOCK + t;
+                if (in(k, i, sp.again, sp.end)) one(slot[k], i);
             }
         }
+        const int j = sp.single();
         if (j >= 0) {
-            const float z[1] = {SKIP && (skip[(j + cut.shift()) >> 3] >> ((j + cut.shift()) & 7) & 1) ? -INFINITY : alone};
-            take<ENT>(a, z, c);
+            const float z[1] = {SKIP && (skip[(j + sp.cut.shift()) >> 3] >> ((j + sp.cut.shift()) & 7) & 1) ? -INFINITY : alone};
+            a.take<ENT>(z, c);
         }
-        return a;
+        return a.a;
     }
 
-    // dz_j = 2^((z_j - m) c) (A + B (z_j - m) c), and `mark` more at j = y
-    template <bool ENT>
-    __device__ __forceinline__ void write(T* out, float m, float c, float A, float B, int y, float mark) {
+    // dz_j = 2^((z_j - m) c) (A + B (z_j - m) c), and `mark` more at j = y (none: -1), where the logit is zy.  MORE: the first chunks of
+    // `next` are on their way when this returns, as after open(): each slot is loaded again when it has been written.
+    template <bool ENT, bool MORE>
+    __device__ __forceinline__ void write(const Span& sp, T* out, float m, float c, float A, float B, int y, float zy, float mark,
+                                          const Span& next) {
+        static_assert(CH > 0);
         const float ref = anchor(m);
-        char* to = (char*)(out + cut.head);
+        char* to = (char*)(out + sp.cut.head);
         auto one = [&](vec raw, int i) {
             const auto v = widened<T>(raw);
             typename Chunk<T>::wide g;
 #pragma unroll
             for (int e = 0; e < E; ++e) g[e] = slope_at<ENT>(v[e], ref, c, A, B);
-            const int at = y - cut.first(i);
-            if (at >= 0 && at < E) {
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (e == at) g[e] += mark;
-            }
             __builtin_nontemporal_store(__builtin_convertvector(g, vec), (any*)(to + (size_t)(unsigned)i * 16));
         };
+        const int j = sp.single();
         if (j >= 0) out[j] = (T)(slope_at<ENT>(alone, ref, c, A, B) + (j == y ? mark : 0.0f));
-        static_assert(CH > 0);
+        if (MORE) open_single(next);
+        const int t = thread();
+        const int next_end = next.first_end();
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            const int i = again + k * BLOCK + (int)threadIdx.x;
-            if (i < end) one(opaque(slot[k]), i);
-            if (again > begin) fetch(k, begin, again);
+            const int i = sp.keep + k * BLOCK + t;
+            if (in(k, i, sp.again, sp.end)) one(opaque(slot[k]), i);
+            if (sp.repeats()) fetch(sp, k, sp.origin, sp.begin, sp.again, t);
+            else if (MORE) fetch(next, k, next.origin, next.begin, next_end, t);
         }
-        for (int from = begin; from < again; from += BLOCK * kSlots) {
-            const int next = from + BLOCK * kSlots;
+        if (sp.repeats()) for (int from = sp.origin; from < sp.again; from += BLOCK * CH) {
+            const int on = from + BLOCK * CH;
 #pragma unroll
-            for (int k = 0; k < kSlots; ++k) {
-                const int i = from + k * BLOCK + (int)threadIdx.x;
-                if (i < again) one(slot[k], i);
-                if (next < again) fetch(k, next, again);
+            for (int k = 0; k < CH; ++k) {
+                const int i = from + k * BLOCK + t;
+                if (in(k, i, sp.begin, sp.again)) one(slot[k], i);
+                if (on < sp.again) fetch(sp, k, on, sp.begin, sp.again, t);
+                else if (MORE) fetch(next, k, next.origin, next.begin, next_end, t);
             }
         }
+        // the label's entry once more, by the thread that wrote its chunk
+        const int i = (y - sp.cut.head) / E;
+        if (y >= sp.cut.head && i >= sp.begin && i < sp.end && ((i - (i < sp.again ? sp.origin : sp.keep)) & (BLOCK - 1)) == (int)threadIdx.x)
+            out[y] = (T)(slope_at<ENT>(zy, ref, c, A, B) + mark);
     }
 
     // zeros in a row, or piece `piece` of `pieces` of it
@@ -198,8 +238,8 @@ struct Row {
         vec v;
 #pragma unroll
         for (int e = 0; e < E; ++e) v[e] = (T)0.0f;
-        for (int i = piece * BLOCK + (int)threadIdx.x; i < cut.whole; i += pieces * BLOCK)
-            __builtin_nontemporal_store(v, (any*)((char*)(out + cut.head) + (size_t)(unsigned)i * 16));
+        for (int i = piece * BLOCK + (int)threadIdx.x - cut.lead(out); i < cut.whole; i += pieces * BLOCK)
+            if (i >= 0) __builtin_nontemporal_store(v, (any*)((char*)(out + cut.head) + (size_t)(unsigned)i * 16));
         const int j = piece == 0 ? cut.single((int)threadIdx.x) : -1;
         if (j >= 0) out[j] = (T)0.0f;
     }
@@ -241,9 +281,12 @@ __global__ __launch_bounds__(BLOCK) void k_token_logprob(LogitsArgs l, TokenArgs
         if (threadIdx.x == 0) put_no_token(a, r);
         return;
     }
-    Row<T, BLOCK, 0, (BLOCK <= 512), SLOTS> z(row, l.vocab);
+    typedef Row<T, BLOCK, 0, true, (BLOCK <= 512), SLOTS> Hold;
+    const typename Hold::Span span(row, l.vocab);
+    Hold z;
+    z.open(span);
     const float zy = label_logit(row, y, l.vocab);
-    const Stat st = block_stat<ENT, BLOCK / 64>(z.template stat<ENT, false>(l.c, nullptr), l.c, lds);
+    const Stat st = block_stat<ENT, BLOCK / 64>(z.template stat<ENT, false>(span, l.c, nullptr), l.c, lds);
     if (threadIdx.x == 0) put_token(l, a, r, st, zy);
 }
 
@@ -262,7 +305,7 @@ __global__ __launch_bounds__(kGradBlock) void k_token_grad(LogitsArgs l, TokenGr
     const Cut<T> cut(row, l.vocab);
     const char* from = (const char*)(row + cut.head);
     char* to = (char*)(out + cut.head);
-    const int i0 = piece * (kGradBlock * kGradChunks) + (int)threadIdx.x;
+    const int i0 = piece * (kGradBlock * kGradChunks) + (int)threadIdx.x - cut.lead(row);
     const int j = piece == 0 ? cut.single((int)threadIdx.x) : -1;
     const int64_t y = a.labels[r];
     const float lse = a.lse[r], rest = a.lse_rest ? a.lse_rest[r] : 0.0f, s = (float)l.s;
@@ -276,14 +319,14 @@ __global__ __launch_bounds__(kGradBlock) void k_token_grad(LogitsArgs l, TokenGr
         for (int e = 0; e < E; ++e) zero[e] = (T)0.0f;
 #pragma unroll
         for (int k = 0; k < kGradChunks; ++k)
-            if (i0 + k * kGradBlock < cut.whole) *(any*)(to + (size_t)(unsigned)(i0 + k * kGradBlock) * 16) = zero;
+            if (i0 + k * kGradBlock >= 0 && i0 + k * kGradBlock < cut.whole) *(any*)(to + (size_t)(unsigned)(i0 + k * kGradBlock) * 16) = zero;
         if (j >= 0) out[j] = (T)0.0f;
         return;
     }
     vec slot[kGradChunks];
 #pragma unroll
     for (int k = 0; k < kGradChunks; ++k)
-        if (i0 + k * kGradBlock < cut.whole) slot[k] = __builtin_nontemporal_load((const any*)(from + (size_t)(unsigned)(i0 + k * kGradBlock) * 16));
+        if (i0 + k * kGradBlock >= 0 && i0 + k * kGradBlock < cut.whole) slot[k] = __builtin_nontemporal_load((const any*)(from + (size_t)(unsigned)(i0 + k * kGradBlock) * 16));
     // p_j (-g - h (log p_j + H))
     const float A = -(g + h * entropy) * s, B = -h * s;
     auto at = [&](float z) {
@@ -294,7 +337,7 @@ __global__ __launch_bounds__(kGradBlock) void k_token_grad(LogitsArgs l, TokenGr
 #pragma unroll
     for (int k = 0; k < kGradChunks; ++k) {
         const int i = i0 + k * kGradBlock;
-        if (i >= cut.whole) break;
+        if (i < 0 || i >= cut.whole) continue;
         const auto v = widened<T>(slot[k]);
         typename Chunk<T>::wide o;
 #pragma unroll
@@ -359,6 +402,7 @@ __device__ __forceinline__ PolicyRow policy_row(const LogitsArgs& l, const Polic
     p.A = over * (ENT ? fmaf(a.entropy_coef, (float)(g.entropy - g.log_s), -t.slope) : -t.slope);
     p.B = ENT ? over * a.entropy_coef * 0.693147180559945309417f : 0.0f;
     p.mark = W * t.slope;
+    if (p.empty) p.A = p.B = p.mark = 0.0f;
     return p;
 }
 __device__ __forceinline__ void put_policy(const PolicyArgs& a, int64_t r, float loss, float logp, float entropy) {
@@ -367,27 +411,87 @@ __device__ __forceinline__ void put_policy(const PolicyArgs& a, int64_t r, float
     if (a.entropy) a.entropy[r] = entropy;
 }
 
-template <typename T, bool ENT, int BLOCK, int CH>
+// The next row from r on, `step` apart, that counts; those before it get their zeros.
+template <typename T, int BLOCK, int CH>
+__device__ __forceinline__ int64_t next_policy_row(const LogitsArgs& l, const PolicyArgs& a, int64_t r, int64_t step) {
+    for (; r < l.rows; r += step) {
+        if (a.labels[r] >= 0 && !(a.weight && a.weight[r] == 0.0f)) break;
+        if (threadIdx.x == 0) put_policy(a, r, 0.0f, 0.0f, 0.0f);
+        Row<T, BLOCK, CH>::clear((T*)l.dz + r * l.ld_dz, l.vocab);
+    }
+    return r;
+}
+
+// TURNS: a workgroup takes rows one after the other, and the next row's chunks are loaded into the registers that this row's gradient
+// has left.  That pays where a compute unit holds one workgroup only (1024 threads): 8192 x 131072 bf16 839 -> 802 us, but with 512
+// threads or fewer, of which it holds several at different points of their rows, 8192 x 32768 204 -> 220 us.  (With the entropy the
+// registers do not suffice.)
+template <typename T, bool ENT, int BLOCK, int CH, bool LONG, bool TURNS>
 __global__ __launch_bounds__(BLOCK) void k_policy(LogitsArgs l, PolicyArgs a, int64_t first) {
+    typedef Row<T, BLOCK, CH, LONG> Hold;
+    typedef typename Hold::Span Span;
+    __shared__ Stat lds[TURNS ? 2 : 1][BLOCK / 64];
+    Hold z;
+    if constexpr (!TURNS) {
+        const int64_t r = first + blockIdx.x, y = a.labels[r];
+        const float w = a.weight ? a.weight[r] : 1.0f;
+        T* out = (T*)l.dz + r * l.ld_dz;
+        if (y < 0 || w == 0.0f) {
+            if (threadIdx.x == 0) put_policy(a, r, 0.0f, 0.0f, 0.0f);
+            Hold::clear(out, l.vocab);
+            return;
+        }
+        const Span span((const T*)l.z + r * l.ld, l.vocab);
+        z.open(span);
+        const float zy = label_logit(span.row, y, l.vocab);
+        const Stat st = block_stat<ENT, BLOCK / 64>(z.template stat<ENT, false>(span, l.c, nullptr), l.c, lds[0]);
+        const PolicyRow p = policy_row<ENT>(l, a, r, w, st, zy);
+        if (threadIdx.x == 0) put_policy(a, r, p.loss, p.logp, p.entropy);
+        z.template write<ENT, false>(span, out, st.m, l.c, p.A, p.B, y < l.vocab ? (int)y : -1, zy, p.mark, span);
+    } else {
+        int64_t r = next_policy_row<T, BLOCK, CH>(l, a, blockIdx.x, gridDim.x);
+        if (r >= l.rows) return;
+        Span span((const T*)l.z + r * l.ld, l.vocab);
+        z.open(span);
+        for (int turn = 0;; turn ^= 1) {
+            const int64_t y = a.labels[r];
+            const float w = a.weight ? a.weight[r] : 1.0f;
+            const float zy = label_logit(span.row, y, l.vocab);
+            const Stat st = block_stat<ENT, BLOCK / 64>(z.template stat<ENT, false>(span, l.c, nullptr), l.c, lds[turn]);
+            const PolicyRow p = policy_row<ENT>(l, a, r, w, st, zy);
+            if (threadIdx.x == 0) put_policy(a, r, p.loss, p.logp, p.entropy);
+            const int64_t on = next_policy_row<T, BLOCK, CH>(l, a, r + gridDim.x, gridDim.x);
+            const bool more = on < l.rows;
+            // (no next row: one chunk of this one again, so that there is one way through)
+            Span next(more ? (const T*)l.z + on * l.ld : span.row, l.vocab);
+            if (!more) next.end = next.begin + 1;
+            z.template write<ENT, true>(span, (T*)l.dz + r * l.ld_dz, st.m, l.c, p.A, p.B, y < l.vocab ? (int)y : -1, zy, p.mark, next);
+            if (!more) return;
+            r = on;
+            span = next;
+        }
+    }
+}
+
+// The same without a gradient.
+template <typename T, bool ENT, int BLOCK, int SLOTS>
+__global__ __launch_bounds__(BLOCK) void k_policy_value(LogitsArgs l, PolicyArgs a, int64_t first) {
     __shared__ Stat lds[BLOCK / 64];
     const int64_t r = first + blockIdx.x;
-    const T* row = (const T*)l.z + r * l.ld;
-    T* out = (T*)l.dz + r * l.ld_dz;
     const int64_t y = a.labels[r];
     const float w = a.weight ? a.weight[r] : 1.0f;
     if (y < 0 || w == 0.0f) {
         if (threadIdx.x == 0) put_policy(a, r, 0.0f, 0.0f, 0.0f);
-        if (l.dz) Row<T, BLOCK, CH>::clear(out, l.vocab);
         return;
     }
-    Row<T, BLOCK, CH> z(row, l.vocab);
-    const float zy = label_logit(row, y, l.vocab);
-    const Stat st = block_stat<ENT, BLOCK / 64>(z.template stat<ENT, false>(l.c, nullptr), l.c, lds);
+    typedef Row<T, BLOCK, 0, true, (BLOCK <= 512), SLOTS> Hold;
+    const typename Hold::Span span((const T*)l.z + r * l.ld, l.vocab);
+    Hold z;
+    z.open(span);
+    const float zy = label_logit(span.row, y, l.vocab);
+    const Stat st = block_stat<ENT, BLOCK / 64>(z.template stat<ENT, false>(span, l.c, nullptr), l.c, lds);
     const PolicyRow p = policy_row<ENT>(l, a, r, w, st, zy);
     if (threadIdx.x == 0) put_policy(a, r, p.loss, p.logp, p.entropy);
-    if (!l.dz) return;
-    if (p.empty) Row<T, BLOCK, CH>::clear(out, l.vocab);
-    else z.template write<ENT>(out, st.m, l.c, p.A, p.B, (int)y, p.mark);
 }
 
 // ---- distillation ----------------------------------------------------------------------------------------------------------
@@ -431,8 +535,9 @@ __device__ __forceinline__ void clear_seen(TopLds s, int vocab) {
 }
 
 // By the first wave.  An index that comes twice keeps its first place only, with the sum of its shares.  The bits of the
-// row's indices are set in `seen`, `by` further on; CLEAR: the words they are in are cleared first (else all are zero already).
-template <typename T, bool CLEAR>
+// row's indices are set in `seen`, `by` further on.  REST: all bits are zero before (else the words in question are cleared here), and
+// the student's statistics over the entries are wanted.
+template <typename T, bool REST>
 __device__ __forceinline__ void read_teacher(const LogitsArgs& l, const DistillArgs& a, int64_t r, const T* row, int by, TopLds s,
                                              Teacher* out) {
     const int lane = threadIdx.x & 63, top = a.top;
@@ -449,32 +554,23 @@ __device__ __forceinline__ void read_teacher(const LogitsArgs& l, const DistillA
         s.at[k] = (int)j;
         s.q[k] = v;
         s.z[k] = j >= 0 ? (float)row[j] : -INFINITY;
-        if (CLEAR && j >= 0) s.seen[((int)j + by) >> 5] = 0;
+        if (!REST && j >= 0) s.seen[((int)j + by) >> 5] = 0;
         most = fmaxf(most, v);
     }
     wave_fence();
     most = anchor(wave_max_f(most));
-    const bool given = a.lse != nullptr;
-    // log q_k = s (a_k - most) - shift
-    double shift;
-    if (given) {
-        shift = (double)a.lse[r] - (double)most * l.s;
-    } else {
-        double total = 0.0;
-        for (int k = lane; k < top; k += 64)
-            if (s.at[k] >= 0) total += (double)exp2_hw((s.q[k] - most) * l.c);
-        total = wave_sum(total);
-        shift = total > 0.0 ? log_d(total) : total;
-    }
-    double cross = 0.0, sum = 0.0;
+    // with e_k = exp(s (a_k - most)):  sums of e, e (a - most), e z, and of nothing else, so that one reduction does
+    double sums[8] = {};
     bool twice = false;
     for (int k = lane; k < top; k += 64) {
         if (s.at[k] < 0) continue;
-        const double lq = ((double)s.q[k] - (double)most) * l.s - shift;
-        const float qk = expf((float)lq);
-        s.q[k] = qk;
-        sum += (double)qk;
-        if (qk != 0.0f) cross += (double)qk * (lq - (double)s.z[k] * l.s);
+        const float d = s.q[k] - most, e = exp2_hw(d * l.c);
+        s.q[k] = e;
+        sums[0] += (double)e;
+        if (e != 0.0f) {
+            sums[1] = fma((double)e, (double)d, sums[1]);
+            sums[2] = fma((double)e, (double)s.z[k], sums[2]);
+        }
         const int place = s.at[k] + by;
         const unsigned bit = 1u << (place & 31);
         twice |= (atomicOr(&s.seen[place >> 5], bit) & bit) != 0;
@@ -497,59 +593,81 @@ __device__ __forceinline__ void read_teacher(const LogitsArgs& l, const DistillA
             if (again >> n & 1) s.at[k] = -1;
         }
     }
-    Stat st{-INFINITY, 0.0f, 0.0f};
+    const double mine = wave_sums8(sums, lane);
+    const double total = lane_bcast(mine, 0), ed = lane_bcast(mine, 1), ez = lane_bcast(mine, 2);
+    // q_k = f e_k and log q_k = s (a_k - most) - shift
+    double f, shift;
+    if (a.lse) {
+        shift = (double)a.lse[r] - (double)most * l.s;
+        f = (double)expf((float)-shift);
+    } else {
+        shift = total > 0.0 ? log_d(total) : total;
+        f = total > 0.0 ? 1.0 / total : total;
+    }
+    Running run;
     int entries = 0;
-    for (int k = lane; k < top; k += 64)
-        if (s.at[k] >= 0) {
+    for (int k0 = 0; k0 < top; k0 += 64) {
+        const int k = k0 + lane;
+        const bool one = k < top && s.at[k] >= 0;
+        entries += __popcll(__ballot(one));
+        if (!one) continue;
+        s.q[k] = (float)(f * (double)s.q[k]);
+        if (REST) {
             const float v[1] = {s.z[k]};
-            take<false>(st, v, l.c);
-            ++entries;
+            run.take<false>(v, l.c);
         }
-    st = wave_stat<false>(st, l.c);
-    cross = wave_sum(cross);
-    sum = wave_sum(sum);
-    const double count = wave_sum((double)entries);
+    }
+    const Stat st = REST ? wave_stat<false>(run.a, l.c) : run.a;
     const int any_lost = __any(lost);
-    if (lane == 0) *out = {cross, sum, st, (int)count, any_lost};
+    if (lane == 0) *out = {f * (l.s * (ed - ez) - shift * total), f * total, st, entries, any_lost};
 }
 
-// Everything about a row of the distillation but its gradient's entries: away from the teacher's dz_j = A 2^((z_j - st.m) c), at one
-// of them W (p_j - q_j).
+// What a row of the distillation's gradient is made of: away from the teacher's dz_j = A 2^((z_j - st.m) c), at one of them
+// W (p_j - q_j).  st: over the row, REST: over what is not among the entries; all: over the row.
 struct DistillRow {
-    Stat all;           // over the whole row
-    float loss, A, W;
+    Stat all;
+    float A, W;
     bool empty;
     __device__ __forceinline__ float at_entry(float z, float q, float c) const {
         return W * (exp2_hw((z - anchor(all.m)) * c) / all.s - q);
     }
 };
-// st: over the row, REST: over what is not among the entries
+// the teacher's share of the rest
+__device__ __forceinline__ double teacher_rest(const LogitsArgs& l, const Teacher& t) {
+    return t.entries < l.vocab && t.sum < 1.0 ? 1.0 - t.sum : 0.0;
+}
 template <bool REST>
 __device__ __forceinline__ DistillRow distill_row(const LogitsArgs& l, const DistillArgs& a, float w, Stat st, const Teacher& t) {
     DistillRow d;
     d.all = REST ? merged(st, t.top, l.c) : st;
-    const RowLog g = row_log(d.all, l.s);
-    double loss = t.entries ? t.cross + t.sum * g.lse : 0.0;
-    float A;
-    if (REST) {
-        // the rest's shares, of the teacher and (its logarithm) of the student
-        const double rest = t.entries < l.vocab && t.sum < 1.0 ? 1.0 - t.sum : 0.0;
-        const double log_t = st.s == 0.0f ? -INFINITY : ((double)st.m - (double)d.all.m) * l.s + log_d((double)st.s) - g.log_s;
-        if (rest > 0.0) loss += rest * (log_d(rest) - log_t);
-        A = st.s == 0.0f ? 0.0f : (float)(((double)expf((float)log_t) - rest) / (double)st.s);
-    } else {
-        A = t.entries ? 1.0f / st.s : 0.0f;
-    }
-    if (d.all.s == 0.0f) loss = t.entries ? INFINITY : 0.0;
-    if (t.lost) loss = NAN;
     d.empty = d.all.s == 0.0f && !t.lost;
-    d.W = loss != loss ? NAN : (float)((double)w * a.scale * l.s);
-    d.A = d.W * A;
-    d.loss = (float)loss;
+    // (a teacher that is no number leaves its mark on every entry)
+    d.W = t.lost || t.cross != t.cross ? NAN : (float)((double)w * a.scale * l.s);
+    if (REST) {
+        // p_j (1 - r / t), the student's share t = sum over the rest / sum over the row
+        const double share = (double)(st.s * exp2_hw(below(st.m, d.all.m, l.c)) / d.all.s);
+        d.A = st.s == 0.0f ? 0.0f : d.W * (float)((share - teacher_rest(l, t)) / (double)st.s);
+    } else {
+        d.A = t.entries ? d.W / st.s : d.W * 0.0f;
+    }
     return d;
 }
+template <bool REST>
+__device__ __forceinline__ float distill_value(const LogitsArgs& l, Stat st, const Teacher& t) {
+    const Stat all = REST ? merged(st, t.top, l.c) : st;
+    if (t.lost) return NAN;
+    if (all.s == 0.0f) return t.entries ? INFINITY : 0.0f;
+    const RowLog g = row_log(all, l.s);
+    double loss = t.entries ? t.cross + t.sum * g.lse : 0.0;
+    if (REST) {
+        const double rest = teacher_rest(l, t);
+        const double log_t = st.s == 0.0f ? -INFINITY : ((double)st.m - (double)all.m) * l.s + log_d((double)st.s) - g.log_s;
+        if (rest > 0.0) loss += rest * (log_d(rest) - log_t);
+    }
+    return (float)loss;
+}
 
-template <typename T, bool REST, int BLOCK, int CH>
+template <typename T, bool REST, int BLOCK, int CH, bool LONG>
 __global__ __launch_bounds__(BLOCK) void k_distill(LogitsArgs l, DistillArgs a, int64_t first) {
     __shared__ Stat lds[BLOCK / 64];
     __shared__ Teacher teacher;
@@ -564,19 +682,22 @@ __global__ __launch_bounds__(BLOCK) void k_distill(LogitsArgs l, DistillArgs a, 
         if (l.dz) Row<T, BLOCK, CH>::clear(out, l.vocab);
         return;
     }
-    Row<T, BLOCK, CH> z(row, l.vocab);
+    typedef Row<T, BLOCK, CH, LONG> Hold;
+    const typename Hold::Span span(row, l.vocab);
+    Hold z;
+    z.open(span);
     if (REST) clear_seen<BLOCK>(s, l.vocab);
-    if (threadIdx.x < 64) read_teacher<T, !REST>(l, a, r, row, z.cut.shift(), s, &teacher);
+    if (threadIdx.x < 64) read_teacher<T, REST>(l, a, r, row, span.cut.shift(), s, &teacher);
     if (REST) __syncthreads();
-    const Stat st = block_stat<false, BLOCK / 64>(z.template stat<false, REST>(l.c, (const unsigned char*)s.seen), l.c, lds);
+    const Stat st = block_stat<false, BLOCK / 64>(z.template stat<false, REST>(span, l.c, (const unsigned char*)s.seen), l.c, lds);
     const DistillRow d = distill_row<REST>(l, a, w, st, teacher);
-    if (threadIdx.x == 0) a.row_loss[r] = d.loss;
+    if (threadIdx.x == 0) a.row_loss[r] = distill_value<REST>(l, st, teacher);
     if (!l.dz) return;
     if (d.empty) {
         Row<T, BLOCK, CH>::clear(out, l.vocab);
         return;
     }
-    z.template write<false>(out, st.m, l.c, d.A, 0.0f, -1, 0.0f);
+    z.template write<false, false>(span, out, st.m, l.c, d.A, 0.0f, -1, 0.0f, 0.0f, span);
     __syncthreads();                          // (the entries' own values come after the row's)
     for (int k = threadIdx.x; k < a.top; k += BLOCK)
         if (s.at[k] >= 0) out[s.at[k]] = (T)d.at_entry(s.z[k], s.q[k], l.c);
@@ -608,9 +729,12 @@ __global__ __launch_bounds__(kSplitBlock) void k_split(LogitsArgs l, const int64
     const T* row = (const T*)l.z + r * l.ld;
     const int64_t y = labels[r];
     if (y < 0 || (weight && weight[r] == 0.0f)) return;
-    Row<T, kSplitBlock, 0, false> z(row, l.vocab, i, splits);
+    typedef Row<T, kSplitBlock, 0, true, false> Hold;
+    const typename Hold::Span span(row, l.vocab, i, splits);
+    Hold z;
+    z.open(span);
     const float zy = label_logit(row, y, l.vocab);
-    const Stat st = block_stat<ENT, kSplitBlock / 64>(z.template stat<ENT, false>(l.c, nullptr), l.c, lds);
+    const Stat st = block_stat<ENT, kSplitBlock / 64>(z.template stat<ENT, false>(span, l.c, nullptr), l.c, lds);
     if (threadIdx.x == 0) {
         ws[r].part[i] = st;
         if (i == 0) ws[r].zy = zy;            // (the second launch may write the gradient over it)
@@ -628,7 +752,8 @@ __global__ __launch_bounds__(kSplitBlock) void k_split_distill(LogitsArgs l, Dis
     if (a.weight && a.weight[r] == 0.0f) return;
     if (i == splits) {
         const Cut<T> cut(row, l.vocab);
-        if (threadIdx.x < 64) read_teacher<T, true>(l, a, r, row, cut.shift(), s, &ws[r].teacher);
+        if (REST) clear_seen<kSplitBlock>(s, l.vocab);
+        if (threadIdx.x < 64) read_teacher<T, REST>(l, a, r, row, cut.shift(), s, &ws[r].teacher);
         __syncthreads();
         for (int k = threadIdx.x; k < a.top; k += kSplitBlock) {
             ws[r].at[k] = s.at[k];
@@ -637,17 +762,20 @@ __global__ __launch_bounds__(kSplitBlock) void k_split_distill(LogitsArgs l, Dis
         }
         return;
     }
-    Row<T, kSplitBlock, 0, false> z(row, l.vocab, i, splits);
+    typedef Row<T, kSplitBlock, 0, true, false> Hold;
+    const typename Hold::Span span(row, l.vocab, i, splits);
+    Hold z;
+    z.open(span);
     if (REST) {
         clear_seen<kSplitBlock>(s, l.vocab);
         for (int k = threadIdx.x; k < a.top; k += kSplitBlock) {
             const int64_t j = teacher_index(a, r * a.ld + k);
             if (j >= 0 && j < l.vocab && teacher_logit(a, r * a.ld + k) != -INFINITY)
-                atomicOr(&s.seen[((int)j + z.cut.shift()) >> 5], 1u << (((int)j + z.cut.shift()) & 31));
+                atomicOr(&s.seen[((int)j + span.cut.shift()) >> 5], 1u << (((int)j + span.cut.shift()) & 31));
         }
         __syncthreads();
     }
-    const Stat st = block_stat<false, kSplitBlock / 64>(z.template stat<false, REST>(l.c, (const unsigned char*)s.seen), l.c, lds);
+    const Stat st = block_stat<false, kSplitBlock / 64>(z.template stat<false, REST>(span, l.c, (const unsigned char*)s.seen), l.c, lds);
     if (threadIdx.x == 0) ws[r].part[i] = st;
 }
 
@@ -688,13 +816,16 @@ __global__ __launch_bounds__(kSplitBlock) void k_join_policy(LogitsArgs l, Polic
         if (l.dz) Row<T, kSplitBlock, kSplitHold>::clear(out, l.vocab, i, splits);
         return;
     }
-    Row<T, kSplitBlock, kSplitHold> z((const T*)l.z + r * l.ld, l.vocab, i, splits);
+    typedef Row<T, kSplitBlock, kSplitHold, true> Hold;
+    const typename Hold::Span span((const T*)l.z + r * l.ld, l.vocab, i, splits);
+    Hold z;
+    z.open(span);
     const Stat st = joined<ENT>(ws[r], splits, l.c);
     const PolicyRow p = policy_row<ENT>(l, a, r, w, st, ws[r].zy);
     if (threadIdx.x == 0 && i == 0) put_policy(a, r, p.loss, p.logp, p.entropy);
     if (!l.dz) return;
     if (p.empty) Row<T, kSplitBlock, kSplitHold>::clear(out, l.vocab, i, splits);
-    else z.template write<ENT>(out, st.m, l.c, p.A, p.B, (int)y, p.mark);
+    else z.template write<ENT, false>(span, out, st.m, l.c, p.A, p.B, y < l.vocab ? (int)y : -1, ws[r].zy, p.mark, span);
 }
 
 template <typename T, bool REST>
@@ -705,7 +836,7 @@ __global__ __launch_bounds__(kSplitBlock) void k_join_distill(LogitsArgs l, Dist
         const int q = threadIdx.x;
         const float w = q < l.rows ? (a.weight ? a.weight[q] : 1.0f) : 0.0f;
         double mine = 0.0;
-        if (w != 0.0f) mine = (double)w * (double)distill_row<REST>(l, a, w, joined_alone(ws[q], splits, l.c), ws[q].teacher).loss;
+        if (w != 0.0f) mine = (double)w * (double)distill_value<REST>(l, joined_alone(ws[q], splits, l.c), ws[q].teacher);
         put_total(mine, a.scale, loss);
         return;
     }
@@ -716,21 +847,31 @@ __global__ __launch_bounds__(kSplitBlock) void k_join_distill(LogitsArgs l, Dist
         if (l.dz) Row<T, kSplitBlock, kSplitHold>::clear(out, l.vocab, i, splits);
         return;
     }
-    Row<T, kSplitBlock, kSplitHold> z((const T*)l.z + r * l.ld, l.vocab, i, splits);
+    typedef Row<T, kSplitBlock, kSplitHold, true> Hold;
+    const typename Hold::Span span((const T*)l.z + r * l.ld, l.vocab, i, splits);
+    Hold z;
+    z.open(span);
     const Stat st = joined<false>(ws[r], splits, l.c);
     const DistillRow d = distill_row<REST>(l, a, w, st, ws[r].teacher);
-    if (threadIdx.x == 0 && i == 0) a.row_loss[r] = d.loss;
+    if (threadIdx.x == 0 && i == 0) a.row_loss[r] = distill_value<REST>(l, st, ws[r].teacher);
     if (!l.dz) return;
     if (d.empty) {
         Row<T, kSplitBlock, kSplitHold>::clear(out, l.vocab, i, splits);
         return;
     }
-    z.template write<false>(out, st.m, l.c, d.A, 0.0f, -1, 0.0f);
+    z.template write<false, false>(span, out, st.m, l.c, d.A, 0.0f, -1, 0.0f, 0.0f, span);
     __syncthreads();                          // (the entries' own values come after the row's)
     for (int k = threadIdx.x; k < a.top; k += kSplitBlock) {
         const int j = ws[r].at[k];
-        if (j >= 0 && z.has(j)) out[j] = (T)d.at_entry(ws[r].z[k], ws[r].q[k], l.c);
+        if (j >= 0 && span.has(j)) out[j] = (T)d.at_entry(ws[r].z[k], ws[r].q[k], l.c);
     }
+}
+
+// how many places of a chunk a row takes, at most, with those before its first that bring it to a line
+template <typename T>
+int most_chunks(const LogitsArgs& l) {
+    const bool lines = ((uintptr_t)l.z & 127) == 0 && l.ld * (int64_t)sizeof(T) % 128 == 0;
+    return l.vocab / Chunk<T>::E + (lines ? 0 : 7);
 }
 
 // f(first row or piece, workgroups) for each launch
@@ -739,22 +880,41 @@ void by_rows(int64_t rows, F f) {
     for (int64_t r = 0; r < rows; r += kRowBlocksMax) f(r, dim3((unsigned)(rows - r < kRowBlocksMax ? rows - r : kRowBlocksMax)));
 }
 
-// f(BLOCK, CH) for rows of `vocab` elements whose gradient is wanted
+// f(BLOCK, SLOTS) for rows of `vocab` elements that are only read
 template <typename T, typename F>
-void by_width(int vocab, F f) {
-    constexpr int E = Chunk<T>::E;
-    const int chunks = vocab / E;
+void by_length(int64_t rows, int vocab, F f) {
+    // Where there are rows for every compute unit, few threads to each; where there are not, many.  bf16, us, 64 / 256 / 512 threads, two
+    // loads each: 16384 x 2000 16.4 / 24.7 / 41, x 8000 45.7 / 48.0 / 58, x 32000 164 / 162 / 163, 3001 x 50021 (f16) 54 / 53 / 47;
+    // 512 and 1024 threads, four loads: 128 x 4000 4.3 (64 threads) / 3.4 (512), 128 x 32768 6.5 (256) / 4.8 (1024).
+    const int chunks = vocab / Chunk<T>::E;
     using std::integral_constant;
-    if (chunks <= 64 * 4) f(integral_constant<int, 64>{}, integral_constant<int, 4>{});
-    else if (chunks <= 128 * 4) f(integral_constant<int, 128>{}, integral_constant<int, 4>{});
-    else if (chunks <= 256 * 4) f(integral_constant<int, 256>{}, integral_constant<int, 4>{});
-    else if (chunks <= 256 * 8) f(integral_constant<int, 256>{}, integral_constant<int, 8>{});
-    else if (chunks <= 512 * 8) f(integral_constant<int, 512>{}, integral_constant<int, 8>{});
-    else if (chunks <= 512 * 10) f(integral_constant<int, 512>{}, integral_constant<int, 10>{});
-    else if (chunks <= 512 * 13) f(integral_constant<int, 512>{}, integral_constant<int, 13>{});
-    else if (chunks <= 512 * 16) f(integral_constant<int, 512>{}, integral_constant<int, 16>{});
-    else if (chunks <= 1024 * 13) f(integral_constant<int, 1024>{}, integral_constant<int, 13>{});
-    else f(integral_constant<int, 1024>{}, integral_constant<int, 16>{});
+    if (rows <= 512) {
+        if (chunks <= 1024) f(integral_constant<int, 512>{}, integral_constant<int, 4>{});
+        else f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+    } else {
+        if (chunks <= 1024) f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+        else if (chunks <= 4096) f(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+        else f(integral_constant<int, 512>{}, integral_constant<int, 2>{});
+    }
+}
+
+// f(BLOCK, CH, LONG) for rows whose gradient is wanted
+template <typename T, typename F>
+void by_width(const LogitsArgs& l, F f) {
+    const int chunks = most_chunks<T>(l);
+    auto go = [&](auto block, auto ch) { f(block, ch, std::false_type{}); };
+    using std::integral_constant;
+    if (chunks <= 64 * 4) go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+    else if (chunks <= 128 * 4) go(integral_constant<int, 128>{}, integral_constant<int, 4>{});
+    else if (chunks <= 256 * 4) go(integral_constant<int, 256>{}, integral_constant<int, 4>{});
+    else if (chunks <= 256 * 8) go(integral_constant<int, 256>{}, integral_constant<int, 8>{});
+    else if (chunks <= 512 * 8) go(integral_constant<int, 512>{}, integral_constant<int, 8>{});
+    else if (chunks <= 512 * 10) go(integral_constant<int, 512>{}, integral_constant<int, 10>{});
+    else if (chunks <= 512 * 13) go(integral_constant<int, 512>{}, integral_constant<int, 13>{});
+    else if (chunks <= 512 * 16) go(integral_constant<int, 512>{}, integral_constant<int, 16>{});
+    else if (chunks <= 1024 * 13) go(integral_constant<int, 1024>{}, integral_constant<int, 13>{});
+    else if (chunks <= 1024 * 16) go(integral_constant<int, 1024>{}, integral_constant<int, 16>{});
+    else f(integral_constant<int, 1024>{}, integral_constant<int, 16>{}, std::true_type{});
 }
 
 }  // namespace
@@ -768,36 +928,24 @@ hipError_t allow_lds(K kernel, size_t bytes) {
 
 template <typename T>
 hipError_t token_logprob_rows(const LogitsArgs& l, const TokenArgs& a, SplitRow* ws, hipStream_t st) {
-    const int chunks = l.vocab / Chunk<T>::E, splits = row_splits(l.rows, l.vocab, sizeof(T), false);
-    if (splits > 1) {
+    if (const int splits = row_splits(l.rows, l.vocab, sizeof(T), false); splits > 1) {
         const auto kernel = a.entropy ? k_split<T, true> : k_split<T, false>;
         hipLaunchKernelGGL(kernel, dim3((unsigned)l.rows * splits), dim3(kSplitBlock), 0, st, l, a.labels, (const float*)nullptr, ws, splits);
         hipLaunchKernelGGL(k_join_token, dim3((unsigned)l.rows), dim3(64), 0, st, l, a, (const SplitRow*)ws, splits);
         return hipGetLastError();
     }
-    auto launch = [&](auto block, auto slots) {
+    by_length<T>(l.rows, l.vocab, [&](auto block, auto slots) {
         constexpr int BLOCK = decltype(block)::value, SLOTS = decltype(slots)::value;
         const auto kernel = a.entropy ? k_token_logprob<T, true, BLOCK, SLOTS> : k_token_logprob<T, false, BLOCK, SLOTS>;
         by_rows(l.rows, [&](int64_t first, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(BLOCK), 0, st, l, a, first); });
-    };
-    // Where there are rows for every compute unit, few threads to each; where there are not, many.  bf16, us, 64 / 256 / 512 threads, two
-    // loads each: 16384 x 2000 16.4 / 24.7 / 41, x 8000 45.7 / 48.0 / 58, x 32000 164 / 162 / 163, 3001 x 50021 (f16) 54 / 53 / 47;
-    // 512 and 1024 threads, four loads: 128 x 4000 4.3 (64 threads) / 3.4 (512), 128 x 32768 6.5 (256) / 4.8 (1024).
-    using std::integral_constant;
-    if (l.rows <= 512) {
-        if (chunks <= 1024) launch(integral_constant<int, 512>{}, integral_constant<int, 4>{});
-        else launch(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
-    } else {
-        if (chunks <= 1024) launch(integral_constant<int, 64>{}, integral_constant<int, 2>{});
-        else if (chunks <= 4096) launch(integral_constant<int, 256>{}, integral_constant<int, 2>{});
-        else launch(integral_constant<int, 512>{}, integral_constant<int, 2>{});
-    }
+    });
     return hipGetLastError();
 }
 
 template <typename T>
 hipError_t token_grad_rows(const LogitsArgs& l, const TokenGradArgs& a, hipStream_t st) {
-    const int64_t piece = (int64_t)kGradBlock * kGradChunks * Chunk<T>::E, pieces = (l.vocab + piece - 1) / piece;
+    constexpr int kPiece = kGradBlock * kGradChunks;
+    const int64_t pieces = (most_chunks<T>(l) + kPiece) / kPiece;      // (one for a row of single elements too)
     const auto kernel = a.d_entropy ? k_token_grad<T, true> : k_token_grad<T, false>;
     by_rows(l.rows * pieces,
             [&](int64_t first, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(kGradBlock), 0, st, l, a, (int)pieces, first); });
@@ -814,10 +962,18 @@ hipError_t policy_rows(const LogitsArgs& l, const PolicyArgs& a, float* loss, Sp
                            (const SplitRow*)ws, splits, loss);
         return hipGetLastError();
     }
-    by_width<T>(l.vocab, [&](auto block, auto ch) {
-        constexpr int BLOCK = decltype(block)::value, CH = decltype(ch)::value;
-        const auto kernel = ent ? k_policy<T, true, BLOCK, CH> : k_policy<T, false, BLOCK, CH>;
+    if (!l.dz) by_length<T>(l.rows, l.vocab, [&](auto block, auto slots) {
+        constexpr int BLOCK = decltype(block)::value, SLOTS = decltype(slots)::value;
+        const auto kernel = ent ? k_policy_value<T, true, BLOCK, SLOTS> : k_policy_value<T, false, BLOCK, SLOTS>;
         by_rows(l.rows, [&](int64_t first, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(BLOCK), 0, st, l, a, first); });
+    });
+    else by_width<T>(l, [&](auto block, auto ch, auto lng) {
+        constexpr int BLOCK = decltype(block)::value, CH = decltype(ch)::value;
+        constexpr bool LONG = decltype(lng)::value;
+        constexpr bool TURNS = BLOCK == 1024 && !LONG;
+        const auto kernel = ent ? k_policy<T, true, BLOCK, CH, LONG, false> : k_policy<T, false, BLOCK, CH, LONG, TURNS>;
+        if (TURNS && !ent) hipLaunchKernelGGL(kernel, dim3((unsigned)(l.rows < kTurnBlocks ? l.rows : kTurnBlocks)), dim3(BLOCK), 0, st, l, a, (int64_t)0);
+        else by_rows(l.rows, [&](int64_t first, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(BLOCK), 0, st, l, a, first); });
     });
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     return launch_weighted_total(a.row_loss, a.weight, l.rows, a.scale, loss, st);
@@ -835,9 +991,10 @@ hipError_t distill_rows(const LogitsArgs& l, const DistillArgs& a, float* loss, 
         return hipGetLastError();
     }
     hipError_t err = hipSuccess;
-    by_width<T>(l.vocab, [&](auto block, auto ch) {
+    by_width<T>(l, [&](auto block, auto ch, auto lng) {
         constexpr int BLOCK = decltype(block)::value, CH = decltype(ch)::value;
-        const auto kernel = a.lse ? k_distill<T, true, BLOCK, CH> : k_distill<T, false, BLOCK, CH>;
+        constexpr bool LONG = decltype(lng)::value;
+        const auto kernel = a.lse ? k_distill<T, true, BLOCK, CH, LONG> : k_distill<T, false, BLOCK, CH, LONG>;
         err = allow_lds(kernel, lds);
         if (err != hipSuccess) return;
         by_rows(l.rows, [&](int64_t first, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(BLOCK), lds, st, l, a, first); });

@@ -146,14 +146,16 @@ struct Row {
     template <bool ENT, bool SKIP>
     __device__ __forceinline__ Stat stat(const Span& sp, float c, const unsigned char* skip) {
         Running a;
-        auto one = [&](vec raw, int i) {
+        auto skipped = [&](int i) -> unsigned {
+            const int at = sp.cut.first(i) + sp.cut.shift();
+            return E == 8 ? skip[at >> 3] : (skip[at >> 3] >> (at & 4)) & 15u;
+        };
+        auto one = [&](vec raw, unsigned bits) {
             const auto v = widened<T>(raw);
             float z[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) z[e] = v[e];
             if constexpr (SKIP) {
-                const int at = sp.cut.first(i) + sp.cut.shift();
-                const unsigned bits = E == 8 ? skip[at >> 3] : (skip[at >> 3] >> (at & 4)) & 15u;
                 if (bits) {
 #pragma unroll
                     for (int e = 0; e < E; ++e)
@@ -169,16 +171,21 @@ struct Row {
 #pragma unroll
             for (int k = 0; k < kSlots; ++k) {
                 const int i = from + k * BLOCK + t;
-                if (in(k, i, sp.begin, first)) one(slot[k], i);
+                if (in(k, i, sp.begin, first)) one(slot[k], SKIP ? skipped(i) : 0);
                 if (next < first) fetch(sp, k, next, sp.begin, first, t);
                 else if (CH > 0) fetch(sp, k, sp.keep, sp.again, sp.end, t);
             }
         }
         if constexpr (CH > 0) {
+            unsigned bits[CH] = {};                   // (all of them asked for before the first is waited for)
+            if constexpr (SKIP) {
+#pragma unroll
+                for (int k = 0; k < CH; ++k) bits[k] = skipped(max(min(sp.keep + k * BLOCK + t, sp.end - 1), 0));
+            }
 #pragma unroll
             for (int k = 0; k < CH; ++k) {
                 const int i = sp.keep + k * BLOCK + t;
-                if (in(k, i, sp.again, sp.end)) one(slot[k], i);
+                if (in(k, i, sp.again, sp.end)) one(slot[k], bits[k]);
             }
         }
         const int j = sp.single();
@@ -534,34 +541,48 @@ __device__ __forceinline__ void clear_seen(TopLds s, int vocab) {
     __syncthreads();
 }
 
-// By the first wave.  An index that comes twice keeps its first place only, with the sum of its shares.  The bits of the
-// row's indices are set in `seen`, `by` further on.  REST: all bits are zero before (else the words in question are cleared here), and
-// the student's statistics over the entries are wanted.
+struct Marks {
+    bool lost, twice;       // of this lane's entries: past the vocabulary, a second time
+};
+// By the first wave: the entries' indices (-1: padding) and the teacher's logits into LDS, and the indices' bits in `seen`, `by` further on.
+// REST: all bits are zero before; else the words in question are cleared here.
+template <bool REST>
+__device__ __forceinline__ Marks mark_entries(const LogitsArgs& l, const DistillArgs& a, int64_t r, int by, TopLds s) {
+    Marks m{false, false};
+    for (int k = threadIdx.x; k < a.top; k += 64) {
+        const int64_t j = teacher_index(a, r * a.ld + k);
+        const float v = teacher_logit(a, r * a.ld + k);
+        m.lost |= j >= l.vocab;
+        const bool none = j < 0 || j >= l.vocab || v == -INFINITY;
+        s.at[k] = none ? -1 : (int)j;
+        s.q[k] = v;
+        if (!REST && !none) s.seen[((int)j + by) >> 5] = 0;
+    }
+    wave_fence();
+    for (int k = threadIdx.x; k < a.top; k += 64)
+        if (s.at[k] >= 0) {
+            const int place = s.at[k] + by;
+            const unsigned bit = 1u << (place & 31);
+            m.twice |= (atomicOr(&s.seen[place >> 5], bit) & bit) != 0;
+        }
+    return m;
+}
+
+// By the first wave, after mark_entries: the entries' shares (an index that comes twice keeps its first place only, with the sum of its
+// shares), the student's logits there and what all of them come to.  REST: the student's statistics over the entries as well.
 template <typename T, bool REST>
-__device__ __forceinline__ void read_teacher(const LogitsArgs& l, const DistillArgs& a, int64_t r, const T* row, int by, TopLds s,
+__device__ __forceinline__ void read_teacher(const LogitsArgs& l, const DistillArgs& a, int64_t r, const T* row, Marks marks, TopLds s,
                                              Teacher* out) {
     const int lane = threadIdx.x & 63, top = a.top;
     float most = -INFINITY;
-    bool lost = false;
     for (int k = lane; k < top; k += 64) {
-        int64_t j = teacher_index(a, r * a.ld + k);
-        float v = teacher_logit(a, r * a.ld + k);
-        lost |= j >= l.vocab;
-        if (j < 0 || j >= l.vocab || v == -INFINITY) {
-            j = -1;
-            v = -INFINITY;
-        }
-        s.at[k] = (int)j;
-        s.q[k] = v;
-        s.z[k] = j >= 0 ? (float)row[j] : -INFINITY;
-        if (!REST && j >= 0) s.seen[((int)j + by) >> 5] = 0;
-        most = fmaxf(most, v);
+        s.z[k] = s.at[k] >= 0 ? (float)row[s.at[k]] : -INFINITY;
+        if (s.at[k] >= 0) most = fmaxf(most, s.q[k]);
     }
     wave_fence();
     most = anchor(wave_max_f(most));
     // with e_k = exp(s (a_k - most)):  sums of e, e (a - most), e z, and of nothing else, so that one reduction does
     double sums[8] = {};
-    bool twice = false;
     for (int k = lane; k < top; k += 64) {
         if (s.at[k] < 0) continue;
         const float d = s.q[k] - most, e = exp2_hw(d * l.c);
@@ -571,12 +592,9 @@ __device__ __forceinline__ void read_teacher(const LogitsArgs& l, const DistillA
             sums[1] = fma((double)e, (double)d, sums[1]);
             sums[2] = fma((double)e, (double)s.z[k], sums[2]);
         }
-        const int place = s.at[k] + by;
-        const unsigned bit = 1u << (place & 31);
-        twice |= (atomicOr(&s.seen[place >> 5], bit) & bit) != 0;
     }
     wave_fence();
-    if (__any(twice)) {
+    if (__any(marks.twice)) {
         unsigned again = 0;                       // one bit for each of this lane's entries (kMaxTop / 64 = 16 of them)
         for (int k = lane, n = 0; k < top; k += 64, ++n) {
             float share = 0.0f;
@@ -618,7 +636,7 @@ __device__ __forceinline__ void read_teacher(const LogitsArgs& l, const DistillA
         }
     }
     const Stat st = REST ? wave_stat<false>(run.a, l.c) : run.a;
-    const int any_lost = __any(lost);
+    const int any_lost = __any(marks.lost);
     if (lane == 0) *out = {f * (l.s * (ed - ez) - shift * total), f * total, st, entries, any_lost};
 }
 
@@ -687,8 +705,10 @@ __global__ __launch_bounds__(BLOCK) void k_distill(LogitsArgs l, DistillArgs a, 
     Hold z;
     z.open(span);
     if (REST) clear_seen<BLOCK>(s, l.vocab);
-    if (threadIdx.x < 64) read_teacher<T, REST>(l, a, r, row, span.cut.shift(), s, &teacher);
+    Marks marks{false, false};
+    if (threadIdx.x < 64) marks = mark_entries<REST>(l, a, r, span.cut.shift(), s);
     if (REST) __syncthreads();
+    if (threadIdx.x < 64) read_teacher<T, REST>(l, a, r, row, marks, s, &teacher);
     const Stat st = block_stat<false, BLOCK / 64>(z.template stat<false, REST>(span, l.c, (const unsigned char*)s.seen), l.c, lds);
     const DistillRow d = distill_row<REST>(l, a, w, st, teacher);
     if (threadIdx.x == 0) a.row_loss[r] = distill_value<REST>(l, st, teacher);
@@ -753,7 +773,7 @@ __global__ __launch_bounds__(kSplitBlock) void k_split_distill(LogitsArgs l, Dis
     if (i == splits) {
         const Cut<T> cut(row, l.vocab);
         if (REST) clear_seen<kSplitBlock>(s, l.vocab);
-        if (threadIdx.x < 64) read_teacher<T, REST>(l, a, r, row, cut.shift(), s, &ws[r].teacher);
+        if (threadIdx.x < 64) read_teacher<T, REST>(l, a, r, row, mark_entries<REST>(l, a, r, cut.shift(), s), s, &ws[r].teacher);
         __syncthreads();
         for (int k = threadIdx.x; k < a.top; k += kSplitBlock) {
             ws[r].at[k] = s.at[k];

@@ -72,7 +72,8 @@ struct Span {
         begin = pieces == 1 || piece == 0 ? 0 : min(piece * each - lead, cut.whole);
         end = pieces == 1 ? cut.whole : max(min((piece + 1) * each - lead, cut.whole), begin);
         origin = begin == 0 ? -lead : begin;
-        again = LONG && (SURE || end - origin > HOLD) ? max(((end - (HOLD - 16) + lead + 7) & ~7) - lead, begin) : begin;
+        if (HOLD == 0) again = end;
+        else again = LONG && (SURE || end - origin > HOLD) ? max(((end - (HOLD - 16) + lead + 7) & ~7) - lead, begin) : begin;
         keep = repeats() ? again : origin;
         singles = piece == 0;
     }
@@ -133,6 +134,15 @@ struct Row {
         if (to > sp.begin) {
 #pragma unroll
             for (int k = 0; k < kSlots; ++k) fetch(sp, k, sp.origin, sp.begin, to, t);
+        }
+    }
+    // Straight to what write() expects, where the statistics are known already: the last chunks in the slots.
+    __device__ __forceinline__ void open_last(const Span& sp) {
+        open_single(sp);
+        const int t = thread();
+        if (sp.end > sp.again) {
+#pragma unroll
+            for (int k = 0; k < kSlots; ++k) fetch(sp, k, sp.keep, sp.again, sp.end, t);
         }
     }
     // (the same bits, but to the compiler a new value: else it keeps the 32-bit values of a 16-bit row as well, twice the registers)
@@ -839,7 +849,7 @@ __global__ __launch_bounds__(kSplitBlock) void k_join_policy(LogitsArgs l, Polic
     typedef Row<T, kSplitBlock, kSplitHold, true> Hold;
     const typename Hold::Span span((const T*)l.z + r * l.ld, l.vocab, i, splits);
     Hold z;
-    z.open(span);
+    z.open_last(span);
     const Stat st = joined<ENT>(ws[r], splits, l.c);
     const PolicyRow p = policy_row<ENT>(l, a, r, w, st, ws[r].zy);
     if (threadIdx.x == 0 && i == 0) put_policy(a, r, p.loss, p.logp, p.entropy);
@@ -870,7 +880,7 @@ __global__ __launch_bounds__(kSplitBlock) void k_join_distill(LogitsArgs l, Dist
     typedef Row<T, kSplitBlock, kSplitHold, true> Hold;
     const typename Hold::Span span((const T*)l.z + r * l.ld, l.vocab, i, splits);
     Hold z;
-    z.open(span);
+    z.open_last(span);
     const Stat st = joined<false>(ws[r], splits, l.c);
     const DistillRow d = distill_row<REST>(l, a, w, st, ws[r].teacher);
     if (threadIdx.x == 0 && i == 0) a.row_loss[r] = distill_value<REST>(l, st, ws[r].teacher);

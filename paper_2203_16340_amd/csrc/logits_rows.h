@@ -6,6 +6,7 @@
 // and every gradient here is, away from a few marked entries, 2^a_j (A + B a_j) with numbers A, B of the row.
 #pragma once
 
+#include <algorithm>
 #include <type_traits>
 
 #include "logits.h"
@@ -975,7 +976,7 @@ hipError_t token_logprob_rows(const LogitsArgs& l, const TokenArgs& a, SplitRow*
 template <typename T>
 hipError_t token_grad_rows(const LogitsArgs& l, const TokenGradArgs& a, hipStream_t st) {
     constexpr int kPiece = kGradBlock * kGradChunks;
-    const int64_t pieces = (most_chunks<T>(l) + kPiece) / kPiece;      // (one for a row of single elements too)
+    const int64_t pieces = (std::max(most_chunks<T>(l), 1) + kPiece - 1) / kPiece;      // (one for a row of single elements too)
     const auto kernel = a.d_entropy ? k_token_grad<T, true> : k_token_grad<T, false>;
     by_rows(l.rows * pieces,
             [&](int64_t first, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(kGradBlock), 0, st, l, a, (int)pieces, first); });

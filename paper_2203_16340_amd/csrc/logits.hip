@@ -5,6 +5,7 @@ namespace lb {
 
 namespace {
 
+// One workgroup, so that the order of the sum is fixed: 4.7 us for 8192 rows, 1.4 for a few.
 constexpr int kTotalBlock = 1024;
 
 __global__ __launch_bounds__(kTotalBlock) void k_weighted_total(const float* row_loss, const float* weight, int64_t n, double scale,

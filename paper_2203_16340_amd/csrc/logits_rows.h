@@ -4,6 +4,12 @@
 // With a_j = (z_j - m) c, m the row's maximum, S = sum_j 2^a_j, T = sum_j a_j 2^a_j (Stat in logits.h):
 //     lse = m s + ln S,   p_j = 2^a_j / S,   H = ln S - ln 2 T / S,
 // and every gradient here is, away from a few marked entries, 2^a_j (A + B a_j) with numbers A, B of the row.
+//
+// All of it is bound by memory: 4 to 10 operations and one or two exponentials an entry against 2 or 4 bytes read (and as many
+// written).  So a row is read once where it fits a workgroup's registers, in 16-byte chunks a thread with all loads in flight at
+// once, and its sums and maxima are taken while they arrive: a maximum and a sum for each thread, joined over the wave by lane
+// permutations and over the workgroup through LDS, behind one barrier.  (The exponentials are no bound: with one multiply-add in
+// place of a difference and a product in both passes, the times were the same.)
 #pragma once
 
 #include <algorithm>
@@ -289,6 +295,8 @@ __device__ __forceinline__ void put_no_token(const TokenArgs& a, int64_t r) {
     if (a.entropy) a.entropy[r] = 0.0f;
 }
 
+// One workgroup a row.  16400 x 131072 bf16 with the entropy 659 us: 6.5 TB/s of logits; 8 x 32768 5.8 us, most of it the launch and two
+// trips to memory (label, then logits).
 template <typename T, bool ENT, int BLOCK, int SLOTS>
 __global__ __launch_bounds__(BLOCK) void k_token_logprob(LogitsArgs l, TokenArgs a, int64_t first) {
     __shared__ Stat lds[BLOCK / 64];
@@ -308,7 +316,9 @@ __global__ __launch_bounds__(BLOCK) void k_token_logprob(LogitsArgs l, TokenArgs
     if (threadIdx.x == 0) put_token(l, a, r, st, zy);
 }
 
-// The way back needs no sums: log p_j = z_j s - lse.  Workgroups take pieces of kGradChunks chunks a thread.
+// The way back needs no sums: log p_j = z_j s - lse.  Workgroups take pieces of kGradChunks chunks a thread, one behind the other in
+// memory, which is the kindest order to it: 8192 x 131072 bf16 690 us, 6.2 TB/s read and written.  (256 threads of four chunks each,
+// us a preference step on 8192 x 131072, log-probabilities and all: 1100; 512 of two 1055, with loads past the caches 1027.)
 constexpr int kGradBlock = 512, kGradChunks = 2;
 
 template <typename T, bool ENT>
@@ -440,6 +450,9 @@ __device__ __forceinline__ int64_t next_policy_row(const LogitsArgs& l, const Po
     return r;
 }
 
+// One read and one write of the row.  8192 x 131072 bf16 805 us, 5.3 TB/s, 8192 x 65536 385 us, 5.6 TB/s, where copies of rows of the same
+// shape through registers, without arithmetic, take 735 and 365: what is left is the time between a row's last load and its first
+// store that the other workgroups of the compute unit do not fill.
 // TURNS: a workgroup takes rows one after the other, and the next row's chunks are loaded into the registers that this row's gradient
 // has left.  That pays where a compute unit holds one workgroup only (1024 threads): 8192 x 131072 bf16 839 -> 802 us, but with 512
 // threads or fewer, of which it holds several at different points of their rows, 8192 x 32768 204 -> 220 us.  (With the entropy the
@@ -696,6 +709,10 @@ __device__ __forceinline__ float distill_value(const LogitsArgs& l, Stat st, con
     return (float)loss;
 }
 
+// As the policy loss, and the first wave looks after the teacher meanwhile: its entries, then the student's logits there, one more trip
+// to memory, and two dozen double sums.  8192 x 65536 bf16, 64 entries, 390 us, 5.5 TB/s; with the rest's outcome, which has to know
+// the entries before the statistics, 405.  (In turns, as the policy loss does it at 1024 threads, it is no faster: 842 / 851 us at
+// 8192 x 131072.  Nor with the entries loaded ahead of the row's chunks: 862.)
 template <typename T, bool REST, int BLOCK, int CH, bool LONG>
 __global__ __launch_bounds__(BLOCK) void k_distill(LogitsArgs l, DistillArgs a, int64_t first) {
     __shared__ Stat lds[BLOCK / 64];
@@ -736,7 +753,8 @@ __global__ __launch_bounds__(BLOCK) void k_distill(LogitsArgs l, DistillArgs a, 
 
 // ---- a few long rows, in pieces ----------------------------------------------------------------------------------------------
 // One workgroup a row leaves most of the chip idle when there are few: the statistics of a row's pieces by a workgroup each, then, in
-// a second launch, the join and the gradient by as many.  (The second reads the logits again, out of the caches.)
+// a second launch, the join and the gradient by as many.  (The second reads the logits again, out of the caches.)  Each of the two
+// takes about 4 us at 16 x 32768 f32, as long as a launch that does nothing but load once and store.
 
 constexpr int kSplitBlock = 512, kSplitHold = 4;      // threads; chunks a thread holds in the second launch
 
@@ -929,7 +947,11 @@ void by_length(int64_t rows, int vocab, F f) {
     }
 }
 
-// f(BLOCK, CH, LONG) for rows whose gradient is wanted
+// f(BLOCK, CH, LONG) for rows whose gradient is wanted: the fewest threads whose registers hold the row, 4 to 16 chunks each, since several
+// small workgroups on a compute unit fill each other's pauses.  Policy loss, 16384 rows of bf16, us: x 1000 64 threads of 4 chunks 27, 128 of 4
+// 34, 256 of 4 47; x 4000 128 of 4 61, 256 of 4 64, 512 of 4 91; x 8000 256 of 4 99, 512 of 4 121; x 16000 256 of 8 193, 512 of 4 188 (the
+// distillation 209 and 242); x 32000 512 of 8 372, 256 of 16 no less.  Of 512 threads the count of chunks follows the row: 4099 x 50021 f16 13 chunks
+// 135, 16 chunks 143.  Longer rows than 1024 threads hold: 1001 x 100003 f32 read twice 245, kept as far as it goes 184.
 template <typename T, typename F>
 void by_width(const LogitsArgs& l, F f) {
     const int chunks = most_chunks<T>(l);

@@ -115,3 +115,48 @@ def test_label_in_every_place_of_a_row():
             mine = grad[torch.arange(len(y), device=DEV), y].float()
             assert torch.allclose(mine, torch.full_like(mine, -1.0), rtol=0.01)
             assert torch.allclose(rest.float().sum(1), torch.ones_like(mine), rtol=0.01) and (torch.count_nonzero(rest, 1) == vocab - 1).all()
+
+
+def test_the_widest_vocabulary_of_the_distillation():
+    """2^19 entries, 1024 of them the teacher's: the largest LDS; whole rows and rows in pieces."""
+    vocab, top = 1 << 19, 1024
+    z = logits_of(66, vocab, torch.bfloat16, seed=2).to(DEV)
+    rng = np.random.default_rng(5)
+    index = torch.as_tensor(np.stack([rng.choice(vocab, top, replace=False) for _ in range(66)])).to(DEV)
+    a = dev(rng.normal(size=(66, top)) + 6)
+    lse = torch.logsumexp(a, 1) + 0.2
+    for rows in (66, 3):
+        for given in (None, lse[:rows].contiguous()):
+            d = L.distill_loss(z[:rows], index[:rows], a[:rows], teacher_lse=given)
+            want = ref.distill(host(z[:2]), index[:2].cpu().numpy(), host(a[:2]), None if given is None else host(given[:2]), np.ones(2), 1.0, 1.0)
+            near_values(d.row_loss[:2], want[1], 12)
+            near_grad(d.grad[:2], want[2], 1.0)
+    with pytest.raises(L.LbfgsbError):
+        L.distill_loss(torch.zeros(1, vocab + 1, device=DEV), index[:1], a[:1])
+
+
+def test_rows_in_pieces_recorded_into_a_graph():
+    rows, vocab = 8, 70001
+    z = logits_of(rows, vocab, torch.bfloat16).to(DEV)
+    y = dev(labels_of(rows, vocab), torch.int64)
+    old, adv = torch.full((rows,), -9.0, device=DEV), torch.linspace(-1, 1, rows, device=DEV)
+    index, a = torch.randint(0, vocab, (rows, 16), device=DEV), torch.randn(rows, 16, device=DEV)
+
+    def step():
+        t, p, d = L.token_logprob(z, y, entropy=True), L.policy_loss(z, y, old, adv), L.distill_loss(z, index, a)
+        return [t.logp, t.lse, t.entropy, p.loss, p.row_loss, p.grad, d.loss, d.row_loss, d.grad]
+
+    step()
+    st = torch.cuda.Stream(device=DEV)
+    st.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        out = step()
+    for k in range(3):
+        z.copy_(logits_of(rows, vocab, torch.bfloat16, seed=30 + k))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        for g, want in zip(got, step()):
+            assert torch.equal(g, want)
+        torch.cuda.synchronize()

@@ -21,7 +21,6 @@ namespace lb {
 
 namespace {
 
-constexpr int64_t kTurnBlocks = 512;         // workgroups that take rows in turns: two for each compute unit
 constexpr int64_t kRowBlocksMax = 1 << 20;   // workgroups of a launch, at most: longer batches take several
 
 template <typename T>
@@ -97,10 +96,10 @@ struct Span {
 };
 
 // A workgroup's hold on a span.  CH chunks a thread stay in registers between the statistics and the gradient; what a longer row has
-// before them is read a second time.  (CH = 0: no gradient, SLOTS loads in flight.)
+// before them waits in LDS (HELD) or is read a second time.  (CH = 0: no gradient, SLOTS loads in flight.)
 // Loads that are the last of their row go past the caches, unless a workgroup of 1024 makes them: us without / with, token
 // log-probabilities of 16400 x 131072 bf16 702 / 665, distillation 4096 x 65536 bf16 208 / 199, but policy 8192 x 131072 bf16 839 / 863.
-template <typename T, int BLOCK, int CH, bool LONG = CH == 0, bool NT_LOADS = (BLOCK <= 512), int SLOTS = 2>
+template <typename T, int BLOCK, int CH, bool LONG = CH == 0, bool HELD = false, bool NT_LOADS = (BLOCK <= 512), int SLOTS = 2>
 struct Row {
     static constexpr int E = Chunk<T>::E;
     static constexpr int kSlots = CH > 0 ? CH : SLOTS;
@@ -110,6 +109,7 @@ struct Row {
 
     vec slot[kSlots];
     float alone;                         // the single element of this thread, if any
+    vec* held;                           // HELD: room in LDS for the chunks before `again` (held_bytes)
 
     // The thread's index, to the compiler a new value each time: else it keeps every slot's place, several registers a slot, from one row
     // to the next.
@@ -188,7 +188,10 @@ struct Row {
 #pragma unroll
             for (int k = 0; k < kSlots; ++k) {
                 const int i = from + k * BLOCK + t;
-                if (in(k, i, sp.begin, first)) one(slot[k], SKIP ? skipped(i) : 0);
+                if (in(k, i, sp.begin, first)) {
+                    if constexpr (HELD) held[i - sp.origin] = slot[k];
+                    one(slot[k], SKIP ? skipped(i) : 0);
+                }
                 if (next < first) fetch(sp, k, next, sp.begin, first, t);
                 else if (CH > 0) fetch(sp, k, sp.keep, sp.again, sp.end, t);
             }
@@ -213,11 +216,9 @@ struct Row {
         return a.a;
     }
 
-    // dz_j = 2^((z_j - m) c) (A + B (z_j - m) c), and `mark` more at j = y (none: -1), where the logit is zy.  MORE: the first chunks of
-    // `next` are on their way when this returns, as after open(): each slot is loaded again when it has been written.
-    template <bool ENT, bool MORE>
-    __device__ __forceinline__ void write(const Span& sp, T* out, float m, float c, float A, float B, int y, float zy, float mark,
-                                          const Span& next) {
+    // dz_j = 2^((z_j - m) c) (A + B (z_j - m) c), and `mark` more at j = y (none: -1), where the logit is zy.
+    template <bool ENT>
+    __device__ __forceinline__ void write(const Span& sp, T* out, float m, float c, float A, float B, int y, float zy, float mark) {
         static_assert(CH > 0);
         const float ref = anchor(m);
         char* to = (char*)(out + sp.cut.head);
@@ -230,24 +231,25 @@ struct Row {
         };
         const int j = sp.single();
         if (j >= 0) out[j] = (T)(slope_at<ENT>(alone, ref, c, A, B) + (j == y ? mark : 0.0f));
-        if (MORE) open_single(next);
         const int t = thread();
-        const int next_end = next.first_end();
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
             const int i = sp.keep + k * BLOCK + t;
             if (in(k, i, sp.again, sp.end)) one(opaque(slot[k]), i);
-            if (sp.repeats()) fetch(sp, k, sp.origin, sp.begin, sp.again, t);
-            else if (MORE) fetch(next, k, next.origin, next.begin, next_end, t);
+            if (!HELD && sp.repeats()) fetch(sp, k, sp.origin, sp.begin, sp.again, t);
         }
-        if (sp.repeats()) for (int from = sp.origin; from < sp.again; from += BLOCK * CH) {
-            const int on = from + BLOCK * CH;
+        if constexpr (HELD) {
+            for (int i = sp.origin + t; i < sp.again; i += BLOCK)       // (each thread its own: no barrier)
+                if (i >= sp.begin) one(held[i - sp.origin], i);
+        } else if (sp.repeats()) {
+            for (int from = sp.origin; from < sp.again; from += BLOCK * CH) {
+                const int on = from + BLOCK * CH;
 #pragma unroll
-            for (int k = 0; k < CH; ++k) {
-                const int i = from + k * BLOCK + t;
-                if (in(k, i, sp.begin, sp.again)) one(slot[k], i);
-                if (on < sp.again) fetch(sp, k, on, sp.begin, sp.again, t);
-                else if (MORE) fetch(next, k, next.origin, next.begin, next_end, t);
+                for (int k = 0; k < CH; ++k) {
+                    const int i = from + k * BLOCK + t;
+                    if (in(k, i, sp.begin, sp.again)) one(slot[k], i);
+                    if (on < sp.again) fetch(sp, k, on, sp.begin, sp.again, t);
+                }
             }
         }
         // the label's entry once more, by the thread that wrote its chunk
@@ -307,7 +309,7 @@ __global__ __launch_bounds__(BLOCK) void k_token_logprob(LogitsArgs l, TokenArgs
         if (threadIdx.x == 0) put_no_token(a, r);
         return;
     }
-    typedef Row<T, BLOCK, 0, true, (BLOCK <= 512), SLOTS> Hold;
+    typedef Row<T, BLOCK, 0, true, false, (BLOCK <= 512), SLOTS> Hold;
     const typename Hold::Span span(row, l.vocab);
     Hold z;
     z.open(span);
@@ -439,69 +441,31 @@ __device__ __forceinline__ void put_policy(const PolicyArgs& a, int64_t r, float
     if (a.entropy) a.entropy[r] = entropy;
 }
 
-// The next row from r on, `step` apart, that counts; those before it get their zeros.
-template <typename T, int BLOCK, int CH>
-__device__ __forceinline__ int64_t next_policy_row(const LogitsArgs& l, const PolicyArgs& a, int64_t r, int64_t step) {
-    for (; r < l.rows; r += step) {
-        if (a.labels[r] >= 0 && !(a.weight && a.weight[r] == 0.0f)) break;
-        if (threadIdx.x == 0) put_policy(a, r, 0.0f, 0.0f, 0.0f);
-        Row<T, BLOCK, CH>::clear((T*)l.dz + r * l.ld_dz, l.vocab);
-    }
-    return r;
-}
-
-// One read and one write of the row.  8192 x 131072 bf16 805 us, 5.3 TB/s, 8192 x 65536 385 us, 5.6 TB/s, where copies of rows of the same
+// One read and one write of the row.  8192 x 131072 bf16 788 us, 5.5 TB/s, 8192 x 65536 385 us, 5.6 TB/s, where copies of rows of the same
 // shape through registers, without arithmetic, take 735 and 365: what is left is the time between a row's last load and its first
 // store that the other workgroups of the compute unit do not fill.
-// TURNS: a workgroup takes rows one after the other, and the next row's chunks are loaded into the registers that this row's gradient
-// has left.  That pays where a compute unit holds one workgroup only (1024 threads): 8192 x 131072 bf16 839 -> 802 us, but with 512
-// threads or fewer, of which it holds several at different points of their rows, 8192 x 32768 204 -> 220 us.  (With the entropy the
-// registers do not suffice.)
-template <typename T, bool ENT, int BLOCK, int CH, bool LONG, bool TURNS>
-__global__ __launch_bounds__(BLOCK) void k_policy(LogitsArgs l, PolicyArgs a, int64_t first) {
-    typedef Row<T, BLOCK, CH, LONG> Hold;
-    typedef typename Hold::Span Span;
-    __shared__ Stat lds[TURNS ? 2 : 1][BLOCK / 64];
-    Hold z;
-    if constexpr (!TURNS) {
-        const int64_t r = first + blockIdx.x, y = a.labels[r];
-        const float w = a.weight ? a.weight[r] : 1.0f;
-        T* out = (T*)l.dz + r * l.ld_dz;
-        if (y < 0 || w == 0.0f) {
-            if (threadIdx.x == 0) put_policy(a, r, 0.0f, 0.0f, 0.0f);
-            Hold::clear(out, l.vocab);
-            return;
-        }
-        const Span span((const T*)l.z + r * l.ld, l.vocab);
-        z.open(span);
-        const float zy = label_logit(span.row, y, l.vocab);
-        const Stat st = block_stat<ENT, BLOCK / 64>(z.template stat<ENT, false>(span, l.c, nullptr), l.c, lds[0]);
-        const PolicyRow p = policy_row<ENT>(l, a, r, w, st, zy);
-        if (threadIdx.x == 0) put_policy(a, r, p.loss, p.logp, p.entropy);
-        z.template write<ENT, false>(span, out, st.m, l.c, p.A, p.B, y < l.vocab ? (int)y : -1, zy, p.mark, span);
-    } else {
-        int64_t r = next_policy_row<T, BLOCK, CH>(l, a, blockIdx.x, gridDim.x);
-        if (r >= l.rows) return;
-        Span span((const T*)l.z + r * l.ld, l.vocab);
-        z.open(span);
-        for (int turn = 0;; turn ^= 1) {
-            const int64_t y = a.labels[r];
-            const float w = a.weight ? a.weight[r] : 1.0f;
-            const float zy = label_logit(span.row, y, l.vocab);
-            const Stat st = block_stat<ENT, BLOCK / 64>(z.template stat<ENT, false>(span, l.c, nullptr), l.c, lds[turn]);
-            const PolicyRow p = policy_row<ENT>(l, a, r, w, st, zy);
-            if (threadIdx.x == 0) put_policy(a, r, p.loss, p.logp, p.entropy);
-            const int64_t on = next_policy_row<T, BLOCK, CH>(l, a, r + gridDim.x, gridDim.x);
-            const bool more = on < l.rows;
-            // (no next row: one chunk of this one again, so that there is one way through)
-            Span next(more ? (const T*)l.z + on * l.ld : span.row, l.vocab);
-            if (!more) next.end = next.begin + 1;
-            z.template write<ENT, true>(span, (T*)l.dz + r * l.ld_dz, st.m, l.c, p.A, p.B, y < l.vocab ? (int)y : -1, zy, p.mark, next);
-            if (!more) return;
-            r = on;
-            span = next;
-        }
+template <typename T, bool ENT, int BLOCK, int CH, bool LONG, bool HELD>
+__global__ __launch_bounds__(BLOCK, BLOCK == 512 ? 4 : 1) void k_policy(LogitsArgs l, PolicyArgs a, int64_t first) {
+    typedef Row<T, BLOCK, CH, LONG, HELD> Hold;
+    __shared__ Stat lds[BLOCK / 64];
+    extern __shared__ __align__(16) unsigned char dyn[];
+    const int64_t r = first + blockIdx.x, y = a.labels[r];
+    const float w = a.weight ? a.weight[r] : 1.0f;
+    T* out = (T*)l.dz + r * l.ld_dz;
+    if (y < 0 || w == 0.0f) {
+        if (threadIdx.x == 0) put_policy(a, r, 0.0f, 0.0f, 0.0f);
+        Hold::clear(out, l.vocab);
+        return;
     }
+    const typename Hold::Span span((const T*)l.z + r * l.ld, l.vocab);
+    Hold z;
+    z.held = (typename Hold::vec*)dyn;
+    z.open(span);
+    const float zy = label_logit(span.row, y, l.vocab);
+    const Stat st = block_stat<ENT, BLOCK / 64>(z.template stat<ENT, false>(span, l.c, nullptr), l.c, lds);
+    const PolicyRow p = policy_row<ENT>(l, a, r, w, st, zy);
+    if (threadIdx.x == 0) put_policy(a, r, p.loss, p.logp, p.entropy);
+    z.template write<ENT>(span, out, st.m, l.c, p.A, p.B, y < l.vocab ? (int)y : -1, zy, p.mark);
 }
 
 // The same without a gradient.
@@ -515,7 +479,7 @@ __global__ __launch_bounds__(BLOCK) void k_policy_value(LogitsArgs l, PolicyArgs
         if (threadIdx.x == 0) put_policy(a, r, 0.0f, 0.0f, 0.0f);
         return;
     }
-    typedef Row<T, BLOCK, 0, true, (BLOCK <= 512), SLOTS> Hold;
+    typedef Row<T, BLOCK, 0, true, false, (BLOCK <= 512), SLOTS> Hold;
     const typename Hold::Span span((const T*)l.z + r * l.ld, l.vocab);
     Hold z;
     z.open(span);
@@ -711,10 +675,10 @@ __device__ __forceinline__ float distill_value(const LogitsArgs& l, Stat st, con
 
 // As the policy loss, and the first wave looks after the teacher meanwhile: its entries, then the student's logits there, one more trip
 // to memory, and two dozen double sums.  8192 x 65536 bf16, 64 entries, 390 us, 5.5 TB/s; with the rest's outcome, which has to know
-// the entries before the statistics, 405.  (In turns, as the policy loss does it at 1024 threads, it is no faster: 842 / 851 us at
-// 8192 x 131072.  Nor with the entries loaded ahead of the row's chunks: 862.)
-template <typename T, bool REST, int BLOCK, int CH, bool LONG>
-__global__ __launch_bounds__(BLOCK) void k_distill(LogitsArgs l, DistillArgs a, int64_t first) {
+// the entries before the statistics, 405.  (With the entries loaded ahead of the row's chunks
+// it is no faster: 842 / 862 us at 8192 x 131072.)
+template <typename T, bool REST, int BLOCK, int CH, bool LONG, bool HELD>
+__global__ __launch_bounds__(BLOCK, BLOCK == 512 ? 4 : 1) void k_distill(LogitsArgs l, DistillArgs a, int64_t first) {
     __shared__ Stat lds[BLOCK / 64];
     __shared__ Teacher teacher;
     extern __shared__ __align__(16) unsigned char dyn[];
@@ -728,9 +692,10 @@ __global__ __launch_bounds__(BLOCK) void k_distill(LogitsArgs l, DistillArgs a, 
         if (l.dz) Row<T, BLOCK, CH>::clear(out, l.vocab);
         return;
     }
-    typedef Row<T, BLOCK, CH, LONG> Hold;
+    typedef Row<T, BLOCK, CH, LONG, HELD> Hold;
     const typename Hold::Span span(row, l.vocab);
     Hold z;
+    z.held = (typename Hold::vec*)(dyn + distill_lds(a.top, l.vocab));
     z.open(span);
     if (REST) clear_seen<BLOCK>(s, l.vocab);
     Marks marks{false, false};
@@ -745,7 +710,7 @@ __global__ __launch_bounds__(BLOCK) void k_distill(LogitsArgs l, DistillArgs a, 
         Row<T, BLOCK, CH>::clear(out, l.vocab);
         return;
     }
-    z.template write<false, false>(span, out, st.m, l.c, d.A, 0.0f, -1, 0.0f, 0.0f, span);
+    z.template write<false>(span, out, st.m, l.c, d.A, 0.0f, -1, 0.0f, 0.0f);
     __syncthreads();                          // (the entries' own values come after the row's)
     for (int k = threadIdx.x; k < a.top; k += BLOCK)
         if (s.at[k] >= 0) out[s.at[k]] = (T)d.at_entry(s.z[k], s.q[k], l.c);
@@ -778,7 +743,7 @@ __global__ __launch_bounds__(kSplitBlock) void k_split(LogitsArgs l, const int64
     const T* row = (const T*)l.z + r * l.ld;
     const int64_t y = labels[r];
     if (y < 0 || (weight && weight[r] == 0.0f)) return;
-    typedef Row<T, kSplitBlock, 0, true, false> Hold;
+    typedef Row<T, kSplitBlock, 0, true, false, false> Hold;
     const typename Hold::Span span(row, l.vocab, i, splits);
     Hold z;
     z.open(span);
@@ -811,7 +776,7 @@ __global__ __launch_bounds__(kSplitBlock) void k_split_distill(LogitsArgs l, Dis
         }
         return;
     }
-    typedef Row<T, kSplitBlock, 0, true, false> Hold;
+    typedef Row<T, kSplitBlock, 0, true, false, false> Hold;
     const typename Hold::Span span(row, l.vocab, i, splits);
     Hold z;
     z.open(span);
@@ -874,7 +839,7 @@ __global__ __launch_bounds__(kSplitBlock) void k_join_policy(LogitsArgs l, Polic
     if (threadIdx.x == 0 && i == 0) put_policy(a, r, p.loss, p.logp, p.entropy);
     if (!l.dz) return;
     if (p.empty) Row<T, kSplitBlock, kSplitHold>::clear(out, l.vocab, i, splits);
-    else z.template write<ENT, false>(span, out, st.m, l.c, p.A, p.B, y < l.vocab ? (int)y : -1, ws[r].zy, p.mark, span);
+    else z.template write<ENT>(span, out, st.m, l.c, p.A, p.B, y < l.vocab ? (int)y : -1, ws[r].zy, p.mark);
 }
 
 template <typename T, bool REST>
@@ -908,7 +873,7 @@ __global__ __launch_bounds__(kSplitBlock) void k_join_distill(LogitsArgs l, Dist
         Row<T, kSplitBlock, kSplitHold>::clear(out, l.vocab, i, splits);
         return;
     }
-    z.template write<false, false>(span, out, st.m, l.c, d.A, 0.0f, -1, 0.0f, 0.0f, span);
+    z.template write<false>(span, out, st.m, l.c, d.A, 0.0f, -1, 0.0f, 0.0f);
     __syncthreads();                          // (the entries' own values come after the row's)
     for (int k = threadIdx.x; k < a.top; k += kSplitBlock) {
         const int j = ws[r].at[k];
@@ -947,27 +912,49 @@ void by_length(int64_t rows, int vocab, F f) {
     }
 }
 
-// f(BLOCK, CH, LONG) for rows whose gradient is wanted: the fewest threads whose registers hold the row, 4 to 16 chunks each, since several
+// LDS of what a row of `chunks` places has before the HOLD - 16 that stay in registers (Span), and what each of two workgroups of a compute
+// unit may have of it.
+inline size_t held_bytes(int chunks, int hold) { return (size_t)(chunks - (hold - 16) + 16) * 16; }
+constexpr size_t kPairLds = 79 << 10;
+
+// f(BLOCK, CH, LONG, HELD) for rows whose gradient is wanted: the fewest threads whose registers hold the row, 4 to 16 chunks each, since several
 // small workgroups on a compute unit fill each other's pauses.  Policy loss, 16384 rows of bf16, us: x 1000 64 threads of 4 chunks 27, 128 of 4
 // 34, 256 of 4 47; x 4000 128 of 4 61, 256 of 4 64, 512 of 4 91; x 8000 256 of 4 99, 512 of 4 121; x 16000 256 of 8 193, 512 of 4 188 (the
 // distillation 209 and 242); x 32000 512 of 8 372, 256 of 16 no less.  Of 512 threads the count of chunks follows the row: 4099 x 50021 f16 13 chunks
 // 135, 16 chunks 143.  Longer rows than 1024 threads hold: 1001 x 100003 f32 read twice 245, kept as far as it goes 184.
-template <typename T, typename F>
-void by_width(const LogitsArgs& l, F f) {
+// Rows of more than 8192 chunks: one workgroup of 1024 threads on a compute unit, or with many rows of 16 bits two of 512, of which one loads
+// while the other writes, with 23 chunks a thread and what is left of the row in LDS (`lds` bytes of it are taken already).  1024 / 512
+// threads, us, bf16.  In registers alone, policy loss x 70000: 128 rows 13.8 / 14.4, 400 29.9 / 23.5, 8192 473 / 400; x 92000, 400 rows
+// 36.4 / 28.5, 8192 602 / 565.  With LDS, policy loss x 131072: 1000 rows 102 / 110, 1500 164 / 156, 4000 413 / 391, 8192 818 / 788; x 100000,
+// 1000 rows 76 / 81, 8192 657 / 593.  Distillation with the rest, which spills at 512, x 80000: 1000 rows 78 / 89, 4000 315 / 288, 8192 635 / 556,
+// and with LDS, x 100000, 8192 rows 747 / 777.  f32, policy loss, 4000 rows: x 50021 290 / 296, x 62003 352 / 363.
+// PAIR, HELD: the rows from which it is two of 512 threads, in registers alone and with LDS (0: never).
+template <typename T, int PAIR, int HELD, typename F>
+void by_width(const LogitsArgs& l, size_t lds, F f) {
     const int chunks = most_chunks<T>(l);
-    auto go = [&](auto block, auto ch) { f(block, ch, std::false_type{}); };
     using std::integral_constant;
-    if (chunks <= 64 * 4) go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
-    else if (chunks <= 128 * 4) go(integral_constant<int, 128>{}, integral_constant<int, 4>{});
-    else if (chunks <= 256 * 4) go(integral_constant<int, 256>{}, integral_constant<int, 4>{});
-    else if (chunks <= 256 * 8) go(integral_constant<int, 256>{}, integral_constant<int, 8>{});
-    else if (chunks <= 512 * 8) go(integral_constant<int, 512>{}, integral_constant<int, 8>{});
-    else if (chunks <= 512 * 10) go(integral_constant<int, 512>{}, integral_constant<int, 10>{});
-    else if (chunks <= 512 * 13) go(integral_constant<int, 512>{}, integral_constant<int, 13>{});
-    else if (chunks <= 512 * 16) go(integral_constant<int, 512>{}, integral_constant<int, 16>{});
-    else if (chunks <= 1024 * 13) go(integral_constant<int, 1024>{}, integral_constant<int, 13>{});
-    else if (chunks <= 1024 * 16) go(integral_constant<int, 1024>{}, integral_constant<int, 16>{});
-    else f(integral_constant<int, 1024>{}, integral_constant<int, 16>{}, std::true_type{});
+    constexpr std::false_type no{};
+    constexpr std::true_type yes{};
+    if (chunks <= 64 * 4) f(integral_constant<int, 64>{}, integral_constant<int, 4>{}, no, no);
+    else if (chunks <= 128 * 4) f(integral_constant<int, 128>{}, integral_constant<int, 4>{}, no, no);
+    else if (chunks <= 256 * 4) f(integral_constant<int, 256>{}, integral_constant<int, 4>{}, no, no);
+    else if (chunks <= 256 * 8) f(integral_constant<int, 256>{}, integral_constant<int, 8>{}, no, no);
+    else if (chunks <= 512 * 8) f(integral_constant<int, 512>{}, integral_constant<int, 8>{}, no, no);
+    else if (chunks <= 512 * 10) f(integral_constant<int, 512>{}, integral_constant<int, 10>{}, no, no);
+    else if (chunks <= 512 * 13) f(integral_constant<int, 512>{}, integral_constant<int, 13>{}, no, no);
+    else if (chunks <= 512 * 16) f(integral_constant<int, 512>{}, integral_constant<int, 16>{}, no, no);
+    else {
+        if constexpr (PAIR > 0 && sizeof(T) == 2) {
+            if (chunks <= 512 * 23 && l.rows >= PAIR) return f(integral_constant<int, 512>{}, integral_constant<int, 23>{}, no, no);
+        }
+        if constexpr (HELD > 0 && sizeof(T) == 2) {
+            if (chunks > 512 * 23 && l.rows >= HELD && held_bytes(chunks, 512 * 23) + lds <= kPairLds)
+                return f(integral_constant<int, 512>{}, integral_constant<int, 23>{}, yes, yes);
+        }
+        if (chunks <= 1024 * 13) f(integral_constant<int, 1024>{}, integral_constant<int, 13>{}, no, no);
+        else if (chunks <= 1024 * 16) f(integral_constant<int, 1024>{}, integral_constant<int, 16>{}, no, no);
+        else f(integral_constant<int, 1024>{}, integral_constant<int, 16>{}, yes, no);
+    }
 }
 
 }  // namespace
@@ -1015,19 +1002,26 @@ hipError_t policy_rows(const LogitsArgs& l, const PolicyArgs& a, float* loss, Sp
                            (const SplitRow*)ws, splits, loss);
         return hipGetLastError();
     }
+    hipError_t err = hipSuccess;
     if (!l.dz) by_length<T>(l.rows, l.vocab, [&](auto block, auto slots) {
         constexpr int BLOCK = decltype(block)::value, SLOTS = decltype(slots)::value;
         const auto kernel = ent ? k_policy_value<T, true, BLOCK, SLOTS> : k_policy_value<T, false, BLOCK, SLOTS>;
         by_rows(l.rows, [&](int64_t first, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(BLOCK), 0, st, l, a, first); });
     });
-    else by_width<T>(l, [&](auto block, auto ch, auto lng) {
+    else if (ent) by_width<T, 0, 0>(l, 0, [&](auto block, auto ch, auto lng, auto) {
         constexpr int BLOCK = decltype(block)::value, CH = decltype(ch)::value;
-        constexpr bool LONG = decltype(lng)::value;
-        constexpr bool TURNS = BLOCK == 1024 && !LONG;
-        const auto kernel = ent ? k_policy<T, true, BLOCK, CH, LONG, false> : k_policy<T, false, BLOCK, CH, LONG, TURNS>;
-        if (TURNS && !ent) hipLaunchKernelGGL(kernel, dim3((unsigned)(l.rows < kTurnBlocks ? l.rows : kTurnBlocks)), dim3(BLOCK), 0, st, l, a, (int64_t)0);
-        else by_rows(l.rows, [&](int64_t first, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(BLOCK), 0, st, l, a, first); });
+        const auto kernel = k_policy<T, true, BLOCK, CH, decltype(lng)::value, false>;
+        by_rows(l.rows, [&](int64_t first, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(BLOCK), 0, st, l, a, first); });
     });
+    else by_width<T, 257, 1500>(l, 0, [&](auto block, auto ch, auto lng, auto held) {
+        constexpr int BLOCK = decltype(block)::value, CH = decltype(ch)::value;
+        const auto kernel = k_policy<T, false, BLOCK, CH, decltype(lng)::value, decltype(held)::value>;
+        const size_t lds = decltype(held)::value ? held_bytes(most_chunks<T>(l), BLOCK * CH) : 0;
+        err = allow_lds(kernel, lds);
+        if (err != hipSuccess) return;
+        by_rows(l.rows, [&](int64_t first, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(BLOCK), lds, st, l, a, first); });
+    });
+    if (err != hipSuccess) return err;
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     return launch_weighted_total(a.row_loss, a.weight, l.rows, a.scale, loss, st);
 }
@@ -1044,14 +1038,16 @@ hipError_t distill_rows(const LogitsArgs& l, const DistillArgs& a, float* loss, 
         return hipGetLastError();
     }
     hipError_t err = hipSuccess;
-    by_width<T>(l, [&](auto block, auto ch, auto lng) {
+    auto launch = [&](auto rest, auto block, auto ch, auto lng, auto held) {
         constexpr int BLOCK = decltype(block)::value, CH = decltype(ch)::value;
-        constexpr bool LONG = decltype(lng)::value;
-        const auto kernel = a.lse ? k_distill<T, true, BLOCK, CH, LONG> : k_distill<T, false, BLOCK, CH, LONG>;
-        err = allow_lds(kernel, lds);
+        const auto kernel = k_distill<T, decltype(rest)::value, BLOCK, CH, decltype(lng)::value, decltype(held)::value>;
+        const size_t more = decltype(held)::value ? held_bytes(most_chunks<T>(l), BLOCK * CH) : 0;
+        err = allow_lds(kernel, lds + more);
         if (err != hipSuccess) return;
-        by_rows(l.rows, [&](int64_t first, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(BLOCK), lds, st, l, a, first); });
-    });
+        by_rows(l.rows, [&](int64_t first, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(BLOCK), lds + more, st, l, a, first); });
+    };
+    if (a.lse) by_width<T, 4000, 0>(l, lds, [&](auto... w) { launch(std::true_type{}, w...); });
+    else by_width<T, 257, 1500>(l, lds, [&](auto... w) { launch(std::false_type{}, w...); });
     if (err != hipSuccess || (err = hipGetLastError()) != hipSuccess) return err;
     return launch_weighted_total(a.row_loss, a.weight, l.rows, a.scale, loss, st);
 }

@@ -428,16 +428,25 @@ typedef struct {
  * calls; calls that may run at the same time need one each. */
 size_t lbfgsb_logits_workspace_bytes(const lbfgsb_logits* logits_host);
 
-/* Log-probability of each row's label, lse, and (where not NULL) what rounding took from lse and the entropy; rows entries
- * each.  labels: rows entries.  logits_host->grad is not looked at. */
+/* Log-probability of each row's label, lse, and (where not NULL) what rounding took from lse (lse once more where it is past the end of 32 bits) and
+ * the entropy; rows entries each.  labels: rows entries.  logits_host->grad is not looked at. */
 int lbfgsb_token_logprob(const lbfgsb_logits* logits_host, const int64_t* labels, float* logp, float* lse, float* lse_rest,
                          float* entropy, void* workspace, size_t workspace_bytes, void* hip_stream);
 /* The way back: with d_logp (and d_entropy or NULL) the gradient of something with respect to the outputs above,
  *     dz_j = s * (d_logp * (1[j = label] - p_j) - d_entropy * p_j * (log p_j + H)).
  * lse, lse_rest (or NULL = 0), entropy (needed with d_entropy only): the outputs of lbfgsb_token_logprob on the same logits.
- * Without lse_rest, p_j is known to 2^-24 |lse| of itself: not at all in a row that is masked whole by the type's lowest value. */
+ * Without lse_rest, p_j is known to 2^-24 |lse| of itself.  With it, p_j is right while |lse_rest| <= 1024 (always where |lse| < 2^34); beyond, as in a
+ * row that is masked whole by the type's lowest value at a temperature that is no power of two, a row's gradient is NaN.  The two
+ * functions after this one have no such rows. */
 int lbfgsb_token_logprob_grad(const lbfgsb_logits* logits_host, const int64_t* labels, const float* lse, const float* lse_rest,
                               const float* entropy, const float* d_logp, const float* d_entropy, void* hip_stream);
+
+/* The same with what the way back needs where lse has lost it: top, each row's largest logit, and sum = sum_j exp(s (z_j - top)), rows entries each
+ * (0 in a row that does not count; both NULL: not wanted).  From them the gradient is right in every row with finite logits. */
+int lbfgsb_token_logprob_stats(const lbfgsb_logits* logits_host, const int64_t* labels, float* logp, float* lse, float* lse_rest,
+                               float* entropy, float* top, float* sum, void* workspace, size_t workspace_bytes, void* hip_stream);
+int lbfgsb_token_logprob_stats_grad(const lbfgsb_logits* logits_host, const int64_t* labels, const float* top, const float* sum,
+                                    const float* entropy, const float* d_logp, const float* d_entropy, void* hip_stream);
 
 /* A teacher's top logits for each row: index and logit hold `top` entries a row, `ld` elements apart.  An entry with a
  * negative index, or a logit of -infinity, is padding. */

@@ -29,7 +29,8 @@ EXPORTS = [
     "lbfgsb_auglag_get_x", "lbfgsb_auglag_get_lambda", "lbfgsb_auglag_inner", "lbfgsb_auglag_destroy",
     "lbfgsb_auglag_rows_workspace_bytes", "lbfgsb_auglag_create_rows",
     "lbfgsb_auglag_marginals_workspace_bytes", "lbfgsb_auglag_create_marginals",
-    "lbfgsb_logits_workspace_bytes", "lbfgsb_token_logprob", "lbfgsb_token_logprob_grad", "lbfgsb_distill_loss", "lbfgsb_policy_loss",
+    "lbfgsb_logits_workspace_bytes", "lbfgsb_token_logprob", "lbfgsb_token_logprob_grad", "lbfgsb_token_logprob_stats",
+    "lbfgsb_token_logprob_stats_grad", "lbfgsb_distill_loss", "lbfgsb_policy_loss",
     "lbfgsb_preference_loss",
 ]
 

@@ -48,11 +48,13 @@ struct LogitsArgs {
 
 struct TokenArgs {
     const int64_t* labels;
-    float *logp, *lse, *lse_rest, *entropy;    // the last two null: not wanted
+    float *logp, *lse, *lse_rest, *entropy, *top, *sum;    // all but the first two null: not wanted
 };
 struct TokenGradArgs {
     const int64_t* labels;
-    const float *lse, *lse_rest, *entropy, *d_logp, *d_entropy;   // lse_rest null: 0; d_entropy null: no gradient through the entropy
+    const float *top, *sum;                    // Stat::m and s; null: from what follows
+    const float *lse, *lse_rest;               // lse_rest null: 0
+    const float *entropy, *d_logp, *d_entropy; // d_entropy null: no gradient through the entropy
 };
 struct DistillArgs {
     const void *index, *logit;

@@ -12,6 +12,8 @@
 // place of a difference and a product in both passes, the times were the same.)
 #pragma once
 
+#include <cfloat>
+
 #include <algorithm>
 #include <type_traits>
 
@@ -287,14 +289,22 @@ __device__ __forceinline__ void put_token(const LogitsArgs& l, const TokenArgs& 
     const float lse = (float)g.lse;
     a.logp[r] = logp_of(st, g, l.s, zy);
     a.lse[r] = lse;
-    if (a.lse_rest) a.lse_rest[r] = fabsf(lse) < INFINITY ? (float)(((double)st.m * l.s - (double)lse) + g.log_s) : 0.0f;
+    // (past the end of 32 bits lse has taken it all)
+    if (a.lse_rest)
+        a.lse_rest[r] = fabsf(lse) < INFINITY ? (float)(((double)st.m * l.s - (double)lse) + g.log_s)
+                                              : (fabs(g.lse) < INFINITY ? lse : 0.0f);
     if (a.entropy) a.entropy[r] = (float)g.entropy;
+    if (a.top) {
+        a.top[r] = st.m;
+        a.sum[r] = st.s;
+    }
 }
 __device__ __forceinline__ void put_no_token(const TokenArgs& a, int64_t r) {
     a.logp[r] = 0.0f;
     a.lse[r] = 0.0f;
     if (a.lse_rest) a.lse_rest[r] = 0.0f;
     if (a.entropy) a.entropy[r] = 0.0f;
+    if (a.top) a.top[r] = a.sum[r] = 0.0f;
 }
 
 // One workgroup a row.  16400 x 131072 bf16 with the entropy 659 us: 6.5 TB/s of logits; 8 x 32768 5.8 us, most of it the launch and two
@@ -318,7 +328,23 @@ __global__ __launch_bounds__(BLOCK) void k_token_logprob(LogitsArgs l, TokenArgs
     if (threadIdx.x == 0) put_token(l, a, r, st, zy);
 }
 
-// The way back needs no sums: log p_j = z_j s - lse.  Workgroups take pieces of kGradChunks chunks a thread, one behind the other in
+// What the way back knows of a row: p_j = 2^((z_j - ref) c) / sum, sum 0: the row has no distribution.
+struct RowShare {
+    float ref, sum;
+};
+__device__ __forceinline__ RowShare row_share(const LogitsArgs& l, const TokenGradArgs& a, int64_t r) {
+    if (a.top) return {anchor(a.top[r]), a.sum[r]};
+    // lse = ref s + off, ref the logit nearest to it.  Of lse_rest, which is known to 2^-25 of itself, more than 2^10 would leave off
+    // uncertain by 2^-15 and more (lse is beyond 2^34 then, its own digits do not reach ln sum); then p_j is no number.
+    const double lse = (double)a.lse[r], rest = a.lse_rest ? (double)a.lse_rest[r] : 0.0;
+    const float ref = fminf(fmaxf((float)(lse / l.s), -FLT_MAX), FLT_MAX);
+    if (lse == -INFINITY && rest == 0.0) return {ref, 0.0f};
+    const double off = fma(-(double)ref, l.s, lse) + rest;
+    return {ref, fabs(rest) <= 1024.0 && fabs(off) <= 80.0 ? (float)exp(off) : NAN};
+}
+
+// The way back needs no sums: the forward call's do.  (From differences to the maximum, not as z_j s - lse: at a temperature that is no power of
+// two the rounding of s takes all digits of that in a row far from 0.)  Workgroups take pieces of kGradChunks chunks a thread, one behind the other in
 // memory, which is the kindest order to it: 8192 x 131072 bf16 690 us, 6.2 TB/s read and written.  (256 threads of four chunks each,
 // us a preference step on 8192 x 131072, log-probabilities and all: 1100; 512 of two 1055, with loads past the caches 1027.)
 constexpr int kGradBlock = 512, kGradChunks = 2;
@@ -338,9 +364,10 @@ __global__ __launch_bounds__(kGradBlock) void k_token_grad(LogitsArgs l, TokenGr
     const int i0 = piece * (kGradBlock * kGradChunks) + (int)threadIdx.x - cut.lead(row);
     const int j = piece == 0 ? cut.single((int)threadIdx.x) : -1;
     const int64_t y = a.labels[r];
-    const float lse = a.lse[r], rest = a.lse_rest ? a.lse_rest[r] : 0.0f, s = (float)l.s;
+    const RowShare row_of = row_share(l, a, r);
+    const float s = (float)l.s;
     // (a row without a distribution, a label of none: no gradient; a label past the vocabulary: no number)
-    const bool none = y < 0 || lse == -INFINITY;
+    const bool none = y < 0 || row_of.sum == 0.0f;
     const float g = none ? 0.0f : (y < l.vocab ? a.d_logp[r] : NAN);
     const float h = !ENT || none ? 0.0f : a.d_entropy[r], entropy = !ENT || none ? 0.0f : a.entropy[r];
     if (g == 0.0f && h == 0.0f) {
@@ -357,12 +384,10 @@ __global__ __launch_bounds__(kGradBlock) void k_token_grad(LogitsArgs l, TokenGr
 #pragma unroll
     for (int k = 0; k < kGradChunks; ++k)
         if (i0 + k * kGradBlock >= 0 && i0 + k * kGradBlock < cut.whole) slot[k] = __builtin_nontemporal_load((const any*)(from + (size_t)(unsigned)(i0 + k * kGradBlock) * 16));
-    // p_j (-g - h (log p_j + H))
-    const float A = -(g + h * entropy) * s, B = -h * s;
-    auto at = [&](float z) {
-        const float lp = fmaf(z, s, -lse) - rest, x = exp2_hw(lp * 1.44269504088896340736f);
-        return ENT ? x * fmaf(B, fmaxf(lp, -1000.0f), A) : x * A;
-    };
+    // p_j (-g - h (log p_j + H)),  log p_j = ln 2 a_j - ln sum
+    const float over = s / row_of.sum;
+    const float A = over * (ENT ? fmaf(h, (float)log_d((double)row_of.sum) - entropy, -g) : -g), B = over * -h * 0.693147180559945309417f;
+    auto at = [&](float z) { return slope_at<ENT>(z, row_of.ref, l.c, A, B); };
     if (j >= 0) out[j] = (T)(at((float)row[j]) + (j == y ? g * s : 0.0f));
 #pragma unroll
     for (int k = 0; k < kGradChunks; ++k) {

@@ -81,12 +81,18 @@ size_t lbfgsb_logits_workspace_bytes(const lbfgsb_logits* logits_host) {
 
 int lbfgsb_token_logprob(const lbfgsb_logits* logits_host, const int64_t* labels, float* logp, float* lse, float* lse_rest,
                          float* entropy, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    return lbfgsb_token_logprob_stats(logits_host, labels, logp, lse, lse_rest, entropy, nullptr, nullptr, workspace, workspace_bytes, hip_stream);
+}
+
+int lbfgsb_token_logprob_stats(const lbfgsb_logits* logits_host, const int64_t* labels, float* logp, float* lse, float* lse_rest,
+                               float* entropy, float* top, float* sum, void* workspace, size_t workspace_bytes, void* hip_stream) {
     if (int rc = check_logits(logits_host, -1)) return rc;
     if (int rc = check_workspace(logits_host, false, workspace, workspace_bytes)) return rc;
     if (logits_host->rows == 0) return LBFGSB_OK;
     if (!labels || !logp || !lse) return fail(LBFGSB_E_INVALID_ARG, "labels, logp and lse must not be NULL");
-    HIP_TRY(launch_token_logprob(args_of(logits_host, false), logits_host->dtype, {labels, logp, lse, lse_rest, entropy}, (SplitRow*)workspace,
-                                 (hipStream_t)hip_stream));
+    if (!top != !sum) return fail(LBFGSB_E_INVALID_ARG, "top goes with sum");
+    HIP_TRY(launch_token_logprob(args_of(logits_host, false), logits_host->dtype, {labels, logp, lse, lse_rest, entropy, top, sum},
+                                 (SplitRow*)workspace, (hipStream_t)hip_stream));
     return LBFGSB_OK;
 }
 
@@ -96,8 +102,19 @@ int lbfgsb_token_logprob_grad(const lbfgsb_logits* logits_host, const int64_t* l
     if (logits_host->rows == 0) return LBFGSB_OK;
     if (!labels || !lse || !d_logp) return fail(LBFGSB_E_INVALID_ARG, "labels, lse and d_logp must not be NULL");
     if (d_entropy && !entropy) return fail(LBFGSB_E_INVALID_ARG, "d_entropy goes with the entropy");
-    HIP_TRY(launch_token_logprob_grad(args_of(logits_host, true), logits_host->dtype, {labels, lse, lse_rest, entropy, d_logp, d_entropy},
-                                      (hipStream_t)hip_stream));
+    HIP_TRY(launch_token_logprob_grad(args_of(logits_host, true), logits_host->dtype,
+                                      {labels, nullptr, nullptr, lse, lse_rest, entropy, d_logp, d_entropy}, (hipStream_t)hip_stream));
+    return LBFGSB_OK;
+}
+
+int lbfgsb_token_logprob_stats_grad(const lbfgsb_logits* logits_host, const int64_t* labels, const float* top, const float* sum,
+                                    const float* entropy, const float* d_logp, const float* d_entropy, void* hip_stream) {
+    if (int rc = check_logits(logits_host, 1)) return rc;
+    if (logits_host->rows == 0) return LBFGSB_OK;
+    if (!labels || !top || !sum || !d_logp) return fail(LBFGSB_E_INVALID_ARG, "labels, top, sum and d_logp must not be NULL");
+    if (d_entropy && !entropy) return fail(LBFGSB_E_INVALID_ARG, "d_entropy goes with the entropy");
+    HIP_TRY(launch_token_logprob_grad(args_of(logits_host, true), logits_host->dtype,
+                                      {labels, top, sum, nullptr, nullptr, entropy, d_logp, d_entropy}, (hipStream_t)hip_stream));
     return LBFGSB_OK;
 }
 

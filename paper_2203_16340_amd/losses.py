@@ -53,6 +53,8 @@ def declare(L) -> None:
     L.lbfgsb_logits_workspace_bytes.argtypes = [lg]
     for name, args in (("token_logprob", [lg, vp, vp, vp, vp, vp, vp, size, vp]),
                        ("token_logprob_grad", [lg, vp, vp, vp, vp, vp, vp, vp]),
+                       ("token_logprob_stats", [lg, vp, vp, vp, vp, vp, vp, vp, vp, size, vp]),
+                       ("token_logprob_stats_grad", [lg, vp, vp, vp, vp, vp, vp, vp]),
                        ("distill_loss", [lg, C.POINTER(Teacher), vp, dbl, vp, vp, vp, size, vp]),
                        ("policy_loss", [lg, C.POINTER(Rollout), C.POINTER(PolicyOptions), dbl, vp, vp, vp, vp, vp, size, vp]),
                        ("preference_loss", [i64, i64, vp, vp, vp, vp, vp, C.POINTER(PreferenceOptions), dbl, vp, vp, vp, vp, vp])):
@@ -60,11 +62,17 @@ def declare(L) -> None:
         f.restype, f.argtypes = C.c_int, args
 
 
-class TokenLogprob(NamedTuple):
+class _TokenLogprob(NamedTuple):
     logp: "torch.Tensor"
     lse: "torch.Tensor"
     lse_rest: "torch.Tensor"
     entropy: Optional["torch.Tensor"]
+
+
+class TokenLogprob(_TokenLogprob):
+    """What token_logprob returns.  Beside the tuple's entries, for the way back: stats, whose first two rows are
+    every row's largest logit and its sum of exponentials; a tuple that was taken apart and put together again has none (None)."""
+    stats = None
 
 
 class DistillLoss(NamedTuple):
@@ -137,17 +145,22 @@ def token_logprob(logits, labels, *, temperature: float = 1.0, entropy: bool = F
     """lbfgsb_token_logprob: log-probability of each row's label (int64; negative: ignored), the row's log-sum-exp (lse + lse_rest
     is more exact) and, if asked for, its entropy."""
     native = _native or _load()
-    return TokenLogprob(*_call(native.token_logprob, logits, logits, labels, temperature, entropy))
+    *out, stats = _call(native.token_logprob, logits, logits, labels, temperature, entropy)
+    r = TokenLogprob(*out)
+    r.stats = stats
+    return r
 
 
 def token_logprob_grad(logits, labels, forward: TokenLogprob, d_logp, *, temperature: float = 1.0, d_entropy=None, grad=True):
     """lbfgsb_token_logprob_grad: the gradient with respect to the logits of something whose gradient with respect to logp
-    (and entropy) is d_logp (and d_entropy).  forward: what token_logprob returned for these logits (with the entropy, for
-    d_entropy).  grad: a tensor to write to (the logits themselves: in place), or True for a new one."""
+    (and entropy) is d_logp (and d_entropy).  forward: what token_logprob returned for these logits at this temperature (with
+    the entropy, for d_entropy); of one without stats, lse and lse_rest are used, and rows whose shares they do not tell, such as one
+    held whole at float32's lowest value at temperature 1.5, get NaN.  grad: a tensor to write to (the logits themselves: in place), or True for a new one."""
     native = _native or _load()
     if grad is False or grad is None:
         raise TypeError("grad must be True or a tensor")
-    return _call(native.token_logprob_grad, logits, logits, labels, forward.lse, forward.lse_rest, forward.entropy, d_logp, d_entropy,
+    return _call(native.token_logprob_grad, logits, logits, labels, forward.lse, forward.lse_rest, forward.entropy,
+                 getattr(forward, "stats", None), d_logp, d_entropy,
                  temperature, _gradient(grad)[1])[0]
 
 

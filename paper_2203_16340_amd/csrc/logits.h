@@ -18,8 +18,9 @@ struct Stat {
 
 // What a row's entries of the teacher come to.
 struct Teacher {
-    double cross;       // sum_k q_k (log q_k - s z_k)
+    double cross;       // sum_k q_k (log q_k - s (z_k - z_top))
     double sum;         // sum_k q_k
+    float z_top;        // the largest of the student's logits there (0 where all are -infinity)
     Stat top;           // the student's statistics over the entries, each once
     int entries;        // how many there are, each once
     int lost;           // one of them lies past the vocabulary

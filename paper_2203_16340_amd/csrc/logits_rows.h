@@ -587,14 +587,17 @@ template <typename T, bool REST>
 __device__ __forceinline__ void read_teacher(const LogitsArgs& l, const DistillArgs& a, int64_t r, const T* row, Marks marks, TopLds s,
                                              Teacher* out) {
     const int lane = threadIdx.x & 63, top = a.top;
-    float most = -INFINITY;
+    float most = -INFINITY, z_top = -INFINITY;
     for (int k = lane; k < top; k += 64) {
         s.z[k] = s.at[k] >= 0 ? (float)row[s.at[k]] : -INFINITY;
+        z_top = fmaxf(z_top, s.z[k]);
         if (s.at[k] >= 0) most = fmaxf(most, s.q[k]);
     }
     wave_fence();
-    most = anchor(wave_max_f(most));
-    // with e_k = exp(s (a_k - most)):  sums of e, e (a - most), e z, and of nothing else, so that one reduction does
+    most = lane_bcast_f(anchor(wave_max_f(most)), 0);
+    z_top = lane_bcast_f(anchor(wave_max_f(z_top)), 0);      // (in a scalar register)
+    // with e_k = exp(s (a_k - most)):  sums of e, e (a - most), e (z - z_top), and of nothing else, so that one reduction does.
+    // (Differences to the largest: of a row at the type's lowest value sums of the logits themselves would leave no digit.)
     double sums[8] = {};
     for (int k = lane; k < top; k += 64) {
         if (s.at[k] < 0) continue;
@@ -603,7 +606,9 @@ __device__ __forceinline__ void read_teacher(const LogitsArgs& l, const DistillA
         sums[0] += (double)e;
         if (e != 0.0f) {
             sums[1] = fma((double)e, (double)d, sums[1]);
-            sums[2] = fma((double)e, (double)s.z[k], sums[2]);
+            float from = z_top;
+            asm volatile("" : "+s"(from));            // (widened here, not kept in two more registers)
+            sums[2] = fma((double)e, (double)s.z[k] - (double)from, sums[2]);
         }
     }
     wave_fence();
@@ -650,7 +655,7 @@ __device__ __forceinline__ void read_teacher(const LogitsArgs& l, const DistillA
     }
     const Stat st = REST ? wave_stat<false>(run.a, l.c) : run.a;
     const int any_lost = __any(marks.lost);
-    if (lane == 0) *out = {f * (l.s * (ed - ez) - shift * total), f * total, st, entries, any_lost};
+    if (lane == 0) *out = {f * (l.s * (ed - ez) - shift * total), f * total, z_top, st, entries, any_lost};
 }
 
 // What a row of the distillation's gradient is made of: away from the teacher's dz_j = A 2^((z_j - st.m) c), at one of them
@@ -689,7 +694,7 @@ __device__ __forceinline__ float distill_value(const LogitsArgs& l, Stat st, con
     if (t.lost) return NAN;
     if (all.s == 0.0f) return t.entries ? INFINITY : 0.0f;
     const RowLog g = row_log(all, l.s);
-    double loss = t.entries ? t.cross + t.sum * g.lse : 0.0;
+    double loss = t.entries ? t.cross + t.sum * (((double)all.m - (double)t.z_top) * l.s + g.log_s) : 0.0;
     if (REST) {
         const double rest = teacher_rest(l, t);
         const double log_t = st.s == 0.0f ? -INFINITY : ((double)st.m - (double)all.m) * l.s + log_d((double)st.s) - g.log_s;
@@ -729,13 +734,16 @@ __global__ __launch_bounds__(BLOCK, BLOCK == 512 ? 4 : 1) void k_distill(LogitsA
     if (threadIdx.x < 64) read_teacher<T, REST>(l, a, r, row, marks, s, &teacher);
     const Stat st = block_stat<false, BLOCK / 64>(z.template stat<false, REST>(span, l.c, (const unsigned char*)s.seen), l.c, lds);
     const DistillRow d = distill_row<REST>(l, a, w, st, teacher);
-    if (threadIdx.x == 0) a.row_loss[r] = distill_value<REST>(l, st, teacher);
+    // (the loss after the gradient, when the row's registers are free, or before it where there are plenty: 16384 x 4000 75 / 76 us)
+    constexpr bool early = CH <= 4;
+    if (early && threadIdx.x == 0) a.row_loss[r] = distill_value<REST>(l, st, teacher);
+    if (l.dz && !d.empty) z.template write<false>(span, out, st.m, l.c, d.A, 0.0f, -1, 0.0f, 0.0f);
+    if (!early && threadIdx.x == 0) a.row_loss[r] = distill_value<REST>(l, st, teacher);
     if (!l.dz) return;
     if (d.empty) {
         Row<T, BLOCK, CH>::clear(out, l.vocab);
         return;
     }
-    z.template write<false>(span, out, st.m, l.c, d.A, 0.0f, -1, 0.0f, 0.0f);
     __syncthreads();                          // (the entries' own values come after the row's)
     for (int k = threadIdx.x; k < a.top; k += BLOCK)
         if (s.at[k] >= 0) out[s.at[k]] = (T)d.at_entry(s.z[k], s.q[k], l.c);

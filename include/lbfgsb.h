@@ -463,7 +463,8 @@ typedef struct {
  *   else:      q_k = exp(s a_k - lse), and the rest of the vocabulary is one more outcome, of mass r = max(0, 1 - sum q) for the
  *              teacher and t (the student's p outside the entries):  loss_n = sum_k q_k (log q_k - log p_k) + r (log r - log t),
  *              dz_j = s (p_j - q_j) for the entries, s p_j (1 - r/t) elsewhere.
- * (q_j: zero off the entries; an index that comes twice adds up.)  A row without entries gives zeros.  vocab <= 2^19.
+ * (q_j: zero off the entries; an index that comes twice adds up.)  A row without entries gives zeros, whatever its lse and its
+ * logits are.  vocab <= 2^19.
  * weight: rows entries or NULL.  loss: one float; row_loss: rows entries (loss_n, unweighted). */
 int lbfgsb_distill_loss(const lbfgsb_logits* logits_host, const lbfgsb_teacher* teacher_host, const float* weight, double scale,
                         float* loss, float* row_loss, void* workspace, size_t workspace_bytes, void* hip_stream);

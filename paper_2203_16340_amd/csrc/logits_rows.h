@@ -633,12 +633,14 @@ __device__ __forceinline__ void read_teacher(const LogitsArgs& l, const DistillA
     const double total = lane_bcast(mine, 0), ed = lane_bcast(mine, 1), ez = lane_bcast(mine, 2);
     // q_k = f e_k and log q_k = s (a_k - most) - shift
     double f, shift;
-    if (a.lse) {
+    if (total == 0.0) {               // no entry, whatever the log-sum-exp is
+        f = shift = 0.0;
+    } else if (a.lse) {
         shift = (double)a.lse[r] - (double)most * l.s;
         f = (double)expf((float)-shift);
     } else {
         shift = total > 0.0 ? log_d(total) : total;
-        f = total > 0.0 ? 1.0 / total : total;
+        f = 1.0 / total;
     }
     Running run;
     int entries = 0;
@@ -676,7 +678,7 @@ template <bool REST>
 __device__ __forceinline__ DistillRow distill_row(const LogitsArgs& l, const DistillArgs& a, float w, Stat st, const Teacher& t) {
     DistillRow d;
     d.all = REST ? merged(st, t.top, l.c) : st;
-    d.empty = d.all.s == 0.0f && !t.lost;
+    d.empty = (d.all.s == 0.0f || !t.entries) && !t.lost;
     // (a teacher that is no number leaves its mark on every entry)
     d.W = t.lost || t.cross != t.cross ? NAN : (float)((double)w * a.scale * l.s);
     if (REST) {
@@ -684,7 +686,7 @@ __device__ __forceinline__ DistillRow distill_row(const LogitsArgs& l, const Dis
         const double share = (double)(st.s * exp2_hw(below(st.m, d.all.m, l.c)) / d.all.s);
         d.A = st.s == 0.0f ? 0.0f : d.W * (float)((share - teacher_rest(l, t)) / (double)st.s);
     } else {
-        d.A = t.entries ? d.W / st.s : d.W * 0.0f;
+        d.A = d.W / st.s;
     }
     return d;
 }
@@ -692,9 +694,10 @@ template <bool REST>
 __device__ __forceinline__ float distill_value(const LogitsArgs& l, Stat st, const Teacher& t) {
     const Stat all = REST ? merged(st, t.top, l.c) : st;
     if (t.lost) return NAN;
-    if (all.s == 0.0f) return t.entries ? INFINITY : 0.0f;
+    if (!t.entries) return 0.0f;
+    if (all.s == 0.0f) return INFINITY;
     const RowLog g = row_log(all, l.s);
-    double loss = t.entries ? t.cross + t.sum * (((double)all.m - (double)t.z_top) * l.s + g.log_s) : 0.0;
+    double loss = t.cross + t.sum * (((double)all.m - (double)t.z_top) * l.s + g.log_s);
     if (REST) {
         const double rest = teacher_rest(l, t);
         const double log_t = st.s == 0.0f ? -INFINITY : ((double)st.m - (double)all.m) * l.s + log_d((double)st.s) - g.log_s;

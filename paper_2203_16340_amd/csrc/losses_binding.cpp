@@ -45,6 +45,7 @@ struct Call {
     Maybe grad;
     at::Device dev;
     int64_t rows;
+    bool given = false;      // the gradient is the caller's tensor
     // want: a new gradient; out: one to write to
     Call(const Tensor& z, double temperature, bool want, const Maybe& out) : dev(z.device()), rows(0) {
         lg.dtype = logit_type(z, "logits");
@@ -57,11 +58,18 @@ struct Call {
             if (logit_type(*out, "grad") != lg.dtype || out->sizes() != z.sizes() || out->device() != dev)
                 throw py::type_error("grad must have the type, shape and device of the logits");
             grad = out;
+            given = true;
         } else if (want) {
             grad = at::empty(z.sizes(), z.options());
         }
         lg.grad = grad ? grad->data_ptr() : nullptr;
         lg.ld_grad = grad ? row_stride(*grad) : 0;
+    }
+    // After a call that went well: torch learns that the caller's tensor has been written to, so that a way back which kept it is
+    // refused, as after any operation in place.  (Tensors of inference mode have no count and nobody's way back keeps them.)
+    int done(int rc) const {
+        if (rc == LBFGSB_OK && given && !grad->is_inference()) grad->unsafeGetTensorImpl()->bump_version();
+        return rc;
     }
     Tensor rows_of_floats() const { return at::empty({rows}, at::TensorOptions(dev).dtype(at::kFloat)); }
     Tensor number() const { return at::empty({}, at::TensorOptions(dev).dtype(at::kFloat)); }
@@ -112,7 +120,7 @@ auto token_logprob_grad(const Tensor& z, const Tensor& labels, const Tensor& lse
     } else {
         rc = lbfgsb_token_logprob_grad(&c.lg, y, l, l_rest, h, d, dh, (void*)stream);
     }
-    return std::make_tuple(rc, *c.grad);
+    return std::make_tuple(c.done(rc), *c.grad);
 }
 
 auto distill_loss(const Tensor& z, const Tensor& index, const Tensor& logit, const Maybe& lse, const Maybe& weight, double temperature,
@@ -135,7 +143,7 @@ auto distill_loss(const Tensor& z, const Tensor& index, const Tensor& logit, con
     const float* w = maybe(weight, "weight", c.rows, c.dev);
     Tensor loss = c.number(), row = c.rows_of_floats(), ws = c.workspace(true);
     const int rc = lbfgsb_distill_loss(&c.lg, &t, w, scale, (float*)loss.data_ptr(), (float*)row.data_ptr(), address(ws), bytes(ws), (void*)stream);
-    return std::make_tuple(rc, loss, row, c.grad);
+    return std::make_tuple(c.done(rc), loss, row, c.grad);
 }
 
 auto policy_loss(const Tensor& z, const Tensor& labels, const Tensor& old_logp, const Tensor& advantage, const Maybe& ref_logp,
@@ -151,7 +159,7 @@ auto policy_loss(const Tensor& z, const Tensor& labels, const Tensor& old_logp, 
     if (entropy) h = c.rows_of_floats();
     const int rc = lbfgsb_policy_loss(&c.lg, &p, &o, scale, (float*)loss.data_ptr(), (float*)row.data_ptr(), (float*)logp.data_ptr(),
                                       h ? (float*)h->data_ptr() : nullptr, address(ws), bytes(ws), (void*)stream);
-    return std::make_tuple(rc, loss, row, logp, h, c.grad);
+    return std::make_tuple(c.done(rc), loss, row, logp, h, c.grad);
 }
 
 auto preference_loss(const Tensor& logp, const Maybe& ref_logp, const Tensor& offsets, const Maybe& mask, const Maybe& weight, double beta, int kind,

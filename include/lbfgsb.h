@@ -500,8 +500,8 @@ typedef struct {
 } lbfgsb_preference_options;
 /* The loss on pairs of answers, from the log-probabilities of their tokens (lbfgsb_token_logprob; the gradient goes back through
  * lbfgsb_token_logprob_grad).  Answer i has the tokens offsets[i] <= t < offsets[i+1]; answers 0 .. pairs-1 are the chosen
- * ones, pairs .. 2 pairs-1 the rejected ones of the same pairs.  offsets: 2 pairs + 1 ascending entries (taken into
- * 0 .. tokens where they are not).  mask (or NULL): tokens entries, 0 = does not count.
+ * ones, pairs .. 2 pairs-1 the rejected ones of the same pairs.  offsets: 2 pairs + 1 ascending entries, taken into 0 .. tokens.  Where they
+ * then descend an answer that ends before it begins is empty, others may share tokens, and the whole gradient is NaN.  mask (or NULL): tokens entries, 0 = does not count.
  *     R_i = sum (or mean) over the answer's tokens that count of logp - ref_logp  (ref_logp NULL: of logp; no token: 0),
  *     delta = beta (R_chosen - R_rejected) - margin,
  *     SIGMOID  -(1 - e) log sigmoid(delta) - e log sigmoid(-delta),  HINGE  max(0, 1 - delta),  IPO  ((delta - 1/2)/beta)^2.

@@ -97,8 +97,16 @@ template <typename T>
 hipError_t policy_rows(const LogitsArgs& l, const PolicyArgs& a, float* loss, SplitRow* ws, hipStream_t st);
 template <typename T>
 hipError_t distill_rows(const LogitsArgs& l, const DistillArgs& a, float* loss, SplitRow* ws, hipStream_t st);
+// Offsets of answers that are to ascend, 0 .. tokens, and the gradient that is no number where they do not.
+struct Ascending {
+    const int64_t* offsets;
+    int64_t answers, tokens;
+    float* grad;            // null: nothing to do
+};
+__host__ __device__ inline int64_t into(int64_t v, int64_t tokens) { return v < 0 ? 0 : (v > tokens ? tokens : v); }
 // loss = scale * sum_n weight_n row_loss_n
-hipError_t launch_weighted_total(const float* row_loss, const float* weight, int64_t n, double scale, float* loss, hipStream_t st);
+hipError_t launch_weighted_total(const float* row_loss, const float* weight, int64_t n, double scale, float* loss, hipStream_t st,
+                                 const Ascending& of = {});
 // Pieces that each of a call's rows is split into; 1: none is.
 int row_splits(int64_t rows, int64_t vocab, int size, bool grad);   // size: bytes of a logit; grad: a gradient is wanted
 

@@ -9,7 +9,7 @@ namespace {
 constexpr int kTotalBlock = 1024;
 
 __global__ __launch_bounds__(kTotalBlock) void k_weighted_total(const float* row_loss, const float* weight, int64_t n, double scale,
-                                                                float* loss) {
+                                                                float* loss, Ascending of) {
     __shared__ double lds[kTotalBlock / 64];
     double sum = 0.0;
     for (int64_t i0 = threadIdx.x; i0 < n; i0 += 4 * kTotalBlock) {
@@ -24,9 +24,15 @@ __global__ __launch_bounds__(kTotalBlock) void k_weighted_total(const float* row
         for (int k = 0; k < 4; ++k)
             if (w[k] != 0.0f) sum += (double)w[k] * (double)v[k];   // (what does not count may be infinite)
     }
+    int descend = 0;
+    if (of.grad)
+        for (int64_t i = threadIdx.x; i < of.answers; i += kTotalBlock)
+            descend |= into(of.offsets[i + 1], of.tokens) < into(of.offsets[i], of.tokens);
     sum = wave_sum(sum);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = sum;
-    __syncthreads();
+    // (answers that share tokens: which of them wrote a token's gradient last would be chance)
+    if (__syncthreads_or(descend))
+        for (int64_t t = threadIdx.x; t < of.tokens; t += kTotalBlock) of.grad[t] = NAN;
     if (threadIdx.x == 0) {
         double total = 0.0;
         for (int w = 0; w < kTotalBlock / 64; ++w) total += lds[w];
@@ -53,8 +59,9 @@ int row_splits(int64_t rows, int64_t vocab, int size, bool grad) {
     return (int)(splits < kSplits ? splits : kSplits);
 }
 
-hipError_t launch_weighted_total(const float* row_loss, const float* weight, int64_t n, double scale, float* loss, hipStream_t st) {
-    hipLaunchKernelGGL(k_weighted_total, dim3(1), dim3(kTotalBlock), 0, st, row_loss, weight, n, scale, loss);
+hipError_t launch_weighted_total(const float* row_loss, const float* weight, int64_t n, double scale, float* loss, hipStream_t st,
+                                 const Ascending& of) {
+    hipLaunchKernelGGL(k_weighted_total, dim3(1), dim3(kTotalBlock), 0, st, row_loss, weight, n, scale, loss, of);
     return hipGetLastError();
 }
 

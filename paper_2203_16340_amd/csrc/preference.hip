@@ -13,11 +13,11 @@ constexpr int kPairBlock = 512;
 struct Span {
     int64_t begin, end;
 };
-// the tokens of answer i; offsets outside 0 .. tokens, or that do not ascend, are taken to the nearest that do
+// the tokens of answer i; offsets outside 0 .. tokens are taken to the nearest inside, and an answer whose end comes before its beginning
+// is empty.  (Where offsets descend, answers may share tokens; the closing launch looks after their gradient.)
 __device__ __forceinline__ Span answer(const PreferenceArgs& a, int64_t i) {
-    const int64_t b = a.offsets[i], e = a.offsets[i + 1];
-    const int64_t begin = b < 0 ? 0 : (b > a.tokens ? a.tokens : b);
-    return {begin, e < begin ? begin : (e > a.tokens ? a.tokens : e)};
+    const int64_t begin = into(a.offsets[i], a.tokens), end = into(a.offsets[i + 1], a.tokens);
+    return {begin, end < begin ? begin : end};
 }
 
 struct LogRatio {
@@ -103,7 +103,7 @@ hipError_t launch_preference(const PreferenceArgs& a, float* loss, hipStream_t s
         hipLaunchKernelGGL(k_preference, dim3((unsigned)(a.pairs < 1 ? 1 : (a.pairs < 65536 ? a.pairs : 65536))), dim3(kPairBlock), 0, st, a);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
-    return launch_weighted_total(a.pair_loss, a.weight, a.pairs, a.scale, loss, st);
+    return launch_weighted_total(a.pair_loss, a.weight, a.pairs, a.scale, loss, st, {a.offsets, 2 * a.pairs, a.tokens, a.grad});
 }
 
 }  // namespace lb

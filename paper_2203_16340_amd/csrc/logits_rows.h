@@ -32,8 +32,8 @@ __device__ __forceinline__ typename Chunk<T>::wide widened(typename Chunk<T>::ve
 
 // 2^a (A + B a) at a = (z - ref) c
 template <bool ENT>
-__device__ __forceinline__ float slope_at(float z, float ref, float c, float A, float B) {
-    const float d = (z - ref) * c, x = exp2_hw(d);
+__device__ __forceinline__ float slope_at(float z, float ref, Factor c, float A, float B) {
+    const float d = (z - ref) * c.c, x = exp2_hw(d);
     return ENT ? x * fmaf(B, fmaxf(d, -1000.0f), A) : x * A;
 }
 
@@ -163,7 +163,7 @@ struct Row {
     // Statistics of an open span; ends with the last CH chunks a thread in the slots.  skip (where SKIP): a bit for each entry that stays
     // out (Cut::shift).
     template <bool ENT, bool SKIP>
-    __device__ __forceinline__ Stat stat(const Span& sp, float c, const unsigned char* skip) {
+    __device__ __forceinline__ Stat stat(const Span& sp, Factor c, const unsigned char* skip) {
         Running a;
         auto skipped = [&](int i) -> unsigned {
             const int at = sp.cut.first(i) + sp.cut.shift();
@@ -220,7 +220,7 @@ struct Row {
 
     // dz_j = 2^((z_j - m) c) (A + B (z_j - m) c), and `mark` more at j = y (none: -1), where the logit is zy.
     template <bool ENT>
-    __device__ __forceinline__ void write(const Span& sp, T* out, float m, float c, float A, float B, int y, float zy, float mark) {
+    __device__ __forceinline__ void write(const Span& sp, T* out, float m, Factor c, float A, float B, int y, float zy, float mark) {
         static_assert(CH > 0);
         const float ref = anchor(m);
         char* to = (char*)(out + sp.cut.head);
@@ -285,7 +285,7 @@ __device__ __forceinline__ float label_logit(const T* row, int64_t y, int vocab)
 }
 
 __device__ __forceinline__ void put_token(const LogitsArgs& l, const TokenArgs& a, int64_t r, Stat st, float zy) {
-    const RowLog g = row_log(st, l.s);
+    const RowLog g = row_log(st, l);
     const float lse = (float)g.lse;
     a.logp[r] = logp_of(st, g, l.s, zy);
     a.lse[r] = lse;
@@ -446,7 +446,7 @@ struct PolicyRow {
 // dz_j = W (slope (1[j = y] - p_j) + c_H p_j (log p_j + H)),  log p_j = ln 2 a_j - ln S
 template <bool ENT>
 __device__ __forceinline__ PolicyRow policy_row(const LogitsArgs& l, const PolicyArgs& a, int64_t r, float w, Stat st, float zy) {
-    const RowLog g = row_log(st, l.s);
+    const RowLog g = row_log(st, l);
     PolicyRow p;
     p.empty = st.s == 0.0f;
     p.logp = logp_of(st, g, l.s, zy);
@@ -601,7 +601,7 @@ __device__ __forceinline__ void read_teacher(const LogitsArgs& l, const DistillA
     double sums[8] = {};
     for (int k = lane; k < top; k += 64) {
         if (s.at[k] < 0) continue;
-        const float d = s.q[k] - most, e = exp2_hw(d * l.c);
+        const float d = s.q[k] - most, e = exp2_hw(d * l.c.c);
         s.q[k] = e;
         sums[0] += (double)e;
         if (e != 0.0f) {
@@ -666,8 +666,8 @@ struct DistillRow {
     Stat all;
     float A, W;
     bool empty;
-    __device__ __forceinline__ float at_entry(float z, float q, float c) const {
-        return W * (exp2_hw((z - anchor(all.m)) * c) / all.s - q);
+    __device__ __forceinline__ float at_entry(float z, float q, Factor c) const {
+        return W * (exp2_hw((z - anchor(all.m)) * c.c) / all.s - q);
     }
 };
 // the teacher's share of the rest
@@ -696,7 +696,7 @@ __device__ __forceinline__ float distill_value(const LogitsArgs& l, Stat st, con
     if (t.lost) return NAN;
     if (!t.entries) return 0.0f;
     if (all.s == 0.0f) return INFINITY;
-    const RowLog g = row_log(all, l.s);
+    const RowLog g = row_log(all, l);
     double loss = t.cross + t.sum * (((double)all.m - (double)t.z_top) * l.s + g.log_s);
     if (REST) {
         const double rest = teacher_rest(l, t);
@@ -761,12 +761,12 @@ constexpr int kSplitBlock = 512, kSplitHold = 4;      // threads; chunks a threa
 
 // the statistics of a row, by every wave of the second launch
 template <bool ENT>
-__device__ __forceinline__ Stat joined(const SplitRow& s, int splits, float c) {
+__device__ __forceinline__ Stat joined(const SplitRow& s, int splits, Factor c) {
     const int lane = threadIdx.x & 63;
     return wave_stat<ENT>(lane < splits ? s.part[lane] : Stat{-INFINITY, 0.0f, 0.0f}, c);
 }
 // the same by one lane
-__device__ __forceinline__ Stat joined_alone(const SplitRow& s, int splits, float c) {
+__device__ __forceinline__ Stat joined_alone(const SplitRow& s, int splits, Factor c) {
     Stat a = s.part[0];
     for (int i = 1; i < splits; ++i) a = merged(a, s.part[i], c);
     return a;

@@ -1,5 +1,7 @@
 // C-ABI layer of the losses on logits: argument checks; everything else is enqueued.
+#include <algorithm>
 #include <cmath>
+#include <limits>
 
 #include "logits.h"
 
@@ -59,9 +61,16 @@ int check_workspace(const lbfgsb_logits* l, bool grad, const void* ws, size_t by
     return LBFGSB_OK;
 }
 
+Factor factor_of(double s) {
+    const double c = s * 1.44269504088896340736;
+    // (never 0, which times -infinity is no number)
+    const float high = std::max((float)c, std::numeric_limits<float>::denorm_min()), low = (float)(c - (double)high);
+    return {high, low, s / (double)high};
+}
+
 LogitsArgs args_of(const lbfgsb_logits* l, bool grad) {
     const double s = 1.0 / l->temperature;
-    return {l->z, grad ? l->grad : nullptr, l->rows, l->ld, l->ld_grad, (int)l->vocab, s, (float)(s * 1.44269504088896340736)};
+    return {l->z, grad ? l->grad : nullptr, l->rows, l->ld, l->ld_grad, (int)l->vocab, s, factor_of(s)};
 }
 
 int check_scale(double scale, const float* loss) {

@@ -417,7 +417,7 @@ typedef struct {
     int64_t rows, vocab;   /* rows <= 2^31-1, 1 <= vocab <= 2^30 */
     int64_t ld;            /* elements from one row of z to the next, >= vocab; rows may start on any element */
     const void* z;         /* rows x vocab */
-    double temperature;    /* > 0 */
+    double temperature;    /* > 0, and log2(e) / temperature finite in 32 bits */
     void* grad;            /* gradient with respect to z, rows x vocab; NULL: not wanted.  It may be z itself (with
                               ld_grad == ld): the gradient then takes the logits' place.  It must not overlap z otherwise */
     int64_t ld_grad;

@@ -33,8 +33,9 @@ int check_shape(const lbfgsb_logits* l) {
 int check_logits(const lbfgsb_logits* l, int grad) {
     if (int rc = check_shape(l)) return rc;
     if (l->ld < l->vocab || l->ld > kMaxLd) return fail(LBFGSB_E_INVALID_ARG, "ld must be in vocab..2^31 (got %lld)", (long long)l->ld);
-    if (!(l->temperature > 0.0) || !std::isfinite(l->temperature) || !std::isfinite(1.0 / l->temperature))
-        return fail(LBFGSB_E_INVALID_ARG, "temperature must be positive (got %g)", l->temperature);
+    // (the exponents' factor is held in 32 bits: infinite, it makes a number of no row)
+    if (!(l->temperature > 0.0) || !std::isfinite(l->temperature) || !std::isfinite((float)(1.44269504088896340736 / l->temperature)))
+        return fail(LBFGSB_E_INVALID_ARG, "temperature must be positive, finite and above 4.24e-39 (got %g)", l->temperature);
     if (l->rows == 0) return LBFGSB_OK;
     const size_t b = size_of(l->dtype);
     if (!l->z || misaligned(l->z, b)) return fail(LBFGSB_E_INVALID_ARG, "z is NULL or not aligned to its elements");

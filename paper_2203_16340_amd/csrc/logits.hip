@@ -24,15 +24,17 @@ __global__ __launch_bounds__(kTotalBlock) void k_weighted_total(const float* row
         for (int k = 0; k < 4; ++k)
             if (w[k] != 0.0f) sum += (double)w[k] * (double)v[k];   // (what does not count may be infinite)
     }
-    int descend = 0;
-    if (of.grad)
-        for (int64_t i = threadIdx.x; i < of.answers; i += kTotalBlock)
-            descend |= into(of.offsets[i + 1], of.tokens) < into(of.offsets[i], of.tokens);
     sum = wave_sum(sum);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = sum;
-    // (answers that share tokens: which of them wrote a token's gradient last would be chance)
-    if (__syncthreads_or(descend))
-        for (int64_t t = threadIdx.x; t < of.tokens; t += kTotalBlock) of.grad[t] = NAN;
+    __syncthreads();
+    if (of.grad) {
+        int descend = 0;
+        for (int64_t i = threadIdx.x; i < of.answers; i += kTotalBlock)
+            descend |= into(of.offsets[i + 1], of.tokens) < into(of.offsets[i], of.tokens);
+        // (answers that share tokens: which of them wrote a token's gradient last would be chance)
+        if (__syncthreads_or(descend))
+            for (int64_t t = threadIdx.x; t < of.tokens; t += kTotalBlock) of.grad[t] = NAN;
+    }
     if (threadIdx.x == 0) {
         double total = 0.0;
         for (int w = 0; w < kTotalBlock / 64; ++w) total += lds[w];

@@ -44,7 +44,6 @@ struct SplitRow {
 // every entry cost log-probabilities of 8192 x 131072 bf16 with the entropy 322 / 340 us, without 305 / 310.)
 struct Factor {
     float c, low;           // the nearest, and what is left
-    double unit;            // of the entries' exponents: s / c
     __device__ __forceinline__ float operator()(float d) const { return fmaf(d, c, d * low); }
 };
 struct LogitsArgs {
@@ -134,8 +133,7 @@ __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2
 // no number, ends here as well)
 __device__ __forceinline__ float below(float m, float top, Factor c) { return fmaxf(c(m - top), -1000.0f); }
 __device__ __forceinline__ Stat rescaled(Stat a, float top, Factor c) {
-    // (t goes with the exponents of the entries, which have c alone)
-    const float d = fmaxf((a.m - top) * c.c, -1000.0f), f = exp2_hw(below(a.m, top, c));
+    const float d = below(a.m, top, c), f = exp2_hw(d);
     return {top, a.s * f, (a.t + d * a.s) * f};
 }
 __device__ __forceinline__ Stat merged(Stat a, Stat b, Factor c) {
@@ -205,7 +203,8 @@ struct Running {
 #pragma unroll
         for (int i = 1; i < N; ++i) top = fmaxf(top, z[i]);
         if (top > a.m) {
-            a = rescaled(a, top, c);
+            const float d = fmaxf((a.m - top) * c.c, -1000.0f), f = exp2_hw(d);      // (c alone, as at its entries)
+            a = {top, a.s * f, (a.t + d * a.s) * f};
             ref = top;
         }
         float s[N], t = 0.0f;
@@ -228,10 +227,10 @@ struct Running {
 struct RowLog {
     double log_s, lse, entropy;
 };
-__device__ __forceinline__ RowLog row_log(Stat a, const LogitsArgs& l) {
+__device__ __forceinline__ RowLog row_log(Stat a, double s) {
     if (a.s == 0.0f) return {-INFINITY, -INFINITY, 0.0};
     const double ls = log_d((double)a.s);
-    return {ls, (double)a.m * l.s + ls, ls - l.c.unit * ((double)a.t / (double)a.s)};
+    return {ls, (double)a.m * s + ls, ls - 0.69314718055994530942 * ((double)a.t / (double)a.s)};
 }
 
 }  // namespace lb

@@ -285,7 +285,7 @@ __device__ __forceinline__ float label_logit(const T* row, int64_t y, int vocab)
 }
 
 __device__ __forceinline__ void put_token(const LogitsArgs& l, const TokenArgs& a, int64_t r, Stat st, float zy) {
-    const RowLog g = row_log(st, l);
+    const RowLog g = row_log(st, l.s);
     const float lse = (float)g.lse;
     a.logp[r] = logp_of(st, g, l.s, zy);
     a.lse[r] = lse;
@@ -446,7 +446,7 @@ struct PolicyRow {
 // dz_j = W (slope (1[j = y] - p_j) + c_H p_j (log p_j + H)),  log p_j = ln 2 a_j - ln S
 template <bool ENT>
 __device__ __forceinline__ PolicyRow policy_row(const LogitsArgs& l, const PolicyArgs& a, int64_t r, float w, Stat st, float zy) {
-    const RowLog g = row_log(st, l);
+    const RowLog g = row_log(st, l.s);
     PolicyRow p;
     p.empty = st.s == 0.0f;
     p.logp = logp_of(st, g, l.s, zy);
@@ -696,7 +696,7 @@ __device__ __forceinline__ float distill_value(const LogitsArgs& l, Stat st, con
     if (t.lost) return NAN;
     if (!t.entries) return 0.0f;
     if (all.s == 0.0f) return INFINITY;
-    const RowLog g = row_log(all, l);
+    const RowLog g = row_log(all, l.s);
     double loss = t.cross + t.sum * (((double)all.m - (double)t.z_top) * l.s + g.log_s);
     if (REST) {
         const double rest = teacher_rest(l, t);

@@ -66,7 +66,7 @@ Factor factor_of(double s) {
     const double c = s * 1.44269504088896340736;
     // (never 0, which times -infinity is no number)
     const float high = std::max((float)c, std::numeric_limits<float>::denorm_min()), low = (float)(c - (double)high);
-    return {high, low, s / (double)high};
+    return {high, low};
 }
 
 LogitsArgs args_of(const lbfgsb_logits* l, bool grad) {

@@ -113,8 +113,8 @@ struct Row {
     float alone;                         // the single element of this thread, if any
     vec* held;                           // HELD: room in LDS for the chunks before `again` (held_bytes)
 
-    // The thread's index, to the compiler a new value each time: else it keeps every slot's place, several registers a slot, from one row
-    // to the next.
+    // The thread's index, to the compiler a new value each time: else it keeps what it worked out for one loop over the slots until the
+    // next, one or two registers, which are a wave in the distillation with 13 chunks (80 / 81).
     static __device__ __forceinline__ int thread() {
         int t = (int)threadIdx.x;
         asm volatile("" : "+v"(t));
@@ -697,6 +697,7 @@ __device__ __forceinline__ float distill_value(const LogitsArgs& l, Stat st, con
     if (!t.entries) return 0.0f;
     if (all.s == 0.0f) return INFINITY;
     const RowLog g = row_log(all, l.s);
+    asm volatile("" ::: "memory");            // (the rest of t is read now, not kept through the logarithm)
     double loss = t.cross + t.sum * (((double)all.m - (double)t.z_top) * l.s + g.log_s);
     if (REST) {
         const double rest = teacher_rest(l, t);
@@ -737,16 +738,13 @@ __global__ __launch_bounds__(BLOCK, BLOCK == 512 ? 4 : 1) void k_distill(LogitsA
     if (threadIdx.x < 64) read_teacher<T, REST>(l, a, r, row, marks, s, &teacher);
     const Stat st = block_stat<false, BLOCK / 64>(z.template stat<false, REST>(span, l.c, (const unsigned char*)s.seen), l.c, lds);
     const DistillRow d = distill_row<REST>(l, a, w, st, teacher);
-    // (the loss after the gradient, when the row's registers are free, or before it where there are plenty: 16384 x 4000 75 / 76 us)
-    constexpr bool early = CH <= 4;
-    if (early && threadIdx.x == 0) a.row_loss[r] = distill_value<REST>(l, st, teacher);
-    if (l.dz && !d.empty) z.template write<false>(span, out, st.m, l.c, d.A, 0.0f, -1, 0.0f, 0.0f);
-    if (!early && threadIdx.x == 0) a.row_loss[r] = distill_value<REST>(l, st, teacher);
+    if (threadIdx.x == 0) a.row_loss[r] = distill_value<REST>(l, st, teacher);
     if (!l.dz) return;
     if (d.empty) {
         Row<T, BLOCK, CH>::clear(out, l.vocab);
         return;
     }
+    z.template write<false>(span, out, st.m, l.c, d.A, 0.0f, -1, 0.0f, 0.0f);
     __syncthreads();                          // (the entries' own values come after the row's)
     for (int k = threadIdx.x; k < a.top; k += BLOCK)
         if (s.at[k] >= 0) out[s.at[k]] = (T)d.at_entry(s.z[k], s.q[k], l.c);

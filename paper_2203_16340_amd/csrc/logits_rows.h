@@ -708,8 +708,8 @@ __device__ __forceinline__ float distill_value(const LogitsArgs& l, Stat st, con
 }
 
 // As the policy loss, and the first wave looks after the teacher meanwhile: its entries, then the student's logits there, one more trip
-// to memory, and two dozen double sums.  8192 x 65536 bf16, 64 entries, 390 us, 5.5 TB/s; with the rest's outcome, which has to know
-// the entries before the statistics, 405.  (With the entries loaded ahead of the row's chunks
+// to memory, and two dozen double sums.  8192 x 65536 bf16, 64 entries, 400 us, 5.4 TB/s; with the rest's outcome, which has to know
+// the entries before the statistics, 415.  (With the entries loaded ahead of the row's chunks
 // it is no faster: 842 / 862 us at 8192 x 131072.)
 template <typename T, bool REST, int BLOCK, int CH, bool LONG, bool HELD>
 __global__ __launch_bounds__(BLOCK, BLOCK == 512 ? 4 : 1) void k_distill(LogitsArgs l, DistillArgs a, int64_t first) {
@@ -955,14 +955,16 @@ constexpr size_t kPairLds = 79 << 10;
 // small workgroups on a compute unit fill each other's pauses.  Policy loss, 16384 rows of bf16, us: x 1000 64 threads of 4 chunks 27, 128 of 4
 // 34, 256 of 4 47; x 4000 128 of 4 61, 256 of 4 64, 512 of 4 91; x 8000 256 of 4 99, 512 of 4 121; x 16000 256 of 8 193, 512 of 4 188 (the
 // distillation 209 and 242); x 32000 512 of 8 372, 256 of 16 no less.  Of 512 threads the count of chunks follows the row: 4099 x 50021 f16 13 chunks
-// 135, 16 chunks 143.  Longer rows than 1024 threads hold: 1001 x 100003 f32 read twice 245, kept as far as it goes 184.
+// 135, 16 chunks 143.  Longer rows than 1024 threads hold: 1001 x 100003 f32 read twice 245, kept as far as it goes 184 (both from
+// before loads went past the caches and chunks began on lines; 148 since).
 // Rows of more than 8192 chunks: one workgroup of 1024 threads on a compute unit, or with many rows of 16 bits two of 512, of which one loads
 // while the other writes, with 23 chunks a thread and what is left of the row in LDS (`lds` bytes of it are taken already).  1024 / 512
 // threads, us, bf16.  In registers alone, policy loss x 70000: 128 rows 13.8 / 14.4, 400 29.9 / 23.5, 8192 473 / 400; x 92000, 400 rows
 // 36.4 / 28.5, 8192 602 / 565.  With LDS, policy loss x 131072: 1000 rows 102 / 110, 1500 164 / 156, 4000 413 / 391, 8192 818 / 788; x 100000,
 // 1000 rows 76 / 81, 8192 657 / 593.  Distillation with the rest, which spills at 512, x 80000: 1000 rows 78 / 89, 4000 315 / 288, 8192 635 / 556,
 // and with LDS, x 100000, 8192 rows 747 / 777.  f32, policy loss, 4000 rows: x 50021 290 / 296, x 62003 352 / 363.
-// PAIR, HELD: the rows from which it is two of 512 threads, in registers alone and with LDS (0: never).
+// PAIR, HELD: the rows from which it is two of 512 threads, in registers alone and with LDS (0: never): from where on the pair won at every count
+// above.  (Between two of them how full the last round of 256 or 512 workgroups is decides, which these counts do not follow.)
 template <typename T, int PAIR, int HELD, typename F>
 void by_width(const LogitsArgs& l, size_t lds, F f) {
     const int chunks = most_chunks<T>(l);

@@ -64,6 +64,7 @@ struct TokenGradArgs {
     const float *top, *sum;                    // Stat::m and s; null: from what follows
     const float *lse, *lse_rest;               // lse_rest null: 0
     const float *entropy, *d_logp, *d_entropy; // d_entropy null: no gradient through the entropy
+    double temperature;
 };
 struct DistillArgs {
     const void *index, *logit;

@@ -337,10 +337,10 @@ __device__ __forceinline__ RowShare row_share(const LogitsArgs& l, const TokenGr
     // lse = ref s + off, ref the logit nearest to it.  Of lse_rest, which is known to 2^-25 of itself, more than 2^10 would leave off
     // uncertain by 2^-15 and more (lse is beyond 2^34 then, its own digits do not reach ln sum); then p_j is no number.
     const double lse = (double)a.lse[r], rest = a.lse_rest ? (double)a.lse_rest[r] : 0.0;
-    const float ref = fminf(fmaxf((float)(lse / l.s), -FLT_MAX), FLT_MAX);
+    const float ref = fminf(fmaxf((float)(lse * a.temperature), -FLT_MAX), FLT_MAX);
     if (lse == -INFINITY && rest == 0.0) return {ref, 0.0f};
     const double off = fma(-(double)ref, l.s, lse) + rest;
-    return {ref, fabs(rest) <= 1024.0 && fabs(off) <= 80.0 ? (float)exp(off) : NAN};
+    return {ref, fabs(rest) <= 1024.0 && fabs(off) <= 80.0 ? exp2_hw((float)off * 1.44269504088896340736f) : NAN};
 }
 
 // The way back needs no sums: the forward call's do.  (From differences to the maximum, not as z_j s - lse: at a temperature that is no power of
@@ -386,7 +386,8 @@ __global__ __launch_bounds__(kGradBlock) void k_token_grad(LogitsArgs l, TokenGr
         if (i0 + k * kGradBlock >= 0 && i0 + k * kGradBlock < cut.whole) slot[k] = __builtin_nontemporal_load((const any*)(from + (size_t)(unsigned)(i0 + k * kGradBlock) * 16));
     // p_j (-g - h (log p_j + H)),  log p_j = ln 2 a_j - ln sum
     const float over = s / row_of.sum;
-    const float A = over * (ENT ? fmaf(h, (float)log_d((double)row_of.sum) - entropy, -g) : -g), B = over * -h * 0.693147180559945309417f;
+    const float log_sum = 0.693147180559945309417f * __builtin_amdgcn_logf(row_of.sum);      // (to 1e-6: every thread works it out)
+    const float A = over * (ENT ? fmaf(h, log_sum - entropy, -g) : -g), B = over * -h * 0.693147180559945309417f;
     auto at = [&](float z) { return slope_at<ENT>(z, row_of.ref, l.c, A, B); };
     if (j >= 0) out[j] = (T)(at((float)row[j]) + (j == y ? g * s : 0.0f));
 #pragma unroll

@@ -113,7 +113,7 @@ int lbfgsb_token_logprob_grad(const lbfgsb_logits* logits_host, const int64_t* l
     if (!labels || !lse || !d_logp) return fail(LBFGSB_E_INVALID_ARG, "labels, lse and d_logp must not be NULL");
     if (d_entropy && !entropy) return fail(LBFGSB_E_INVALID_ARG, "d_entropy goes with the entropy");
     HIP_TRY(launch_token_logprob_grad(args_of(logits_host, true), logits_host->dtype,
-                                      {labels, nullptr, nullptr, lse, lse_rest, entropy, d_logp, d_entropy}, (hipStream_t)hip_stream));
+                                      {labels, nullptr, nullptr, lse, lse_rest, entropy, d_logp, d_entropy, logits_host->temperature}, (hipStream_t)hip_stream));
     return LBFGSB_OK;
 }
 
@@ -124,7 +124,7 @@ int lbfgsb_token_logprob_stats_grad(const lbfgsb_logits* logits_host, const int6
     if (!labels || !top || !sum || !d_logp) return fail(LBFGSB_E_INVALID_ARG, "labels, top, sum and d_logp must not be NULL");
     if (d_entropy && !entropy) return fail(LBFGSB_E_INVALID_ARG, "d_entropy goes with the entropy");
     HIP_TRY(launch_token_logprob_grad(args_of(logits_host, true), logits_host->dtype,
-                                      {labels, top, sum, nullptr, nullptr, entropy, d_logp, d_entropy}, (hipStream_t)hip_stream));
+                                      {labels, top, sum, nullptr, nullptr, entropy, d_logp, d_entropy, logits_host->temperature}, (hipStream_t)hip_stream));
     return LBFGSB_OK;
 }
 

@@ -4,8 +4,9 @@ logits, the clipped policy loss and the preference loss.  The tensors are checke
 
 Logits are 2-d float32, bfloat16 or float16 CUDA tensors with unit column stride (rows may be spaced apart and start on any
 element).  Everything is enqueued on torch's current stream of the logits' device; nothing synchronises.  Every call
-returns plain tensors: the gradient is a result, and `logits.backward(r.grad)` hands it on to whatever made the logits.  A gradient
-written over the logits counts as an operation in place: if what made them kept them (a tanh does), backward refuses.
+returns plain tensors without history, whether the logits require a gradient (or carry a tangent) or not: the gradient is a result, and
+`logits.backward(r.grad)` hands it on to whatever made the logits.  A gradient written over the logits counts as an
+operation in place: if what made them kept them (a tanh does), backward refuses.
 """
 from __future__ import annotations
 

@@ -512,6 +512,89 @@ int lbfgsb_preference_loss(int64_t tokens, int64_t pairs, const float* logp, con
                            const uint8_t* mask, const float* weight, const lbfgsb_preference_options* opt_host, double scale,
                            float* loss, float* pair_loss, float* rewards, float* grad, void* hip_stream);
 
+/* ---- rollouts: products with 4-bit weights, tokens drawn, drafts verified ------------------------
+ * What the policy loss above is given: tokens and their log-probabilities when they were drawn.  A drafter (for instance
+ * a copy of the head in 4 bits, lbfgsb_matvec4) proposes tokens drawn from its own logits (lbfgsb_draw_tokens), and the
+ * target's logits for all of them at once tell how many stand (lbfgsb_verify_draft): what is emitted is distributed as if
+ * the target had drawn it.  Random numbers are arguments.  All calls only enqueue kernels, like those above. */
+
+/* W in 4 bits: w_ij = scale_ig (code_ij - zero_ig), g = j / group, code_ij in 0..15; without zeros 8 is in their place.
+ * groups(cols) = ceil(cols / group); the last group of a row may end early. */
+typedef struct {
+    int64_t rows, cols;    /* 1 <= rows <= 2^28, 1 <= cols <= 2^24, 2^35 entries at most (rows taken to 64, cols to 128) */
+    int64_t group;         /* a power of two, 32 or more, at most 2^24 */
+    int scale_type;        /* LBFGSB_F32, LBFGSB_BF16 or LBFGSB_F16: element type of scale and zero */
+    const uint8_t* codes;  /* rows x ceil(cols / 2), row by row: column j in byte j / 2, low four bits for even j */
+    const void* scale;     /* rows x groups(cols), row by row */
+    const void* zero;      /* likewise, any numbers; or NULL */
+} lbfgsb_weights4;
+
+/* Takes w (rows x cols, `ld` elements from one row to the next, of type dtype) to the nearest codes, group by group:
+ *   zero wanted:  scale = (hi - lo) / 15 with lo = min(0, min w) and hi = max(0, max w),  zero = round(-lo / scale) in 0..15;
+ *   NULL:         scale = max |w| / 7;
+ * scale is rounded to its type first, code = round(w / scale) + zero (or 8), held in 0..15.  A group of zeros gets scale 0.
+ * A group that holds NaN, infinity or a spread past its scale's type gets a scale that is no finite number.  The struct's
+ * pointers are written to. */
+int lbfgsb_quantize4(int dtype, int64_t ld, const void* w, const lbfgsb_weights4* to_host, void* hip_stream);
+
+/* The layout that lbfgsb_matvec4 reads: made once from the plain one, kept by the caller. */
+size_t lbfgsb_packed4_bytes(const lbfgsb_weights4* weights_host);   /* 0 on invalid arguments; pointers: whether zero is NULL */
+int lbfgsb_pack4(const lbfgsb_weights4* weights_host, void* packed, size_t packed_bytes, void* hip_stream);
+
+/* y = x W^T: x is `tokens` rows of weights_host->cols entries of x_type, y as many rows of weights_host->rows entries of y_type
+ * (LBFGSB_F32 or x_type), ld_x and ld_y elements apart; rows may start on any element.  packed (16-byte aligned) is what lbfgsb_pack4
+ * made of these weights; of the struct the sizes, scale_type and whether zero is NULL are read.  Made for a few tokens:
+ * every 64 of them read the weights once more.  tokens = 0 is allowed.
+ * Products are exact, sums in 32 bits, the result is rounded once.  y_r is not finite (NaN or infinite) where x_r holds NaN or infinity, or where
+ * |x_r| over a group adds up past 2^124.  y must not overlap x or packed. */
+int lbfgsb_matvec4(const lbfgsb_weights4* weights_host, const void* packed, int64_t tokens, int x_type, int64_t ld_x, const void* x,
+                   int y_type, int64_t ld_y, void* y, void* hip_stream);
+
+/* A token for each row of logits, from a number u in [0, 1) for each: with p the row's distribution as above,
+ *     token = the smallest j with p_0 + ... + p_j > u,   logp = log p_token.
+ * A masked entry (-infinity) is never drawn; one of less than 2^-100 of the row's largest may count as 0.  u below 0 counts as 0, 1 and above as
+ * the last number below 1.  A row without a distribution (all -infinity; NaN or +infinity in it), and one with u = NaN, gives token -1 and logp NaN.
+ * The sums are good for 1e-7: a u that is nearer than that to a token's border may give its neighbour.  vocab <= 2^21; grad is not
+ * looked at.  The workspace goes by the size that lbfgsb_draw_workspace_bytes gives, as for the losses. */
+size_t lbfgsb_draw_workspace_bytes(const lbfgsb_logits* logits_host);
+int lbfgsb_draw_tokens(const lbfgsb_logits* logits_host, const float* uniform, int64_t* tokens, float* logp, void* workspace,
+                       size_t workspace_bytes, void* hip_stream);
+
+/* Drafted tokens of each request, against the target's logits.  Position t of request i has its logits at
+ * z + i * ld_request + t * ld (t = 0 .. drafts), the drafter's at draft_z + i * draft_ld_request + t * draft_ld (t < drafts). */
+typedef struct {
+    int dtype;                        /* LBFGSB_F32, LBFGSB_BF16 or LBFGSB_F16: element type of both */
+    int64_t requests, drafts, vocab;  /* requests * (drafts + 1) <= 2^31-1, 0 <= drafts <= 128, 1 <= vocab <= 2^21 */
+    const void* z;
+    int64_t ld, ld_request;           /* >= vocab, where there is more than one */
+    double temperature;
+    const void* draft_z;              /* NULL: the drafter is certain of each of its tokens */
+    int64_t draft_ld, draft_ld_request;
+    double draft_temperature;
+    const float* draft_logp;          /* requests x drafts: the drafter's log-probabilities of the drafted tokens (lbfgsb_draw_tokens);
+                                         NULL: they are worked out from draft_z */
+    const int64_t* drafted;           /* requests x drafts */
+    const int64_t* lengths;           /* requests entries: how many drafts there are, held to at most `drafts`; NULL: all.  A negative
+                                         one marks a request that has ended: nothing of it is read */
+    const float* uniform;             /* requests x drafts: u */
+    const float* last_uniform;        /* requests entries: v */
+} lbfgsb_drafts;
+/* With p_t and q_t the two distributions at position t and x_t the drafted token: x_t is accepted if q_t(x_t) > 0 and u_t q_t(x_t) <
+ * p_t(x_t).  At the first x_t that is not, a token is drawn by v (as above, from the running sums) from max(p_t - q_t, 0), or from p_t where that is
+ * 0 throughout; after all accepted, from p at the position behind them.
+ *   draft_z NULL:     q_t = 1 at x_t, 0 elsewhere.
+ *   draft_logp given: q_t(j) = exp(draft_logp_t + (draft_z_tj - draft_z_tx) / draft_temperature).
+ * A drafted token outside the vocabulary, and one whose q_t(x_t) is not finite (its own logit or draft_logp infinite or NaN; without draft_logp: NaN or
+ * +infinity anywhere in the drafter's row, or -infinity throughout), counts as q_t = 0: it is not accepted and p_t is drawn from.  With draft_logp the
+ * drafter's row is read only where its token is not accepted; if that gives no finite q_t, p_t is drawn from.
+ * Positions behind a request's length are not read, whatever they hold.
+ * tokens, logp: requests x (drafts + 1): what is emitted, accepted tokens and then the drawn one, with the target's log-probabilities;
+ * -1 and 0 behind it.  count: requests entries, how many are emitted.  Where the drawn token's row has no distribution, or v is NaN, the token is
+ * -1, its logp NaN, and it is not counted. */
+size_t lbfgsb_verify_workspace_bytes(const lbfgsb_drafts* drafts_host);
+int lbfgsb_verify_draft(const lbfgsb_drafts* drafts_host, int64_t* tokens, int64_t* count, float* logp, void* workspace,
+                        size_t workspace_bytes, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

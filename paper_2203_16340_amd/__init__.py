@@ -32,6 +32,8 @@ EXPORTS = [
     "lbfgsb_logits_workspace_bytes", "lbfgsb_token_logprob", "lbfgsb_token_logprob_grad", "lbfgsb_token_logprob_stats",
     "lbfgsb_token_logprob_stats_grad", "lbfgsb_distill_loss", "lbfgsb_policy_loss",
     "lbfgsb_preference_loss",
+    "lbfgsb_quantize4", "lbfgsb_packed4_bytes", "lbfgsb_pack4", "lbfgsb_matvec4", "lbfgsb_draw_workspace_bytes", "lbfgsb_draw_tokens",
+    "lbfgsb_verify_workspace_bytes", "lbfgsb_verify_draft",
 ]
 
 
@@ -173,6 +175,7 @@ def lib():
         L.lbfgsb_auglag_destroy.restype = None
         L.lbfgsb_auglag_destroy.argtypes = [vp]
         losses.declare(L)
+        rollouts.declare(L)
         _lib = L
     return _lib
 
@@ -593,7 +596,9 @@ def solver_for_problem(prob, device="cuda:0", **option_overrides) -> Solver:
     return s
 
 
-from . import losses  # noqa: E402  (it uses what is above)
+from . import losses, rollouts  # noqa: E402  (they use what is above)
 from .losses import (  # noqa: E402
     DistillLoss, PolicyLoss, PreferenceLoss, TokenLogprob, distill_loss, policy_loss, preference_loss, token_logprob,
     token_logprob_grad)
+from .rollouts import (  # noqa: E402
+    Codes4, DrawTokens, VerifyDraft, Weights4, draw_tokens, matvec4, pack4, quantize4, verify_draft)

@@ -1,0 +1,72 @@
+// Tokens drawn from rows of logits and drafted tokens verified: arguments, and the launches of draws.hip.
+#pragma once
+
+#include "logits.h"
+
+namespace lb {
+
+constexpr int64_t kMaxDrawVocab = 1 << 21;
+constexpr int64_t kMaxDrafts = 128;
+
+// A row's entries are summed in blocks of this many bytes, a wave's two loads, which begin on 16-byte boundaries of the logits.
+// What is kept of a block, sum_j 2^((z_j - ref) c), tells where in the row a running sum is passed; the one block is then read again.
+constexpr int kBlockBytes = 2048;
+struct BlockSum {
+    float ref, sum;
+};
+// blocks of a row, at most (the first may begin before the row does)
+inline int64_t blocks_of(int64_t vocab, int size) { return (vocab * size + (16 - size) + kBlockBytes - 1) / kBlockBytes; }
+
+// Rows of logits: `each` of them for a request.
+struct RowSet {
+    const void* z;
+    int64_t ld, ld_request;
+    int each;
+};
+
+struct DrawArgs {
+    const void* z;
+    int64_t rows, ld;
+    int vocab;
+    double s;                // 1 / temperature
+    Factor c;
+    const float* uniform;
+    int64_t* tokens;
+    float* logp;
+};
+
+struct VerifyArgs {
+    RowSet target, draft;    // draft.z null: q is 1 at the drafted token
+    int64_t requests;
+    int drafts, vocab;
+    double s, draft_s;
+    Factor c, draft_c;
+    const float* draft_logp; // null: from draft.z
+    const int64_t *drafted, *lengths;
+    const float *uniform, *last_uniform;
+    int64_t *tokens, *count;
+    float* logp;
+};
+
+// What is drawn from at the end of a request, and where.
+struct Decision {
+    int t;                   // position; -1: the request has ended
+    int mode;                // kFromTarget ..
+    int x;                   // kWithout: the token that is left out
+    float m;                 // kRest: p_j = 2^((z_j - m) c) inv
+    float inv;
+    float q_ref, q_factor;   //        q_j = 2^((zq_j - q_ref) cq) q_factor
+};
+enum { kFromTarget = 0, kWithout = 1, kRest = 2 };
+
+// where the parts of a call's workspace are, in bytes (draws.hip); whole: how much there is of it
+struct VerifySpace {
+    size_t target, draft, rest, decision, whole;
+};
+VerifySpace verify_space(int64_t requests, int64_t drafts, int64_t vocab, int size, bool draft_rows, bool draft_sums);
+size_t draw_space(int64_t rows, int64_t vocab, int size);
+
+hipError_t launch_draw(const DrawArgs& a, int dtype, void* ws, hipStream_t st);
+hipError_t launch_verify(const VerifyArgs& a, int dtype, void* ws, hipStream_t st);
+
+}  // namespace lb

@@ -1,53 +1,9 @@
 // C-ABI layer of the losses on logits: argument checks; everything else is enqueued.
-#include <algorithm>
-#include <cmath>
-#include <limits>
-
-#include "logits.h"
+#include "logits_checks.h"
 
 using namespace lb;
 
 namespace {
-
-#define HIP_TRY(expr)                                                                           \
-    do {                                                                                        \
-        hipError_t e_ = (expr);                                                                 \
-        if (e_ != hipSuccess) return fail(LBFGSB_E_HIP, "%s: %s", #expr, hipGetErrorString(e_)); \
-    } while (0)
-
-constexpr int64_t kMaxRows = (1ll << 31) - 1, kMaxVocab = 1ll << 30, kMaxLd = 1ll << 31;
-
-bool is_logit_type(int dtype) { return dtype == LBFGSB_F32 || dtype == LBFGSB_BF16 || dtype == LBFGSB_F16; }
-size_t size_of(int dtype) { return dtype == LBFGSB_F32 ? 4 : 2; }
-bool misaligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) != 0; }
-
-int check_shape(const lbfgsb_logits* l) {
-    if (!l) return fail(LBFGSB_E_INVALID_ARG, "logits is NULL");
-    if (!is_logit_type(l->dtype)) return fail(LBFGSB_E_INVALID_ARG, "logits: unknown dtype %d", l->dtype);
-    if (l->rows < 0 || l->rows > kMaxRows) return fail(LBFGSB_E_INVALID_ARG, "rows must be in 0..2^31-1 (got %lld)", (long long)l->rows);
-    if (l->vocab < 1 || l->vocab > kMaxVocab) return fail(LBFGSB_E_INVALID_ARG, "vocab must be in 1..2^30 (got %lld)", (long long)l->vocab);
-    return LBFGSB_OK;
-}
-
-// grad: the call writes one; 1: it has to, 0: if there is one, -1: it does not
-int check_logits(const lbfgsb_logits* l, int grad) {
-    if (int rc = check_shape(l)) return rc;
-    if (l->ld < l->vocab || l->ld > kMaxLd) return fail(LBFGSB_E_INVALID_ARG, "ld must be in vocab..2^31 (got %lld)", (long long)l->ld);
-    // (the exponents' factor is held in 32 bits: infinite, it makes a number of no row)
-    if (!(l->temperature > 0.0) || !std::isfinite(l->temperature) || !std::isfinite((float)(1.44269504088896340736 / l->temperature)))
-        return fail(LBFGSB_E_INVALID_ARG, "temperature must be positive, finite and above 4.24e-39 (got %g)", l->temperature);
-    if (l->rows == 0) return LBFGSB_OK;
-    const size_t b = size_of(l->dtype);
-    if (!l->z || misaligned(l->z, b)) return fail(LBFGSB_E_INVALID_ARG, "z is NULL or not aligned to its elements");
-    if (grad < 0 || (!l->grad && !grad)) return LBFGSB_OK;
-    if (!l->grad || misaligned(l->grad, b)) return fail(LBFGSB_E_INVALID_ARG, "grad is NULL or not aligned to its elements");
-    if (l->ld_grad < l->vocab || l->ld_grad > kMaxLd) return fail(LBFGSB_E_INVALID_ARG, "ld_grad must be in vocab..2^31 (got %lld)", (long long)l->ld_grad);
-    const uintptr_t z = (uintptr_t)l->z, g = (uintptr_t)l->grad;
-    const uintptr_t nz = ((l->rows - 1) * l->ld + l->vocab) * b, ng = ((l->rows - 1) * l->ld_grad + l->vocab) * b;
-    if (z < g + ng && g < z + nz && !(z == g && (l->ld == l->ld_grad || l->rows == 1)))
-        return fail(LBFGSB_E_INVALID_ARG, "grad overlaps z without being z");
-    return LBFGSB_OK;
-}
 
 size_t workspace_of(const lbfgsb_logits* l, bool grad) {
     if (l->rows == 0 || row_splits(l->rows, l->vocab, (int)size_of(l->dtype), grad) == 1) return 0;
@@ -55,18 +11,7 @@ size_t workspace_of(const lbfgsb_logits* l, bool grad) {
 }
 
 int check_workspace(const lbfgsb_logits* l, bool grad, const void* ws, size_t bytes) {
-    const size_t need = workspace_of(l, grad);
-    if (need == 0) return LBFGSB_OK;
-    if (!ws || misaligned(ws, 256)) return fail(LBFGSB_E_INVALID_ARG, "workspace is NULL or not aligned to 256 bytes");
-    if (bytes < need) return fail(LBFGSB_E_INVALID_ARG, "workspace too small: %zu bytes, need %zu", bytes, need);
-    return LBFGSB_OK;
-}
-
-Factor factor_of(double s) {
-    const double c = s * 1.44269504088896340736;
-    // (never 0, which times -infinity is no number)
-    const float high = std::max((float)c, std::numeric_limits<float>::denorm_min()), low = (float)(c - (double)high);
-    return {high, low};
+    return check_space(workspace_of(l, grad), ws, bytes);
 }
 
 LogitsArgs args_of(const lbfgsb_logits* l, bool grad) {

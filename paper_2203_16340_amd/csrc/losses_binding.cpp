@@ -1,44 +1,9 @@
 // Python's way into the losses on logits: checks of the tensors, new tensors for the results and the C call, in one step.  (The calls
 // take some 3 us each to enqueue what they do; made from Python, the rest of a call on a few rows took 8 to 13 us.)  Every function returns
 // the C entry's code first; what the code says is the caller's to raise.
-#include <torch/extension.h>
-
-#include <optional>
-#include <string>
-#include <tuple>
-
-#include "../../include/lbfgsb.h"
-
-namespace py = pybind11;
-using at::Tensor;
-using Maybe = std::optional<Tensor>;
+#include "binding.h"
 
 namespace {
-
-int logit_type(const Tensor& t, const char* name) {
-    const auto d = t.scalar_type();
-    const int type = d == at::kFloat ? LBFGSB_F32 : (d == at::kBFloat16 ? (int)LBFGSB_BF16 : (d == at::kHalf ? (int)LBFGSB_F16 : -1));
-    if (type < 0 || !t.is_cuda() || t.dim() != 2 || (t.stride(1) != 1 && t.size(1) != 1))
-        throw py::type_error(std::string(name) + " must be a 2-d float32/bfloat16/float16 CUDA tensor with unit column stride");
-    return type;
-}
-
-int64_t row_stride(const Tensor& t) { return t.size(0) > 1 ? t.stride(0) : t.size(1); }
-
-// the address of a contiguous 1-d tensor of `numel` entries
-template <typename T = float>
-T* vec(const Tensor& t, const char* name, int64_t numel, const at::Device& dev, at::ScalarType type = at::kFloat) {
-    if (t.scalar_type() != type || t.device() != dev || !t.is_contiguous())
-        throw py::type_error(std::string(name) + " must be a contiguous " + c10::toString(type) + " tensor on " + dev.str());
-    if (t.dim() != 1 || t.size(0) != numel)
-        throw py::value_error(std::string(name) + " must be 1-d with " + std::to_string(numel) + " entries, got " + std::to_string(t.numel()) +
-                              " in " + std::to_string(t.dim()) + " dimensions");
-    return (T*)t.data_ptr();
-}
-template <typename T = float>
-T* maybe(const Maybe& t, const char* name, int64_t numel, const at::Device& dev) {
-    return t ? vec<T>(*t, name, numel, dev) : nullptr;
-}
 
 struct Call {
     lbfgsb_logits lg;
@@ -65,10 +30,8 @@ struct Call {
         lg.grad = grad ? grad->data_ptr() : nullptr;
         lg.ld_grad = grad ? row_stride(*grad) : 0;
     }
-    // After a call that went well: torch learns that the caller's tensor has been written to, so that a way back which kept it is
-    // refused, as after any operation in place.  (Tensors of inference mode have no count and nobody's way back keeps them.)
     int done(int rc) const {
-        if (rc == LBFGSB_OK && given && !grad->is_inference()) grad->unsafeGetTensorImpl()->bump_version();
+        if (rc == LBFGSB_OK && given) written(*grad);
         return rc;
     }
     Tensor rows_of_floats() const { return at::empty({rows}, at::TensorOptions(dev).dtype(at::kFloat)); }
@@ -81,9 +44,6 @@ struct Call {
         return n ? at::empty({n}, at::TensorOptions(dev).dtype(at::kByte)) : Tensor();
     }
 };
-void* address(const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
-size_t bytes(const Tensor& t) { return t.defined() ? (size_t)t.numel() : 0; }
-
 auto token_logprob(const Tensor& z, const Tensor& labels, double temperature, bool entropy, int64_t stream) {
     const Call c(z, temperature, false, std::nullopt);
     const int64_t* y = vec<int64_t>(labels, "labels", c.rows, c.dev, at::kLong);
@@ -191,4 +151,5 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
     m.def("distill_loss", &distill_loss);
     m.def("policy_loss", &policy_loss);
     m.def("preference_loss", &preference_loss);
+    add_rollouts(m);
 }

@@ -1,0 +1,388 @@
+"""Drawn tokens and verified drafts through the library, against the 64-bit definitions of rollouts_reference.
+
+A token is right where its part of the running sum, widened by what sums are off, holds the number: an entry's exponent is rounded (2^-24 of at most 40
+that count), its exponential too, and a block's 1024 entries are added in at most 14 steps, so p, and a running sum of p, is off by less
+than (40 + 2 + 14) 2^-24 = 3.4e-6 of itself even if all went one way; of a difference p - q by as much of p.  What stands within 4e-6 of a border (as a share
+of p's whole) may fall to either side; a token without a part never comes.  A log-probability: ln S is off by 3.4e-6, and it is rounded once."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2203_16340_amd as L
+import rollouts_reference as ref
+from gpu_helpers import DEV
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+ROOM = 4e-6
+SHAPES = [(1, 1), (1, 2), (3, 7), (5, 64), (2, 511), (3, 1024), (4, 1025), (3, 4096), (4, 4097), (130, 1000), (2, 50021), (1, 131073), (3, 262147),
+          (300, 2049), (1500, 333)]
+
+
+def logits_of(shape, dtype, seed=0, spread=3.0):
+    g = torch.Generator().manual_seed(seed + 1000003 * shape[0] + shape[-1])
+    return (torch.randn(*shape, generator=g) * spread).to(dtype)
+
+
+def numbers(shape, seed=0):
+    return torch.from_numpy(np.random.default_rng(seed + 13).random(shape, dtype=np.float32))
+
+
+def near_logp(got, want):
+    assert np.array_equal(np.isnan(got), np.isnan(want)), (got, want)
+    fine = ~np.isnan(want)
+    off = np.abs(got[fine] - want[fine]) - (4e-6 + 2.0 ** -23 * np.abs(want[fine]))
+    assert off.size == 0 or off.max() <= 0, off.max()
+
+
+def check_draw(z, u, temperature, got):
+    zh, uh = z.double().cpu().numpy(), u.cpu().numpy()
+    tokens, logp = got.tokens.cpu().numpy(), got.logp.double().cpu().numpy()
+    want_lp, equal = [], 0
+    for r in range(len(zh)):
+        j, lp, p = ref.draw(zh[r], uh[r], 1 / temperature)
+        equal += int(tokens[r] == j)
+        if p is None:
+            assert tokens[r] == -1
+            want_lp.append(np.nan)
+        else:
+            assert ref.room(p, tokens[r], uh[r]) >= -ROOM, (r, tokens[r], j)
+            want_lp.append(ref.log_softmax(zh[r], 1 / temperature)[tokens[r]])
+    assert len(zh) < 20 or equal > 0.9 * len(zh)
+    near_logp(logp, np.array(want_lp))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,vocab", SHAPES)
+def test_draws(rows, vocab, dtype):
+    z, u = logits_of((rows, vocab), TYPES[dtype]).to(DEV), numbers(rows).to(DEV)
+    for temperature in (1.0, 0.6):
+        got = L.draw_tokens(z, u, temperature=temperature)
+        assert got.tokens.dtype == torch.int64 and got.logp.dtype == torch.float32
+        check_draw(z, u, temperature, got)
+        again = L.draw_tokens(z, u, temperature=temperature)
+        assert torch.equal(again.tokens, got.tokens) and torch.equal(again.logp, got.logp)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab", [5, 300, 5000])
+def test_numbers_over_the_whole_range(vocab, dtype):
+    """One row, numbers in a fine grid and at both ends: every token gets its share."""
+    z = logits_of((1, vocab), TYPES[dtype], seed=3, spread=1.5).to(DEV)
+    u = torch.cat([(torch.arange(4000) + 0.5) / 4000, torch.tensor([0.0, 1 - 2.0 ** -24, 1.0, 2.0, -0.5, -0.0, float("inf"), -float("inf")])]).to(DEV)
+    many = z.expand(len(u), vocab).contiguous()
+    check_draw(many, u, 1.0, L.draw_tokens(many, u))
+    p = torch.softmax(z[0].double(), 0)
+    got = torch.bincount(L.draw_tokens(many[:4000], u[:4000]).tokens, minlength=vocab).double() / 4000
+    assert (got - p).abs().max() <= 1.01 / 4000 + 4e-6
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows", [9, 600])
+@pytest.mark.parametrize("vocab", [9, 1030, 40001])
+def test_masked_rows(vocab, rows, dtype):
+    low, top = torch.finfo(TYPES[dtype]).min, torch.finfo(TYPES[dtype]).max
+    z = logits_of((rows, vocab), TYPES[dtype], seed=5)
+    z[0, 1:] = -torch.inf            # one entry left
+    z[1, :] = -torch.inf             # none
+    z[2, 1:] = low                   # one, masked by the lowest value
+    z[3, :] = low                    # all alike: a uniform row
+    z[4, vocab // 2:] = -torch.inf
+    z[5, ::2] = low
+    z[6, 0] = top
+    z[7, :-1] = -torch.inf           # the last entry alone
+    z[8, 3] = torch.nan
+    z, u = z.to(DEV), numbers(rows, 1).to(DEV)
+    for temperature in (1.0, 1.5):
+        got = L.draw_tokens(z, u, temperature=temperature)
+        check_draw(z, u, temperature, got)
+        t = got.tokens.tolist()
+        assert t[0] == 0 and t[1] == -1 and t[2] == 0 and t[6] == 0 and t[7] == vocab - 1 and t[8] == -1
+        assert t[5] % 2 == 1 and t[4] < vocab // 2
+    for v in (0.0, 1 - 2.0 ** -24):
+        t = L.draw_tokens(z, torch.full((rows,), v, device=DEV)).tokens
+        assert not torch.isinf(z[[0, 4, 7], t[[0, 4, 7]]].float()).any()
+
+
+def test_a_number_that_is_none_and_infinite_logits():
+    z = logits_of((4, 600), torch.float32).to(DEV)
+    z[1, 5], z[2, 5] = torch.inf, -torch.inf
+    got = L.draw_tokens(z, torch.tensor([torch.nan, 0.5, 0.5, 0.5], device=DEV))
+    assert (got.tokens[:2] == -1).all() and got.logp[:2].isnan().all() and (got.tokens[2:] >= 0).all() and got.logp[2:].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_extreme_temperatures(dtype):
+    z, u = logits_of((6, 3000), TYPES[dtype]).to(DEV), numbers(6).to(DEV)
+    z[:, 7] = 20.0
+    cold = L.draw_tokens(z, u, temperature=1e-30)
+    assert (cold.tokens == 7).all() and (cold.logp == 0).all()
+    hot = L.draw_tokens(z, u, temperature=1e30)
+    assert (hot.logp + np.log(3000)).abs().max() < 1e-5
+    check_draw(z, u, 1e30, hot)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("start", [0, 1, 3, 5])
+@pytest.mark.parametrize("rows", [6, 700])
+def test_rows_that_begin_anywhere(start, rows, dtype):
+    vocab = 2603
+    store = torch.full((rows, vocab + 11), torch.nan, dtype=TYPES[dtype], device=DEV)
+    z = store[:, start:start + vocab]
+    z.copy_(logits_of((rows, vocab), TYPES[dtype]))
+    u = numbers(rows).to(DEV)
+    check_draw(z, u, 1.0, L.draw_tokens(z, u))
+
+
+def test_rows_further_apart_than_32_bits_tell():
+    vocab, ld = 700, 2 ** 31 - 5
+    store = torch.empty(2 * ld + vocab + 8, dtype=torch.bfloat16, device=DEV)
+    z = store.as_strided((3, vocab), (ld, 1), 3)
+    z.copy_(logits_of((3, vocab), torch.bfloat16))
+    u = numbers(3).to(DEV)
+    check_draw(z, u, 1.0, L.draw_tokens(z, u))
+    v = L.verify_draft(z.unsqueeze(1), torch.empty(3, 0, dtype=torch.int64, device=DEV), torch.empty(3, 0, device=DEV), u)
+    assert torch.equal(v.tokens[:, 0], L.draw_tokens(z.contiguous(), u).tokens)
+
+
+def test_no_rows_and_refusals_of_draws():
+    z, u = torch.zeros(4, 100, device=DEV), torch.zeros(4, device=DEV)
+    none = L.draw_tokens(z[:0], u[:0])
+    assert none.tokens.shape == none.logp.shape == (0,)
+    for bad in (lambda: L.draw_tokens(z.double(), u), lambda: L.draw_tokens(z[0], u), lambda: L.draw_tokens(z.t(), u), lambda: L.draw_tokens(z, u.double()),
+                lambda: L.draw_tokens(z, u.cpu())):
+        with pytest.raises(TypeError):
+            bad()
+    with pytest.raises(ValueError):
+        L.draw_tokens(z, u[:3])
+    for t in (0.0, -1.0, float("nan"), 1e-40):
+        with pytest.raises(L.LbfgsbError):
+            L.draw_tokens(z, u, temperature=t)
+    with pytest.raises(L.LbfgsbError):
+        L.draw_tokens(torch.zeros(1, (1 << 21) + 1, device=DEV, dtype=torch.float16), u[:1])
+
+
+# ---- verification ---------------------------------------------------------------------------------------------------------
+
+
+def drafts_of(n, drafts, vocab, dtype, seed=0, noise=0.5, spread=2.0):
+    """Target and drafter near each other, tokens drawn from the drafter, numbers."""
+    rng = np.random.default_rng(seed + n + 10 * drafts + vocab)
+    z = logits_of((n, drafts + 1, vocab), dtype, seed, spread)
+    zq = (z[:, :drafts].float() + noise * torch.from_numpy(rng.normal(size=(n, drafts, vocab)).astype(np.float32))).to(dtype)
+    x = np.zeros((n, drafts), dtype=np.int64)
+    lq = np.zeros((n, drafts))
+    for i in range(n):
+        for t in range(drafts):
+            lp = ref.log_softmax(zq[i, t].double().numpy(), 1.0)
+            x[i, t] = ref.pick(np.exp(lp), rng.random())
+            lq[i, t] = lp[x[i, t]]
+    return z, zq, torch.from_numpy(x), torch.from_numpy(lq).float(), torch.from_numpy(rng.random((n, drafts), dtype=np.float32)), \
+        torch.from_numpy(rng.random(n, dtype=np.float32))
+
+
+def check_verify(got, z, x, u, v, s=1.0, draft=None, draft_logp=None, lengths=None, sq=1.0):
+    z, x, u, v = z.double().cpu().numpy(), x.cpu().numpy(), u.cpu().numpy(), v.cpu().numpy()
+    draft = None if draft is None else draft.double().cpu().numpy()
+    draft_logp = None if draft_logp is None else draft_logp.cpu().numpy()
+    lengths = None if lengths is None else lengths.tolist()
+    tokens, count, logp = got.tokens.cpu().numpy(), got.count.cpu().numpy(), got.logp.double().cpu().numpy()
+    n, drafts = x.shape
+    assert tokens.shape == logp.shape == (n, drafts + 1) and count.shape == (n,)
+    near = 0
+    for i in range(n):
+        want, want_lp, mass, lp, how_near = ref.verify(z[i], x[i], u[i], v[i], s, None if draft is None else draft[i],
+                                                       None if draft_logp is None else draft_logp[i], None if lengths is None else lengths[i], sq)
+        if how_near <= ROOM:
+            near += 1
+            continue
+        k = len(want)
+        if mass is not None:
+            want[-1] = int(tokens[i, k - 1])
+            assert ref.room(mass, want[-1], v[i]) >= -ROOM, (i, tokens[i])
+            want_lp[-1] = lp[want[-1]]
+        assert tokens[i, :k].tolist() == want, (i, tokens[i], want)
+        assert (tokens[i, k:] == -1).all() and (logp[i, k:] == 0).all()
+        assert count[i] == k - (k > 0 and want[-1] < 0)
+        near_logp(logp[i, :k], np.array(want_lp))
+    assert near <= 0.1 * n
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,drafts,vocab", [(1, 1, 1), (1, 1, 2), (2, 3, 7), (3, 1, 1000), (40, 4, 333), (5, 9, 1025), (4, 2, 4097), (2, 3, 50021), (1, 5, 131073)])
+def test_verification(n, drafts, vocab, dtype):
+    z, zq, x, lq, u, v = drafts_of(n, drafts, vocab, TYPES[dtype])
+    on = [t.to(DEV) for t in (z, zq, x, lq, u, v)]
+    for logp in (None, on[3]):
+        got = L.verify_draft(on[0], on[2], on[4], on[5], draft_logits=on[1], draft_logp=logp)
+        check_verify(got, z, x, u, v, draft=zq, draft_logp=None if logp is None else lq)
+        again = L.verify_draft(on[0], on[2], on[4], on[5], draft_logits=on[1], draft_logp=logp)
+        assert all(torch.equal(a, b) for a, b in zip(got, again))
+    # a drafter that is certain
+    u = u * 0.3
+    got = L.verify_draft(on[0], on[2], u.to(DEV), on[5])
+    check_verify(got, z, x, u, v)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_lengths_and_temperatures(dtype):
+    n, drafts, vocab = 24, 6, 777
+    z, zq, x, lq, u, v = drafts_of(n, drafts, vocab, TYPES[dtype], seed=4)
+    lengths = torch.tensor([0, 1, 2, 3, 4, 5, 6, 7, 100, -1, -100, 2] * 2)
+    # what stands behind a request's length is not looked at
+    for i in range(n):
+        k = min(int(lengths[i]), drafts)
+        z[i, max(k, -1) + 1:], zq[i, max(k, 0):], x[i, max(k, 0):] = torch.nan, torch.nan, 1 << 40
+        if k < 0:
+            z[i] = torch.nan
+    for logp in (None, lq):
+        got = L.verify_draft(z.to(DEV), x.to(DEV), u.to(DEV), v.to(DEV), draft_logits=zq.to(DEV), draft_logp=None if logp is None else lq.to(DEV),
+                             lengths=lengths.to(DEV), temperature=0.8, draft_temperature=1.3)
+        check_verify(got, z, x, u, v, 1 / 0.8, zq, logp, lengths, 1 / 1.3)
+    got = L.verify_draft(z.to(DEV), x.to(DEV), u.to(DEV), v.to(DEV), lengths=lengths.to(DEV), temperature=0.8)
+    check_verify(got, z, x, u, v, 1 / 0.8, lengths=lengths)
+
+
+def test_a_drafter_that_is_the_target():
+    """p = q: nothing is refused, whatever the numbers below 1 (up to what q's rounding leaves of it)."""
+    z, _, x, _, u, v = drafts_of(16, 5, 500, torch.float32, seed=2)
+    u = u * 0.99999
+    got = L.verify_draft(z.to(DEV), x.to(DEV), u.to(DEV), v.to(DEV), draft_logits=z[:, :5].contiguous().to(DEV))
+    assert (got.count == 6).all() and torch.equal(got.tokens[:, :5].cpu(), x)
+    check_verify(got, z, x, u, v, draft=z[:, :5])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_without_a_distribution_and_tokens_outside_the_vocabulary(dtype):
+    n, drafts, vocab = 10, 3, 1100
+    z, zq, x, lq, u, v = drafts_of(n, drafts, vocab, TYPES[dtype], seed=6, noise=0.05)
+    u[:] = 0.05                                     # nearly everything that can be accepted is
+    z[0, 1] = -torch.inf                            # no target at position 1
+    z[1, 3, 5] = torch.nan                          # none behind the last draft
+    zq[2, 0] = -torch.inf                           # no drafter: p is drawn from
+    zq[3, 1, 9] = torch.nan
+    x[4, 0], x[5, 2] = -1, vocab
+    z[6, 0, 1:] = -torch.inf                        # one token only, another drafted
+    x[6, 0] = 7
+    lq[7, 1] = -torch.inf
+    lq[8, 2] = torch.nan
+    v[9] = torch.nan
+    for logp in (None, lq):
+        got = L.verify_draft(z.to(DEV), x.to(DEV), u.to(DEV), v.to(DEV), draft_logits=zq.to(DEV), draft_logp=None if logp is None else lq.to(DEV))
+        check_verify(got, z, x, u, v, draft=zq, draft_logp=logp)
+        assert got.tokens[0, 1] == -1 and got.logp[0, 1].isnan() and got.count[0] == 1
+        assert got.count[4] == 1 and got.tokens[6, 0] == 0 and got.count[6] == 1
+    got = L.verify_draft(z.to(DEV), x.to(DEV), u.to(DEV), v.to(DEV))
+    check_verify(got, z, x, u, v)
+
+
+def test_all_the_mass_on_the_refused_token():
+    """p is 1 at the drafted token, and refused by a number of 1: nothing is left but that token."""
+    z = torch.full((1, 2, 50), -200.0, device=DEV)
+    z[0, 0, 11] = z[0, 1, 3] = 0.0
+    x = torch.tensor([[11]], device=DEV)
+    got = L.verify_draft(z, x, torch.ones(1, 1, device=DEV), torch.full((1,), 0.5, device=DEV))
+    assert got.tokens.tolist() == [[11, -1]] and got.count.tolist() == [1]
+
+
+def test_positions_that_lie_anywhere():
+    n, drafts, vocab = 5, 3, 1203
+    z, zq, x, lq, u, v = drafts_of(n, drafts, vocab, torch.bfloat16, seed=8)
+    store = torch.full((drafts + 1, n, vocab + 9), torch.nan, dtype=torch.bfloat16, device=DEV)
+    zs = store.transpose(0, 1)[:, :, 3:3 + vocab]
+    zs.copy_(z)
+    store = torch.full((n, drafts + 2, vocab + 2), torch.nan, dtype=torch.bfloat16, device=DEV)
+    qs = store[:, 1:1 + drafts, 1:1 + vocab]
+    qs.copy_(zq)
+    on = [t.to(DEV) for t in (x, u, v, lq)]
+    for logp in (None, on[3]):
+        got = L.verify_draft(zs, *on[:3], draft_logits=qs, draft_logp=logp)
+        check_verify(got, z, x, u, v, draft=zq, draft_logp=None if logp is None else lq)
+
+
+def test_no_drafts_is_a_draw():
+    z, u = logits_of((7, 1, 3000), torch.float16).to(DEV), numbers(7).to(DEV)
+    none = torch.empty(7, 0, dtype=torch.int64, device=DEV)
+    got = L.verify_draft(z, none, none.float(), u)
+    want = L.draw_tokens(z[:, 0], u)
+    assert torch.equal(got.tokens[:, 0], want.tokens) and torch.equal(got.logp[:, 0], want.logp) and (got.count == 1).all()
+    got = L.verify_draft(z[:0], none[:0], none[:0].float(), u[:0])
+    assert got.tokens.shape == (0, 1) and got.count.shape == (0,)
+
+
+def test_refusals_of_verifications():
+    z, x = torch.zeros(2, 4, 100, device=DEV), torch.zeros(2, 3, dtype=torch.int64, device=DEV)
+    u, v = torch.zeros(2, 3, device=DEV), torch.zeros(2, device=DEV)
+    q = z[:, :3].contiguous()
+    L.verify_draft(z, x, u, v, draft_logits=q)
+    for bad in (lambda: L.verify_draft(z[0], x, u, v), lambda: L.verify_draft(z.double(), x, u, v), lambda: L.verify_draft(z, x.int(), u, v),
+                lambda: L.verify_draft(z, x, u.double(), v), lambda: L.verify_draft(z, x, u, v, draft_logits=q.half()),
+                lambda: L.verify_draft(z, x, u, v, draft_logits=q.cpu()), lambda: L.verify_draft(z, x, u, v, lengths=v),
+                lambda: L.verify_draft(z.transpose(1, 2), x, u, v), lambda: L.verify_draft(z, x.t().contiguous().t(), u, v)):
+        with pytest.raises(TypeError):
+            bad()
+    for bad in (lambda: L.verify_draft(z, x[:, :2].contiguous(), u, v), lambda: L.verify_draft(z, x, u, v[:1]), lambda: L.verify_draft(z, x, u, v, draft_logits=z),
+                lambda: L.verify_draft(z, x, u, v, draft_logp=u), lambda: L.verify_draft(z[:, :0], x, u, v)):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: L.verify_draft(z, x, u, v, temperature=0.0), lambda: L.verify_draft(z, x, u, v, draft_logits=q, draft_temperature=-1.0),
+                lambda: L.verify_draft(z[:1].expand(2, 4, 100), x, u, v)):
+        with pytest.raises(L.LbfgsbError):
+            bad()
+
+
+def test_a_replayed_graph_and_two_graphs_at_once():
+    """Two captured calls with workspaces of their own, replayed on two streams at the same time, against the plain calls."""
+    n, drafts, vocab = 6, 3, 9000
+    graphs, states = [], []
+    for k in range(2):
+        z, zq, x, lq, u, v = (t.to(DEV) for t in drafts_of(n, drafts, vocab, torch.bfloat16, seed=30 + k))
+        L.verify_draft(z, x, u, v, draft_logits=zq)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            r = L.verify_draft(z, x, u, v, draft_logits=zq)
+            d = L.draw_tokens(z[:, 0], v)
+        graphs.append(graph)
+        states.append((z, zq, x, u, v, r, d))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for turn in range(4):
+        for z, zq, x, u, v, _, _ in states:
+            u.copy_(numbers((n, drafts), turn))
+            v.copy_(numbers(n, 50 + turn))
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        for z, zq, x, u, v, r, d in states:
+            want = L.verify_draft(z, x, u, v, draft_logits=zq)
+            assert all(torch.equal(a, b) for a, b in zip(r, want))
+            assert torch.equal(d.tokens, L.draw_tokens(z[:, 0], v).tokens)
+
+
+# ---- together ---------------------------------------------------------------------------------------------------------------
+
+
+def test_drafted_by_4_bits_and_verified_what_is_emitted_is_the_targets():
+    """Head in 4 bits -> drawn tokens -> verification by the head itself, on many copies of one position: the first tokens' shares are the
+    target's p, and their log-probabilities token_logprob's."""
+    g = torch.Generator(DEV).manual_seed(1)
+    vocab, width, n = 24, 64, 20000
+    head = torch.randn(vocab, width, device=DEV, generator=g) * 0.25
+    w = L.pack4(*L.quantize4(head, group=32, symmetric=True), group=32)
+    h = torch.randn(1, width, device=DEV, generator=g).expand(n, width).contiguous()
+    zq = L.matvec4(h, w)
+    assert torch.equal(zq[:1].expand(n, vocab), zq)
+    d = L.draw_tokens(zq, torch.rand(n, device=DEV, generator=g))
+    z = (h @ head.t())[:, None].expand(n, 2, vocab).contiguous()
+    r = L.verify_draft(z, d.tokens[:, None], torch.rand(n, 1, device=DEV, generator=g), torch.rand(n, device=DEV, generator=g), draft_logits=zq[:, None],
+                       draft_logp=d.logp[:, None])
+    p = torch.softmax(z[0, 0].double(), 0)
+    share = torch.bincount(r.tokens[:, 0], minlength=vocab).double() / n
+    # (5 standard deviations of a share)
+    assert ((share - p).abs() <= 5 * (p * (1 - p) / n).sqrt() + 1e-9).all()
+    assert 0.5 < (r.count == 2).float().mean() < 1
+    want = L.token_logprob(z[:, 0].contiguous(), r.tokens[:, 0].contiguous()).logp
+    assert (r.logp[:, 0] - want).abs().max() < 1e-5

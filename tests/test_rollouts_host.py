@@ -1,0 +1,143 @@
+"""What makes rollouts without a GPU: struct layouts, and refusals that come before any device work."""
+import ctypes as C
+import os
+import subprocess
+
+import pytest
+import torch
+
+import paper_2203_16340_amd as L
+from paper_2203_16340_amd import losses as S
+from paper_2203_16340_amd import rollouts as R
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def test_struct_layouts_match_the_header(tmp_path):
+    pairs = [("lbfgsb_weights4", R.Weights4Struct, "scale_type"), ("lbfgsb_weights4", R.Weights4Struct, "zero"),
+             ("lbfgsb_drafts", R.Drafts, "ld_request"), ("lbfgsb_drafts", R.Drafts, "draft_z"), ("lbfgsb_drafts", R.Drafts, "draft_logp"),
+             ("lbfgsb_drafts", R.Drafts, "last_uniform")]
+    src = tmp_path / "sz.c"
+    src.write_text('#include <stdio.h>\n#include <stddef.h>\n#include "lbfgsb.h"\nint main(void){' +
+                   "".join(f'printf("%zu %zu ", sizeof({c}), offsetof({c}, {f}));' for c, _, f in pairs) + "return 0;}\n")
+    exe = tmp_path / "sz"
+    subprocess.run(["gcc", "-I", os.path.join(ROOT, "include"), str(src), "-o", str(exe)], check=True)
+    got = [int(t) for t in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split()]
+    assert got == [v for _, s, f in pairs for v in (C.sizeof(s), getattr(s, f).offset)]
+
+
+def _weights(rows=100, cols=70, group=32, scale_type=1, codes=0x1000, scale=0x2000, zero=None):
+    return R.Weights4Struct(rows, cols, group, scale_type, codes, scale, zero)
+
+
+BAD_WEIGHTS = [dict(rows=0), dict(rows=(1 << 28) + 1), dict(cols=0), dict(cols=(1 << 24) + 1), dict(rows=1 << 28, cols=129), dict(group=16), dict(group=48),
+               dict(group=0), dict(group=1 << 25), dict(scale_type=0), dict(scale_type=4)]
+
+
+@pytest.mark.parametrize("bad", BAD_WEIGHTS, ids=str)
+def test_weights_are_checked(bad):
+    lib, w = L.lib(), _weights(**bad)
+    b = C.byref(w)
+    assert lib.lbfgsb_packed4_bytes(b) == 0
+    assert lib.lbfgsb_quantize4(1, 1 << 25, 0x9000, b, None) == L.E_INVALID_ARG
+    assert lib.lbfgsb_pack4(b, 0x10000, 1 << 40, None) == L.E_INVALID_ARG
+    assert lib.lbfgsb_matvec4(b, 0x10000, 1, 1, 70, 0x9000, 1, 100, 0x900000, None) == L.E_INVALID_ARG
+    assert lib.lbfgsb_last_error()
+
+
+def test_packed_size():
+    lib = L.lib()
+    # 2 blocks of 64 rows, 1 step of 128 columns: 8192 bytes of codes; 3 groups: 2 * 3 * 64 scales of 4 bytes, as many zeros
+    assert lib.lbfgsb_packed4_bytes(C.byref(_weights())) == 8192 + 1536
+    assert lib.lbfgsb_packed4_bytes(C.byref(_weights(zero=0x3000))) == 8192 + 3072
+    assert lib.lbfgsb_packed4_bytes(C.byref(_weights(scale_type=2))) == 8192 + 768
+    assert lib.lbfgsb_packed4_bytes(C.byref(_weights(rows=128, cols=129, group=128, scale_type=3))) == 16384 + 512
+    assert lib.lbfgsb_packed4_bytes(None) == 0
+
+
+def test_quantising_and_packing_are_checked():
+    lib, w = L.lib(), _weights()
+    b = C.byref(w)
+    bad = [lib.lbfgsb_quantize4(0, 70, 0x9000, b, None), lib.lbfgsb_quantize4(1, 69, 0x9000, b, None), lib.lbfgsb_quantize4(1, 70, None, b, None),
+           lib.lbfgsb_quantize4(1, 70, 0x9002, b, None), lib.lbfgsb_quantize4(1, 70, 0x9000, None, None),
+           lib.lbfgsb_pack4(b, None, 1 << 30, None), lib.lbfgsb_pack4(b, 0x10008, 1 << 30, None), lib.lbfgsb_pack4(b, 0x10000, 8192 + 1535, None)]
+    for kw in (dict(codes=None), dict(scale=None), dict(scale=0x2002), dict(zero=0x2001)):
+        v = _weights(**kw)
+        bad += [lib.lbfgsb_quantize4(1, 70, 0x9000, C.byref(v), None), lib.lbfgsb_pack4(C.byref(v), 0x10000, 1 << 30, None)]
+    assert bad == [L.E_INVALID_ARG] * len(bad)
+
+
+def test_products_are_checked():
+    lib, w = L.lib(), _weights()
+
+    def call(tokens=2, x_type=1, ld_x=70, x=0x100000, y_type=1, ld_y=100, y=0x200000, packed=0x10000, weights=C.byref(w)):
+        return lib.lbfgsb_matvec4(weights, packed, tokens, x_type, ld_x, x, y_type, ld_y, y, None)
+
+    for kw in (dict(tokens=-1), dict(tokens=1 << 31), dict(x_type=0), dict(y_type=2), dict(x_type=2, y_type=3), dict(ld_x=69), dict(ld_y=99),
+               dict(x=None), dict(y=None), dict(x=0x100002), dict(y=0x200001), dict(packed=None), dict(packed=0x10004), dict(weights=None),
+               dict(y=0x100000), dict(y=0x100000 - 400), dict(y=0x10000 + 8192)):
+        assert call(**kw) == L.E_INVALID_ARG, kw
+    assert call(tokens=0, x=None, y=None, packed=None) == L.OK
+
+
+def test_draws_are_checked():
+    lib = L.lib()
+
+    def call(lg, u=0x3000, tokens=0x4000, logp=0x5000, ws=0x100000, n=1 << 30):
+        return lib.lbfgsb_draw_tokens(C.byref(lg) if lg is not None else None, u, tokens, logp, ws, n, None)
+
+    def lg(dtype=1, rows=4, vocab=100, ld=100, z=0x10000, temperature=1.0):
+        return S.Logits(dtype, rows, vocab, ld, z, temperature, None, 0)
+
+    for kw in (dict(dtype=0), dict(rows=-1), dict(rows=1 << 31), dict(vocab=0), dict(vocab=(1 << 21) + 1, ld=1 << 22), dict(ld=99), dict(z=None),
+               dict(z=0x10001), dict(temperature=0.0), dict(temperature=float("nan")), dict(temperature=1e-320)):
+        assert call(lg(**kw)) == L.E_INVALID_ARG, kw
+    assert call(None) == call(lg(), u=None) == call(lg(), tokens=None) == call(lg(), logp=None) == L.E_INVALID_ARG
+    assert call(lg(rows=0, z=None), u=None, tokens=None, logp=None, ws=None, n=0) == L.OK
+    big = lg(rows=9, vocab=50000, ld=50000)
+    n = lib.lbfgsb_draw_workspace_bytes(C.byref(big))
+    if n:
+        assert n % 256 == 0 and call(big, n=n - 1) == call(big, ws=0x100008, n=n) == L.E_INVALID_ARG
+    assert lib.lbfgsb_draw_workspace_bytes(C.byref(lg(vocab=1 << 22))) == 0 and lib.lbfgsb_draw_workspace_bytes(None) == 0
+
+
+def _drafts(**kw):
+    at = dict(dtype=1, requests=3, drafts=4, vocab=1000, z=0x10000, ld=1000, ld_request=5000, temperature=1.0, draft_z=0x90000, draft_ld=1000,
+              draft_ld_request=4000, draft_temperature=1.0, draft_logp=0x1000, drafted=0x2000, lengths=None, uniform=0x3000, last_uniform=0x4000)
+    at.update(kw)
+    return R.Drafts(*[at[n] for n, _ in R.Drafts._fields_])
+
+
+def _verify(d, tokens=0x5000, count=0x6000, logp=0x7000, ws=0x100000, n=1 << 40):
+    return L.lib().lbfgsb_verify_draft(C.byref(d) if d is not None else None, tokens, count, logp, ws, n, None)
+
+
+BAD_DRAFTS = [dict(dtype=0), dict(requests=-1), dict(requests=1 << 30), dict(drafts=-1), dict(drafts=129), dict(vocab=0), dict(vocab=(1 << 21) + 1),
+              dict(z=None), dict(z=0x10002), dict(draft_z=0x90001), dict(ld=999), dict(ld_request=999), dict(draft_ld=999), dict(draft_ld_request=-1),
+              dict(temperature=0.0), dict(temperature=float("inf")), dict(draft_temperature=-1.0), dict(draft_z=None), dict(drafted=None), dict(uniform=None),
+              dict(last_uniform=None)]
+
+
+@pytest.mark.parametrize("bad", BAD_DRAFTS, ids=str)
+def test_drafts_are_checked(bad):
+    assert _verify(_drafts(**bad)) == L.E_INVALID_ARG and L.lib().lbfgsb_last_error()
+
+
+def test_outputs_and_workspace_of_a_verification():
+    lib = L.lib()
+    assert _verify(None) == _verify(_drafts(), tokens=None) == _verify(_drafts(), count=None) == _verify(_drafts(), logp=None) == L.E_INVALID_ARG
+    for kw in ({}, dict(draft_logp=None), dict(draft_z=None, draft_logp=None), dict(drafts=0)):
+        d = _drafts(**kw)
+        n = lib.lbfgsb_verify_workspace_bytes(C.byref(d))
+        assert n > 0 and n % 256 == 0
+        assert _verify(d, n=n - 1) == _verify(d, ws=None) == _verify(d, ws=0x100010) == L.E_INVALID_ARG
+    assert _verify(_drafts(requests=0, z=None), tokens=None, count=None, logp=None) == L.OK
+    assert lib.lbfgsb_verify_workspace_bytes(None) == 0
+
+
+@pytest.mark.parametrize("call", [lambda t: L.draw_tokens(t, t[0]), lambda t: L.quantize4(t), lambda t: L.pack4(t.to(torch.uint8), t),
+                                  lambda t: L.matvec4(t, L.Weights4(t, 4, 4, 32, 1, False)),
+                                  lambda t: L.verify_draft(t[None], t[None, 0].long(), t, t[0])])
+def test_tensors_on_the_host_are_refused(call):
+    with pytest.raises(TypeError):
+        call(torch.zeros(4, 4))

@@ -14,7 +14,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblbfgsb.so")
 BINDING = os.path.join(HERE, "_losses.so")
 SOURCES = ["fused.hip", "narrow.hip", "small.hip", "symmetric.hip", "gram.hip", "api.hip", "apass.hip", "resident.hip", "transport.hip", "vec.hip",
-           "logits.hip", "logits_f32.hip", "logits_bf16.hip", "logits_f16.hip", "preference.hip", "losses_api.hip", "draws.hip", "weights4.hip", "rollouts_api.hip"]
+           "logits.hip", "logits_f32.hip", "logits_bf16.hip", "logits_f16.hip", "preference.hip", "losses_api.hip", "draws.hip", "weights4.hip", "matvec4_f32.hip", "matvec4_bf16.hip", "matvec4_f16.hip", "rollouts_api.hip"]
 BINDING_SOURCES = ["losses_binding.cpp", "rollouts_binding.cpp"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",

@@ -1,0 +1,391 @@
+// Products y = x W^T of a few rows x with weights of 4 bits.  Included once for each type of x.
+//
+// With w = scale (code - zero) a group's part of a product is scale (sum_j code_j x_j - zero sum_j x_j).  Codes are whole numbers of 4 bits, exact in
+// bf16 and f16, so the first sum is matrix instructions on the codes themselves, with exact products and sums in 32 bits; the second is formed once
+// for all rows of W, and scale and zero enter once a group.  x in 32 bits goes in as three bf16 parts, which hold its 24 bits.
+//
+// Bound by memory: half a byte and one or two instructions a weight.  A code becomes a matrix operand in 7/8 of an instruction: a byte
+// 0 .. 15 is, read as an 8-bit float with 3 bits of mantissa, that number times 2^-9 (denormal below 8, the first binade from there), so masking
+// the two halves of a word and four conversions of pairs with a scale of 2^9 make eight of them.
+#pragma once
+
+#include "weights4.h"
+
+namespace lb {
+
+namespace {
+
+typedef unsigned int u4 __attribute__((ext_vector_type(4)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+
+template <typename T>
+struct Operand;
+template <>
+struct Operand<__bf16> {
+    typedef __bf16 vec __attribute__((ext_vector_type(8)));
+    typedef __bf16 pair __attribute__((ext_vector_type(2)));
+    static __device__ __forceinline__ pair codes(unsigned v, bool high) {
+        return high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, 512.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, 512.0f, false);
+    }
+    static __device__ __forceinline__ f4 product(vec a, vec b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+template <>
+struct Operand<_Float16> {
+    typedef _Float16 vec __attribute__((ext_vector_type(8)));
+    typedef _Float16 pair __attribute__((ext_vector_type(2)));
+    static __device__ __forceinline__ pair codes(unsigned v, bool high) {
+        return high ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v, 512.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v, 512.0f, false);
+    }
+    static __device__ __forceinline__ f4 product(vec a, vec b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+};
+template <typename T>
+struct OperandOf { typedef T type; };
+template <>
+struct OperandOf<float> { typedef __bf16 type; };
+
+// eight codes as an operand, in the order of their columns
+template <typename M>
+__device__ __forceinline__ typename Operand<M>::vec unpacked(unsigned word) {
+    const unsigned low = word & 0x0f0f0f0fu, high = (word >> 4) & 0x0f0f0f0fu;
+    const auto a = Operand<M>::codes(low, false), b = Operand<M>::codes(low, true), c = Operand<M>::codes(high, false), d = Operand<M>::codes(high, true);
+    return {a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// Eight entries of x as operands: itself, or its bf16 parts.
+template <typename X>
+struct Parts {
+    static constexpr int N = 1;
+    typedef typename Operand<X>::vec vec;
+    vec p[1];
+    __device__ __forceinline__ void set(const X (&x)[8]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[0][e] = x[e];
+    }
+};
+template <>
+struct Parts<float> {
+    static constexpr int N = 3;
+    typedef Operand<__bf16>::vec vec;
+    vec p[3];
+    __device__ __forceinline__ void set(const float (&x)[8]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            // (each difference is exact; an infinite x leaves NaN behind it, and so does one that rounds to infinity)
+            const __bf16 a = (__bf16)x[e];
+            const float r = x[e] - (float)a;
+            const __bf16 b = (__bf16)r;
+            p[0][e] = a;
+            p[1][e] = b;
+            p[2][e] = (__bf16)(r - (float)b);
+        }
+    }
+};
+
+// a scale's value; half: 16 bits are an f16 and no bf16
+__device__ __forceinline__ float value_of(float s, bool) { return s; }
+__device__ __forceinline__ float value_of(uint16_t s, bool half) {
+    return half ? (float)__builtin_bit_cast(_Float16, s) : __builtin_bit_cast(float, (unsigned)s << 16);
+}
+// NT scales that stand side by side
+template <typename S, int NT>
+struct Scales {
+    typedef S vec __attribute__((ext_vector_type(NT)));
+};
+
+// What a launch is made of: waves of a workgroup that take rows beside each other, and waves that share their steps.
+struct Shape {
+    int row_waves, step_waves;
+    int chunk_log2;          // steps of x that are in LDS at a time: at least one for each of the waves that share them
+};
+// Pieces of x that a thread brings to LDS at a time: with one wave of rows for 16 rows of x, and four for more, that is enough for a step a wave.
+constexpr int row_waves_of(int T) { return T == 1 ? 1 : 4; }
+constexpr int pieces_of(int T) { return 4 * T / row_waves_of(T); }
+
+// (no wait for loads from memory, which stay on their way over it)
+__device__ __forceinline__ void barrier_for_lds() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// x of a few steps in LDS as operands: 16 bytes are eight columns of a row, and the four such of an instruction's depth stand together, then the rows,
+// then instructions and steps.  A 32-bit x is three planes of that.  A thread's pieces of the next chunk are on their way while this one is used.
+template <typename X, int P>
+struct Stage {
+    typedef typename OperandOf<X>::type M;
+    typedef typename Operand<M>::vec vec;
+    static constexpr int kPieces = P;           // of a thread
+    static constexpr int kParts = Parts<X>::N;
+    X piece[kPieces][8];
+    // The thread's index, to the compiler a new value each time: else it keeps the addresses of all pieces, and of their single entries, over
+    // the loop, some 100 registers.
+    __device__ __forceinline__ static int thread() {
+        int t = (int)threadIdx.x;
+        asm volatile("" : "+v"(t));
+        return t;
+    }
+    // pieces of a chunk: rows << (chunk_log2 + 4)
+    __device__ __forceinline__ static bool split(int tid, int k, int rows, int chunk_log2, int* row, int* step, int* j, int* kq) {
+        const int q = tid + k * (int)blockDim.x;
+        *kq = q & 3;
+        *j = (q >> 2) & 3;
+        *step = (q >> 4) & ((1 << chunk_log2) - 1);
+        *row = q >> (4 + chunk_log2);
+        return *row < rows;
+    }
+    __device__ __forceinline__ void load(const X* x, int64_t ld, int rows, int cols, int first, int chunk_log2) {
+        typedef X wide __attribute__((ext_vector_type(8), aligned(sizeof(X))));
+        const int tid = thread();
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) {
+            int row, step, j, kq;
+            const bool some = split(tid, k, rows, chunk_log2, &row, &step, &j, &kq);
+            const int col = (first + step) * kStepCols + 32 * j + 8 * kq;
+            const X* from = x + row * ld + col;
+            if (some && col + 8 <= cols) {
+                const wide v = *(const wide*)from;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) piece[k][e] = v[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) piece[k][e] = some && col + e < cols ? from[e] : (X)0.0f;
+            }
+        }
+    }
+    // and the sums of x over the groups, or the steps' parts of them: for each step, 4 / G times 16 T of them, in the order of the result registers
+    template <int G, int T>
+    __device__ __forceinline__ void store(vec* lds, float* totals, int rows, int chunk_log2) const {
+        const int tid = thread();
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) {
+            int row, step, j, kq;
+            if (!split(tid, k, rows, chunk_log2, &row, &step, &j, &kq)) continue;
+            Parts<X> p;
+            p.set(piece[k]);
+#pragma unroll
+            for (int n = 0; n < kParts; ++n) lds[(((((n << chunk_log2) + step) * 4 + j) * rows + row) << 2) + kq] = p.p[n];
+            float sum = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum += (float)piece[k][e];
+            sum += dpp_move_f<kDppXor1>(sum);
+            sum += dpp_move_f<kDppXor2>(sum);
+            if (G >= 2) sum += dpp_move_f<kDppHalfMirror>(sum);
+            if (G == 4) sum += dpp_move_f<kDppMirror>(sum);
+            if (kq == 0 && j % G == 0) totals[(step * (4 / G) + j / G) * (16 * T) + (row & ~15) + 4 * (row & 3) + ((row >> 2) & 3)] = sum;
+        }
+    }
+};
+
+// A wave's share of up to 16 T rows of x against NT tiles of a block.  The waves' sums are joined in LDS in a fixed order.
+// x's row i of 16 stands at row 4 (i % 4) + i / 4 of the operand, so that up to four rows take one of the four result registers; where there are
+// fewer rows the rest of the operand repeats the last, and what comes of it is not looked at.
+// S: what scales are held in, float or 16 bits.
+template <typename X, typename S, int G, int NT, int T>    // G: matrix instructions between two groups, 1, 2 or 4
+__global__ __launch_bounds__(512, T > 1 ? 2 : (sizeof(X) == 4 ? 3 : 4)) void k_matvec4(Matvec4Args a, Shape shape) {
+    extern __shared__ char shared[];
+    typedef typename OperandOf<X>::type M;
+    typedef typename Operand<M>::vec vec;
+    typedef typename Scales<S, NT>::vec SN;
+    constexpr int kRows = 16 * NT, kParts = Parts<X>::N;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int c = lane & 15, kq = lane >> 4;
+    const int row_wave = wave % shape.row_waves, waves = shape.step_waves, part = wave / shape.row_waves;
+    const int64_t units = a.w.blocks() * (4 / NT), first_unit = (int64_t)blockIdx.x * shape.row_waves;      // of NT tiles
+    const int64_t unit = first_unit + row_wave < units ? first_unit + row_wave : units - 1, block = unit / (4 / NT);
+    const int tile = (int)(unit % (4 / NT)) * NT;
+    const int64_t x0 = (int64_t)blockIdx.y * (16 * T);
+    const int have = (int)(a.tokens - x0 < 16 * T ? a.tokens - x0 : 16 * T);
+    const X* x = (const X*)a.x + x0 * a.ld_x;
+    const int steps = a.w.steps(), cols = a.w.cols, groups = a.w.groups(), chunk = 1 << shape.chunk_log2;
+    const char* codes = (const char*)a.packed + (size_t)block * steps * kStepBytes + tile * kTileBytes + lane * 16;
+    const S* scales = (const S*)((const char*)a.packed + a.w.code_bytes()) + (size_t)block * groups * kBlockRows * (1 + a.w.zeros) + 4 * c + tile;
+    const int each = kBlockRows * (1 + a.w.zeros);
+    const bool half_scales = a.w.scale_type == LBFGSB_F16;
+
+    f4 y[NT][T];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int u = 0; u < T; ++u) y[t][u] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+
+    struct Step {
+        u4 w[NT];
+        SN scale[4 / G], zero[4 / G];
+    };
+    auto load = [&](Step& st, int s) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) st.w[t] = __builtin_nontemporal_load((const u4*)(codes + (size_t)s * kStepBytes + t * kTileBytes));
+#pragma unroll
+        for (int g = 0; g < 4 / G; ++g) {
+            // (a last group may end before its step does; what comes after it is 0 times the scale of a group that is there)
+            const int at = min((s * kStepCols + g * G * 32) >> a.w.group_log2, groups - 1);
+            const S* from = scales + (size_t)at * each;
+            st.scale[g] = *(const SN*)from;
+            if (a.w.zeros) st.zero[g] = *(const SN*)(from + kBlockRows);
+        }
+    };
+    int row_at[T];
+#pragma unroll
+    for (int u = 0; u < T; ++u) row_at[u] = min(16 * u + 4 * (c & 3) + (c >> 2), have - 1) * 4 + kq;
+    auto multiply = [&](const Step& st, const vec* in, const f4* totals) {       // in: the step's operands
+        f4 sum[NT][T];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (j % G == 0) {
+#pragma unroll
+                for (int u = 0; u < T; ++u)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) sum[t][u] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+            }
+            // (or the compiler has the operands of all four at once, and spills)
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            vec w[NT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) w[t] = unpacked<M>(st.w[t][j]);
+#pragma unroll
+            for (int u = 0; u < T; ++u)
+#pragma unroll
+                for (int n = 0; n < kParts; ++n) {
+                    const vec v = in[(((n << shape.chunk_log2) * 4 + j) * have << 2) + row_at[u]];
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) sum[t][u] = Operand<M>::product(v, w[t], sum[t][u]);
+                }
+            if (j % G == G - 1) {
+                const int g = j / G;
+#pragma unroll
+                for (int u = 0; u < T; ++u) {
+                    const f4 all = totals[(g * T + u) * 4 + kq];
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const float scale = value_of(st.scale[g][t], half_scales), zero = a.w.zeros ? value_of(st.zero[g][t], half_scales) : 8.0f;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (T > 1 || r == 0 || have > 4) y[t][u][r] = fmaf(scale, fmaf(-zero, all[r], sum[t][u][r]), y[t][u][r]);
+                    }
+                }
+            }
+        }
+    };
+
+    // In turn i a wave takes step part + i * waves.  kDepth steps of codes are on their way at once; loads come back in order, so what is asked
+    // for last must be needed last, and no branch stands around those of the main loop, or all of them would be waited for behind it.
+    constexpr int kDepth = NT == 1 ? 4 : 2;
+    const int turns = (steps + waves - 1) / waves;
+    auto step_of = [&](int i) { return min(part + i * waves, steps - 1); };
+    Stage<X, pieces_of(T)> stage;
+    vec* lds = (vec*)shared;
+    const int operands = kParts * (have * 16 << shape.chunk_log2);  // of a chunk, in 16 bytes
+    const int room = operands + (16 / G * T << shape.chunk_log2);   // with the sums behind them
+    stage.load(x, a.ld_x, have, cols, 0, shape.chunk_log2);
+    Step at[kDepth];
+#pragma unroll
+    for (int d = 0; d < kDepth; ++d) load(at[d], step_of(d));
+    stage.template store<G, T>(lds, (float*)(lds + operands), have, shape.chunk_log2);
+    barrier_for_lds();
+    int chunk_at = 0, half = 0;                                     // first step of the chunk in LDS, and where it is
+    if (chunk < steps) stage.load(x, a.ld_x, have, cols, chunk, shape.chunk_log2);
+    auto turn = [&](int i, const Step& st) {
+        if (i * waves >= chunk_at + chunk) {                        // (all waves come to a chunk's end in the same turn: a chunk is a number of turns)
+            half ^= 1;
+            stage.template store<G, T>(lds + half * room, (float*)(lds + half * room + operands), have, shape.chunk_log2);
+            barrier_for_lds();
+            chunk_at += chunk;
+            if (chunk_at + chunk < steps) stage.load(x, a.ld_x, have, cols, chunk_at + chunk, shape.chunk_log2);
+        }
+        const int s = part + i * waves;
+        if (s < steps) multiply(st, lds + half * room + (s - chunk_at) * 16 * have, (const f4*)(lds + half * room + operands) + (s - chunk_at) * (16 / G * T));
+    };
+    int i = 0;
+    for (; i + 2 * kDepth <= turns; i += kDepth) {
+#pragma unroll
+        for (int d = 0; d < kDepth; ++d) {
+            turn(i + d, at[d]);
+            load(at[d], step_of(i + d + kDepth));
+        }
+    }
+    for (; i < turns; i += kDepth) {
+#pragma unroll
+        for (int d = 0; d < kDepth; ++d) {
+            if (i + d < turns) turn(i + d, at[d]);
+            if (i + d + kDepth < turns) load(at[d], step_of(i + d + kDepth));
+        }
+    }
+
+    // register r holds row 4 r + kq of 16
+    __syncthreads();
+    float* sums = (float*)shared;
+    const int all_rows = shape.row_waves * kRows;
+#pragma unroll
+    for (int u = 0; u < T; ++u)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = 16 * u + 4 * r + kq;
+            if (i < have) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t) sums[(part * have + i) * all_rows + row_wave * kRows + NT * c + t] = y[t][u][r];
+            }
+        }
+    __syncthreads();
+    for (int k = threadIdx.x; k < have * all_rows; k += blockDim.x) {
+        const int i = k / all_rows, o = k % all_rows;
+        const int64_t of = first_unit + o / kRows, row = of / (4 / NT) * kBlockRows + o % kRows / NT * 4 + of % (4 / NT) * NT + o % NT;
+        float sum = 0.0f;
+        for (int w = 0; w < waves; ++w) sum += sums[w * have * all_rows + k];
+        if (row < a.w.rows) {
+            const int64_t to = (x0 + i) * a.ld_y + row;
+            if (a.y_type == LBFGSB_F32) ((float*)a.y)[to] = sum;
+            else ((X*)a.y)[to] = (X)sum;
+        }
+    }
+}
+
+template <typename X, typename S, int G, int NT, int T>
+hipError_t matvec4_in(const Matvec4Args& a, int step_waves, hipStream_t st) {
+    constexpr int row_waves = row_waves_of(T);
+    const int64_t units = a.w.blocks() * (4 / NT), steps = a.w.steps();
+    const int have = a.tokens < 16 * T ? (int)a.tokens : 16 * T;
+    while (step_waves > steps) step_waves /= 2;
+    Shape shape{row_waves, step_waves, 0};
+    const int threads = row_waves * step_waves * 64;
+    // a chunk: whole turns of the waves, no more than the threads' pieces, and no more than there is
+    while ((1 << shape.chunk_log2) < step_waves) ++shape.chunk_log2;
+    while ((2 << shape.chunk_log2) * 16 * have <= pieces_of(T) * threads && (1 << shape.chunk_log2) < steps) ++shape.chunk_log2;
+    const size_t chunk_bytes = (size_t)(Parts<X>::N * have * 256 + 256 / G * T) << shape.chunk_log2, sums = (size_t)step_waves * have * row_waves * 16 * NT * 4;
+    const size_t x_bytes = (1 << shape.chunk_log2) < steps ? 2 * chunk_bytes : chunk_bytes;
+    const int64_t pass = 16 * T * 32768;
+    for (int64_t x0 = 0; x0 < a.tokens; x0 += pass) {
+        Matvec4Args p = a;
+        p.x = (const char*)a.x + x0 * a.ld_x * sizeof(X);
+        p.y = (char*)a.y + x0 * a.ld_y * (a.y_type == LBFGSB_F32 ? 4 : sizeof(X));
+        p.tokens = a.tokens - x0 < pass ? a.tokens - x0 : pass;
+        hipLaunchKernelGGL((k_matvec4<X, S, G, NT, T>), dim3((unsigned)((units + row_waves - 1) / row_waves), (unsigned)((p.tokens + 16 * T - 1) / (16 * T))),
+                           dim3(threads), x_bytes > sums ? x_bytes : sums, st, p, shape);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+template <typename X, typename S, int G>
+hipError_t matvec4(const Matvec4Args& a, hipStream_t st) {
+    const bool wide = a.w.blocks() >= 256;
+    if (a.tokens <= 16) return wide ? matvec4_in<X, S, G, G == 1 ? 2 : 4, 1>(a, 4, st) : matvec4_in<X, S, G, 1, 1>(a, 8, st);
+    if (a.tokens <= 32 || sizeof(X) == 4) return wide ? matvec4_in<X, S, G, G == 1 ? 2 : 4, 2>(a, 2, st) : matvec4_in<X, S, G, 1, 2>(a, 2, st);
+    if constexpr (sizeof(X) == 2) return wide ? matvec4_in<X, S, G, G == 4 ? 4 : 2, 4>(a, 2, st) : matvec4_in<X, S, G, 1, 4>(a, 2, st);
+    return hipErrorInvalidValue;
+}
+
+template <typename X, typename S>
+hipError_t matvec4_by_group(const Matvec4Args& a, hipStream_t st) {
+    return a.w.group_log2 == 5 ? matvec4<X, S, 1>(a, st) : (a.w.group_log2 == 6 ? matvec4<X, S, 2>(a, st) : matvec4<X, S, 4>(a, st));
+}
+
+}  // namespace
+
+template <typename X>
+hipError_t matvec4_of(const Matvec4Args& a, hipStream_t st) {
+    return a.w.scale_type == LBFGSB_F32 ? matvec4_by_group<X, float>(a, st) : matvec4_by_group<X, uint16_t>(a, st);
+}
+
+}  // namespace lb

@@ -1,0 +1,8 @@
+// Products of rows of type _Float16 with 4-bit weights.
+#include "matvec4.h"
+
+namespace lb {
+
+template hipError_t matvec4_of<_Float16>(const Matvec4Args&, hipStream_t);
+
+}  // namespace lb

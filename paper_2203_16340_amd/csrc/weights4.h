@@ -36,5 +36,8 @@ hipError_t launch_quantize4(int dtype, int64_t ld, const void* w, int64_t rows, 
                             void* zero, hipStream_t st);
 hipError_t launch_pack4(const Packed4& w, const uint8_t* codes, const void* scale, const void* zero, void* packed, hipStream_t st);
 hipError_t launch_matvec4(const Matvec4Args& a, int x_type, hipStream_t st);
+// the same for one type of x, tokens > 0 (matvec4.h)
+template <typename X>
+hipError_t matvec4_of(const Matvec4Args& a, hipStream_t st);
 
 }  // namespace lb

@@ -32,7 +32,7 @@ EXPORTS = [
     "lbfgsb_logits_workspace_bytes", "lbfgsb_token_logprob", "lbfgsb_token_logprob_grad", "lbfgsb_token_logprob_stats",
     "lbfgsb_token_logprob_stats_grad", "lbfgsb_distill_loss", "lbfgsb_policy_loss",
     "lbfgsb_preference_loss",
-    "lbfgsb_quantize4", "lbfgsb_packed4_bytes", "lbfgsb_pack4", "lbfgsb_matvec4", "lbfgsb_draw_workspace_bytes", "lbfgsb_draw_tokens",
+    "lbfgsb_quantize4", "lbfgsb_packed4_bytes", "lbfgsb_pack4", "lbfgsb_matvec4_workspace_bytes", "lbfgsb_matvec4", "lbfgsb_draw_workspace_bytes", "lbfgsb_draw_tokens",
     "lbfgsb_verify_workspace_bytes", "lbfgsb_verify_draft",
 ]
 

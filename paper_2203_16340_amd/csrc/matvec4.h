@@ -9,6 +9,8 @@
 // the two halves of a word and four conversions of pairs with a scale of 2^9 make eight of them.
 #pragma once
 
+#include <type_traits>
+
 #include "weights4.h"
 
 namespace lb {
@@ -97,9 +99,16 @@ struct Shape {
     int row_waves, step_waves;
     int chunk_log2;          // steps of x that are in LDS at a time: at least one for each of the waves that share them
 };
-// Pieces of x that a thread brings to LDS at a time: with one wave of rows for 16 rows of x, and four for more, that is enough for a step a wave.
 constexpr int row_waves_of(int T) { return T == 1 ? 1 : 4; }
-constexpr int pieces_of(int T) { return 4 * T / row_waves_of(T); }
+
+// x as operands, step by step, in units of 16 bytes (eight columns of a row): for each of a step's four instructions its four such, and for each of those the
+// rows one behind the other, so that 16 lanes read 256 bytes.  A 32-bit x is three planes of that.  Behind a step's operands (more than 16 rows) stand the
+// sums of x over its groups, or over its part of one: 4 / G times 16 T floats, in the order of the result registers.
+template <typename X>
+__host__ __device__ constexpr int operand_units(int rows) { return Parts<X>::N * 16 * rows; }
+template <typename X>
+__host__ __device__ constexpr int step_units(int G, int T, int rows) { return operand_units<X>(rows) + (T == 1 ? 0 : 16 / G * T); }
+__device__ __forceinline__ int unit_at(int part, int j, int kq, int rows, int row) { return ((part * 4 + j) * 4 + kq) * rows + row; }
 
 // (no wait for loads from memory, which stay on their way over it)
 __device__ __forceinline__ void barrier_for_lds() {
@@ -107,24 +116,35 @@ __device__ __forceinline__ void barrier_for_lds() {
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
+// The thread's index, to the compiler a new value each time: else it keeps the addresses of all that a thread brings to LDS, single entries too,
+// over the loop, some 100 registers.
+__device__ __forceinline__ int fresh_thread() {
+    int t = (int)threadIdx.x;
+    asm volatile("" : "+v"(t));
+    return t;
+}
 
-// x of a few steps in LDS as operands: 16 bytes are eight columns of a row, and the four such of an instruction's depth stand together, then the rows,
-// then instructions and steps.  A 32-bit x is three planes of that.  A thread's pieces of the next chunk are on their way while this one is used.
-template <typename X, int P>
-struct Stage {
-    typedef typename OperandOf<X>::type M;
-    typedef typename Operand<M>::vec vec;
-    static constexpr int kPieces = P;           // of a thread
-    static constexpr int kParts = Parts<X>::N;
-    X piece[kPieces][8];
-    // The thread's index, to the compiler a new value each time: else it keeps the addresses of all pieces, and of their single entries, over
-    // the loop, some 100 registers.
-    __device__ __forceinline__ static int thread() {
-        int t = (int)threadIdx.x;
-        asm volatile("" : "+v"(t));
-        return t;
+// eight entries of a row from column col on, 0 past its end
+template <typename X>
+__device__ __forceinline__ void eight(const X* row, int col, int cols, bool some, X (&v)[8]) {
+    typedef X wide __attribute__((ext_vector_type(8), aligned(sizeof(X))));
+    if (some && col + 8 <= cols) {
+        const wide w = *(const wide*)(row + col);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = w[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = some && col + e < cols ? row[col + e] : (X)0.0f;
     }
-    // pieces of a chunk: rows << (chunk_log2 + 4)
+}
+
+// What brings x to LDS, a few steps at a time; a thread's pieces of the next are on their way while these are used.
+// Up to 16 rows: from x itself.
+template <typename X, int G, int T>
+struct Stage {
+    typedef typename Operand<typename OperandOf<X>::type>::vec vec;
+    static constexpr int kPieces = 4;           // of a thread: enough for a step a wave
+    X piece[kPieces][8];
     __device__ __forceinline__ static bool split(int tid, int k, int rows, int chunk_log2, int* row, int* step, int* j, int* kq) {
         const int q = tid + k * (int)blockDim.x;
         *kq = q & 3;
@@ -133,29 +153,17 @@ struct Stage {
         *row = q >> (4 + chunk_log2);
         return *row < rows;
     }
-    __device__ __forceinline__ void load(const X* x, int64_t ld, int rows, int cols, int first, int chunk_log2) {
-        typedef X wide __attribute__((ext_vector_type(8), aligned(sizeof(X))));
-        const int tid = thread();
+    __device__ __forceinline__ void load(const Matvec4Args& a, int64_t x0, int rows, int first, int chunk_log2) {
+        const int tid = fresh_thread();
 #pragma unroll
         for (int k = 0; k < kPieces; ++k) {
             int row, step, j, kq;
             const bool some = split(tid, k, rows, chunk_log2, &row, &step, &j, &kq);
-            const int col = (first + step) * kStepCols + 32 * j + 8 * kq;
-            const X* from = x + row * ld + col;
-            if (some && col + 8 <= cols) {
-                const wide v = *(const wide*)from;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) piece[k][e] = v[e];
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) piece[k][e] = some && col + e < cols ? from[e] : (X)0.0f;
-            }
+            eight((const X*)a.x + (x0 + row) * a.ld_x, (first + step) * kStepCols + 32 * j + 8 * kq, a.w.cols, some, piece[k]);
         }
     }
-    // and the sums of x over the groups, or the steps' parts of them: for each step, 4 / G times 16 T of them, in the order of the result registers
-    template <int G, int T>
-    __device__ __forceinline__ void store(vec* lds, float* totals, int rows, int chunk_log2) const {
-        const int tid = thread();
+    __device__ __forceinline__ void store(vec* lds, int rows, int chunk_log2) const {
+        const int tid = fresh_thread();
 #pragma unroll
         for (int k = 0; k < kPieces; ++k) {
             int row, step, j, kq;
@@ -163,18 +171,59 @@ struct Stage {
             Parts<X> p;
             p.set(piece[k]);
 #pragma unroll
-            for (int n = 0; n < kParts; ++n) lds[(((((n << chunk_log2) + step) * 4 + j) * rows + row) << 2) + kq] = p.p[n];
-            float sum = 0.0f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum += (float)piece[k][e];
-            sum += dpp_move_f<kDppXor1>(sum);
-            sum += dpp_move_f<kDppXor2>(sum);
-            if (G >= 2) sum += dpp_move_f<kDppHalfMirror>(sum);
-            if (G == 4) sum += dpp_move_f<kDppMirror>(sum);
-            if (kq == 0 && j % G == 0) totals[(step * (4 / G) + j / G) * (16 * T) + (row & ~15) + 4 * (row & 3) + ((row >> 2) & 3)] = sum;
+            for (int n = 0; n < Parts<X>::N; ++n) lds[step * step_units<X>(G, T, rows) + unit_at(n, j, kq, rows, row)] = p.p[n];
         }
     }
+    static bool fits(int chunk, int rows, int threads) { return chunk * 16 * rows <= kPieces * threads; }
 };
+// More rows: as k_operands4 laid them out, since every workgroup would do as much for them as for its products (65536 x 4096 with 48 rows: 83 us).
+template <typename X, int G, int T>
+struct LaidOut {
+    typedef typename Operand<typename OperandOf<X>::type>::vec vec;
+    static constexpr int kPieces = (step_units<X>(G, T, 16 * T) + 64 * row_waves_of(T) - 1) / (64 * row_waves_of(T));
+    vec piece[kPieces];
+    __device__ __forceinline__ void load(const Matvec4Args& a, int64_t x0, int rows, int first, int chunk_log2) {
+        const int units = step_units<X>(G, T, rows), steps = a.w.steps();
+        const vec* from = (const vec*)a.operands + x0 / (16 * T) * steps * step_units<X>(G, T, 16 * T) + (size_t)first * units;
+        const int most = min(1 << chunk_log2, steps - first) * units - 1, tid = fresh_thread();
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) piece[k] = from[min(tid + k * (int)blockDim.x, most)];
+    }
+    __device__ __forceinline__ void store(vec* lds, int rows, int chunk_log2) const {
+        const int all = step_units<X>(G, T, rows) << chunk_log2, tid = fresh_thread();
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k)
+            if (tid + k * (int)blockDim.x < all) lds[tid + k * (int)blockDim.x] = piece[k];
+    }
+    static bool fits(int chunk, int rows, int threads) { return chunk * step_units<X>(G, T, rows) <= kPieces * threads; }
+};
+
+// A thread for eight entries of x.
+template <typename X, int G, int T>
+__global__ __launch_bounds__(256) void k_operands4(Matvec4Args a) {
+    typedef typename Operand<typename OperandOf<X>::type>::vec vec;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, at = i >> 4;
+    const int steps = a.w.steps(), kq = (int)i & 3, j = (int)(i >> 2) & 3;
+    const int64_t token = at / steps, pass = token / (16 * T);
+    if (token >= a.tokens) return;              // (16 lanes at a time: they share a row's step)
+    const int step = (int)(at - token * steps), row = (int)(token - pass * (16 * T));
+    const int rows = (int)min(a.tokens - pass * (16 * T), (int64_t)(16 * T));
+    X v[8];
+    eight((const X*)a.x + token * a.ld_x, step * kStepCols + 32 * j + 8 * kq, a.w.cols, true, v);
+    vec* to = (vec*)a.operands + pass * steps * step_units<X>(G, T, 16 * T) + (size_t)step * step_units<X>(G, T, rows);
+    Parts<X> p;
+    p.set(v);
+#pragma unroll
+    for (int n = 0; n < Parts<X>::N; ++n) to[unit_at(n, j, kq, rows, row)] = p.p[n];
+    float sum = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum += (float)v[e];
+    sum += dpp_move_f<kDppXor1>(sum);
+    sum += dpp_move_f<kDppXor2>(sum);
+    if (G >= 2) sum += dpp_move_f<kDppHalfMirror>(sum);
+    if (G == 4) sum += dpp_move_f<kDppMirror>(sum);
+    if (kq == 0 && j % G == 0) ((float*)(to + operand_units<X>(rows)))[j / G * (16 * T) + (row & ~15) + 4 * (row & 3) + ((row >> 2) & 3)] = sum;
+}
 
 // A wave's share of up to 16 T rows of x against NT tiles of a block.  The waves' sums are joined in LDS in a fixed order.
 // x's row i of 16 stands at row 4 (i % 4) + i / 4 of the operand, so that up to four rows take one of the four result registers; where there are
@@ -195,8 +244,7 @@ __global__ __launch_bounds__(512, T > 1 ? 2 : (sizeof(X) == 4 ? 3 : 4)) void k_m
     const int tile = (int)(unit % (4 / NT)) * NT;
     const int64_t x0 = (int64_t)blockIdx.y * (16 * T);
     const int have = (int)(a.tokens - x0 < 16 * T ? a.tokens - x0 : 16 * T);
-    const X* x = (const X*)a.x + x0 * a.ld_x;
-    const int steps = a.w.steps(), cols = a.w.cols, groups = a.w.groups(), chunk = 1 << shape.chunk_log2;
+    const int steps = a.w.steps(), groups = a.w.groups(), chunk = 1 << shape.chunk_log2;
     const char* codes = (const char*)a.packed + (size_t)block * steps * kStepBytes + tile * kTileBytes + lane * 16;
     const S* scales = (const S*)((const char*)a.packed + a.w.code_bytes()) + (size_t)block * groups * kBlockRows * (1 + a.w.zeros) + 4 * c + tile;
     const int each = kBlockRows * (1 + a.w.zeros);
@@ -226,9 +274,14 @@ __global__ __launch_bounds__(512, T > 1 ? 2 : (sizeof(X) == 4 ? 3 : 4)) void k_m
     };
     int row_at[T];
 #pragma unroll
-    for (int u = 0; u < T; ++u) row_at[u] = min(16 * u + 4 * (c & 3) + (c >> 2), have - 1) * 4 + kq;
-    auto multiply = [&](const Step& st, const vec* in, const f4* totals) {       // in: the step's operands
-        f4 sum[NT][T];
+    for (int u = 0; u < T; ++u) row_at[u] = kq * have + min(16 * u + 4 * (c & 3) + (c >> 2), have - 1);
+    vec ones;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ones[e] = (M)1.0f;
+    auto multiply = [&](const Step& st, const vec* in) {            // in: the step's operands
+        const f4* totals = (const f4*)(in + operand_units<X>(have));
+        f4 sum[NT][T], all1;
+        (void)totals;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             if (j % G == 0) {
@@ -236,6 +289,7 @@ __global__ __launch_bounds__(512, T > 1 ? 2 : (sizeof(X) == 4 ? 3 : 4)) void k_m
                 for (int u = 0; u < T; ++u)
 #pragma unroll
                     for (int t = 0; t < NT; ++t) sum[t][u] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+                all1 = f4{0.0f, 0.0f, 0.0f, 0.0f};
             }
             // (or the compiler has the operands of all four at once, and spills)
             asm volatile("" ::: "memory");
@@ -247,7 +301,9 @@ __global__ __launch_bounds__(512, T > 1 ? 2 : (sizeof(X) == 4 ? 3 : 4)) void k_m
             for (int u = 0; u < T; ++u)
 #pragma unroll
                 for (int n = 0; n < kParts; ++n) {
-                    const vec v = in[(((n << shape.chunk_log2) * 4 + j) * have << 2) + row_at[u]];
+                    const vec v = in[(n * 4 + j) * 4 * have + row_at[u]];
+                    // (up to 16 rows the matrix unit has time for their sums as well)
+                    if (T == 1) all1 = Operand<M>::product(v, ones, all1);
 #pragma unroll
                     for (int t = 0; t < NT; ++t) sum[t][u] = Operand<M>::product(v, w[t], sum[t][u]);
                 }
@@ -255,7 +311,7 @@ __global__ __launch_bounds__(512, T > 1 ? 2 : (sizeof(X) == 4 ? 3 : 4)) void k_m
                 const int g = j / G;
 #pragma unroll
                 for (int u = 0; u < T; ++u) {
-                    const f4 all = totals[(g * T + u) * 4 + kq];
+                    const f4 all = T == 1 ? all1 : totals[(g * T + u) * 4 + kq];
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
                         const float scale = value_of(st.scale[g][t], half_scales), zero = a.w.zeros ? value_of(st.zero[g][t], half_scales) : 8.0f;
@@ -273,28 +329,27 @@ __global__ __launch_bounds__(512, T > 1 ? 2 : (sizeof(X) == 4 ? 3 : 4)) void k_m
     constexpr int kDepth = NT == 1 ? 4 : 2;
     const int turns = (steps + waves - 1) / waves;
     auto step_of = [&](int i) { return min(part + i * waves, steps - 1); };
-    Stage<X, pieces_of(T)> stage;
+    typename std::conditional<T == 1, Stage<X, G, T>, LaidOut<X, G, T>>::type stage;
     vec* lds = (vec*)shared;
-    const int operands = kParts * (have * 16 << shape.chunk_log2);  // of a chunk, in 16 bytes
-    const int room = operands + (16 / G * T << shape.chunk_log2);   // with the sums behind them
-    stage.load(x, a.ld_x, have, cols, 0, shape.chunk_log2);
+    const int per_step = step_units<X>(G, T, have), room = per_step << shape.chunk_log2;
+    stage.load(a, x0, have, 0, shape.chunk_log2);
     Step at[kDepth];
 #pragma unroll
     for (int d = 0; d < kDepth; ++d) load(at[d], step_of(d));
-    stage.template store<G, T>(lds, (float*)(lds + operands), have, shape.chunk_log2);
+    stage.store(lds, have, shape.chunk_log2);
     barrier_for_lds();
     int chunk_at = 0, half = 0;                                     // first step of the chunk in LDS, and where it is
-    if (chunk < steps) stage.load(x, a.ld_x, have, cols, chunk, shape.chunk_log2);
+    if (chunk < steps) stage.load(a, x0, have, chunk, shape.chunk_log2);
     auto turn = [&](int i, const Step& st) {
         if (i * waves >= chunk_at + chunk) {                        // (all waves come to a chunk's end in the same turn: a chunk is a number of turns)
             half ^= 1;
-            stage.template store<G, T>(lds + half * room, (float*)(lds + half * room + operands), have, shape.chunk_log2);
+            stage.store(lds + half * room, have, shape.chunk_log2);
             barrier_for_lds();
             chunk_at += chunk;
-            if (chunk_at + chunk < steps) stage.load(x, a.ld_x, have, cols, chunk_at + chunk, shape.chunk_log2);
+            if (chunk_at + chunk < steps) stage.load(a, x0, have, chunk_at + chunk, shape.chunk_log2);
         }
         const int s = part + i * waves;
-        if (s < steps) multiply(st, lds + half * room + (s - chunk_at) * 16 * have, (const f4*)(lds + half * room + operands) + (s - chunk_at) * (16 / G * T));
+        if (s < steps) multiply(st, lds + half * room + (s - chunk_at) * per_step);
     };
     int i = 0;
     for (; i + 2 * kDepth <= turns; i += kDepth) {
@@ -349,16 +404,23 @@ hipError_t matvec4_in(const Matvec4Args& a, int step_waves, hipStream_t st) {
     Shape shape{row_waves, step_waves, 0};
     const int threads = row_waves * step_waves * 64;
     // a chunk: whole turns of the waves, no more than the threads' pieces, and no more than there is
+    typedef typename std::conditional<T == 1, Stage<X, G, T>, LaidOut<X, G, T>>::type Bring;
     while ((1 << shape.chunk_log2) < step_waves) ++shape.chunk_log2;
-    while ((2 << shape.chunk_log2) * 16 * have <= pieces_of(T) * threads && (1 << shape.chunk_log2) < steps) ++shape.chunk_log2;
-    const size_t chunk_bytes = (size_t)(Parts<X>::N * have * 256 + 256 / G * T) << shape.chunk_log2, sums = (size_t)step_waves * have * row_waves * 16 * NT * 4;
+    while (Bring::fits(2 << shape.chunk_log2, have, threads) && (1 << shape.chunk_log2) < steps) ++shape.chunk_log2;
+    const size_t chunk_bytes = (size_t)step_units<X>(G, T, have) * 16 << shape.chunk_log2, sums = (size_t)step_waves * have * row_waves * 16 * NT * 4;
     const size_t x_bytes = (1 << shape.chunk_log2) < steps ? 2 * chunk_bytes : chunk_bytes;
-    const int64_t pass = 16 * T * 32768;
+    // (a launch takes 65535 workgroups the second way and fewer than 2^32 threads)
+    const int64_t tiles = (1 << 27) / (steps * 16 * T), pass = 16 * T * (tiles < 1 ? 1 : (tiles < 32768 ? tiles : 32768));
     for (int64_t x0 = 0; x0 < a.tokens; x0 += pass) {
         Matvec4Args p = a;
         p.x = (const char*)a.x + x0 * a.ld_x * sizeof(X);
         p.y = (char*)a.y + x0 * a.ld_y * (a.y_type == LBFGSB_F32 ? 4 : sizeof(X));
         p.tokens = a.tokens - x0 < pass ? a.tokens - x0 : pass;
+        if (T > 1) {
+            p.operands = (char*)a.operands + (size_t)(x0 / (16 * T)) * steps * step_units<X>(G, T, 16 * T) * 16;
+            const int64_t blocks = (p.tokens * steps * 16 + 255) / 256;
+            hipLaunchKernelGGL((k_operands4<X, G, T>), dim3((unsigned)blocks), dim3(256), 0, st, p);
+        }
         hipLaunchKernelGGL((k_matvec4<X, S, G, NT, T>), dim3((unsigned)((units + row_waves - 1) / row_waves), (unsigned)((p.tokens + 16 * T - 1) / (16 * T))),
                            dim3(threads), x_bytes > sums ? x_bytes : sums, st, p, shape);
         const hipError_t e = hipGetLastError();
@@ -370,18 +432,26 @@ hipError_t matvec4_in(const Matvec4Args& a, int step_waves, hipStream_t st) {
 template <typename X, typename S, int G>
 hipError_t matvec4(const Matvec4Args& a, hipStream_t st) {
     const bool wide = a.w.blocks() >= 256;
-    if (a.tokens <= 16) return wide ? matvec4_in<X, S, G, G == 1 ? 2 : 4, 1>(a, 4, st) : matvec4_in<X, S, G, 1, 1>(a, 8, st);
-    if (a.tokens <= 32 || sizeof(X) == 4) return wide ? matvec4_in<X, S, G, G == 1 ? 2 : 4, 2>(a, 2, st) : matvec4_in<X, S, G, 1, 2>(a, 2, st);
+    const int T = tiles_of(a.tokens, sizeof(X));
+    if (T == 1) return wide ? matvec4_in<X, S, G, G == 1 ? 2 : 4, 1>(a, 4, st) : matvec4_in<X, S, G, 1, 1>(a, 8, st);
+    if (T == 2) return wide ? matvec4_in<X, S, G, G == 1 ? 2 : 4, 2>(a, 2, st) : matvec4_in<X, S, G, 1, 2>(a, 2, st);
     if constexpr (sizeof(X) == 2) return wide ? matvec4_in<X, S, G, G == 4 ? 4 : 2, 4>(a, 2, st) : matvec4_in<X, S, G, 1, 4>(a, 2, st);
     return hipErrorInvalidValue;
 }
 
 template <typename X, typename S>
 hipError_t matvec4_by_group(const Matvec4Args& a, hipStream_t st) {
-    return a.w.group_log2 == 5 ? matvec4<X, S, 1>(a, st) : (a.w.group_log2 == 6 ? matvec4<X, S, 2>(a, st) : matvec4<X, S, 4>(a, st));
+    const int g = depth_of(a.w.group_log2);
+    return g == 1 ? matvec4<X, S, 1>(a, st) : (g == 2 ? matvec4<X, S, 2>(a, st) : matvec4<X, S, 4>(a, st));
 }
 
 }  // namespace
+
+template <typename X>
+size_t matvec4_space(const Packed4& w, int64_t tokens) {
+    const int T = tiles_of(tokens, sizeof(X));
+    return T == 1 ? 0 : (size_t)((tokens + 16 * T - 1) / (16 * T)) * w.steps() * step_units<X>(depth_of(w.group_log2), T, 16 * T) * 16;
+}
 
 template <typename X>
 hipError_t matvec4_of(const Matvec4Args& a, hipStream_t st) {

@@ -4,5 +4,6 @@
 namespace lb {
 
 template hipError_t matvec4_of<__bf16>(const Matvec4Args&, hipStream_t);
+template size_t matvec4_space<__bf16>(const Packed4&, int64_t);
 
 }  // namespace lb

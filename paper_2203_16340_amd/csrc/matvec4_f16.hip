@@ -4,5 +4,6 @@
 namespace lb {
 
 template hipError_t matvec4_of<_Float16>(const Matvec4Args&, hipStream_t);
+template size_t matvec4_space<_Float16>(const Packed4&, int64_t);
 
 }  // namespace lb

@@ -4,5 +4,6 @@
 namespace lb {
 
 template hipError_t matvec4_of<float>(const Matvec4Args&, hipStream_t);
+template size_t matvec4_space<float>(const Packed4&, int64_t);
 
 }  // namespace lb

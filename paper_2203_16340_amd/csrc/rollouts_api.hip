@@ -87,8 +87,13 @@ int lbfgsb_pack4(const lbfgsb_weights4* weights_host, void* packed, size_t packe
     return LBFGSB_OK;
 }
 
+size_t lbfgsb_matvec4_workspace_bytes(const lbfgsb_weights4* weights_host, int64_t tokens, int x_type) {
+    if (check_weights(weights_host) || tokens < 1 || tokens > kMaxRows || !is_logit_type(x_type)) return 0;
+    return matvec4_bytes(packed_of(weights_host), tokens, x_type);
+}
+
 int lbfgsb_matvec4(const lbfgsb_weights4* weights_host, const void* packed, int64_t tokens, int x_type, int64_t ld_x, const void* x, int y_type,
-                   int64_t ld_y, void* y, void* hip_stream) {
+                   int64_t ld_y, void* y, void* workspace, size_t workspace_bytes, void* hip_stream) {
     if (int rc = check_weights(weights_host)) return rc;
     const lbfgsb_weights4* w = weights_host;
     if (tokens < 0 || tokens > kMaxRows) return fail(LBFGSB_E_INVALID_ARG, "tokens must be in 0..2^31-1 (got %lld)", (long long)tokens);
@@ -102,8 +107,9 @@ int lbfgsb_matvec4(const lbfgsb_weights4* weights_host, const void* packed, int6
         return fail(LBFGSB_E_INVALID_ARG, "x or y is NULL or not aligned to its elements");
     const Packed4 p = packed_of(w);
     const size_t nx = ((tokens - 1) * ld_x + w->cols) * size_of(x_type), ny = ((tokens - 1) * ld_y + w->rows) * size_of(y_type);
+    if (int rc = check_space(matvec4_bytes(p, tokens, x_type), workspace, workspace_bytes)) return rc;
     if (overlap(x, nx, y, ny) || overlap(packed, p.bytes(), y, ny)) return fail(LBFGSB_E_INVALID_ARG, "y overlaps x or packed");
-    HIP_TRY(launch_matvec4({p, packed, tokens, ld_x, ld_y, x, y, y_type}, x_type, (hipStream_t)hip_stream));
+    HIP_TRY(launch_matvec4({p, packed, tokens, ld_x, ld_y, x, y, y_type, workspace}, x_type, (hipStream_t)hip_stream));
     return LBFGSB_OK;
 }
 

@@ -80,8 +80,9 @@ auto matvec4(const Tensor& x, const Tensor& packed, int64_t rows, int64_t cols, 
         if (type != x.scalar_type() && type != at::kFloat) throw py::type_error("dtype must be that of x or float32");
         y = at::empty({x.size(0), rows}, x.options().dtype(type));
     }
+    Tensor ws = workspace(lbfgsb_matvec4_workspace_bytes(&w, x.size(0), x_type), dev);
     const int rc = lbfgsb_matvec4(&w, packed.data_ptr(), x.size(0), x_type, row_stride(x), x.data_ptr(), type_code(y.scalar_type()), row_stride(y), y.data_ptr(),
-                                  (void*)stream);
+                                  address(ws), bytes(ws), (void*)stream);
     if (rc == LBFGSB_OK && out) written(y);
     return std::make_tuple(rc, y);
 }

@@ -30,14 +30,23 @@ struct Matvec4Args {
     const void* x;
     void* y;
     int y_type;
+    void* operands;              // workspace: x as operands (more than 16 tokens)
 };
+
+// tiles of 16 rows of x that are multiplied in one pass over the weights
+inline int tiles_of(int64_t tokens, size_t size_x) { return tokens <= 16 ? 1 : (tokens <= 32 || size_x == 4 ? 2 : 4); }
+// matrix instructions between two groups
+inline int depth_of(int group_log2) { return group_log2 == 5 ? 1 : (group_log2 == 6 ? 2 : 4); }
 
 hipError_t launch_quantize4(int dtype, int64_t ld, const void* w, int64_t rows, int64_t cols, int64_t group, int scale_type, uint8_t* codes, void* scale,
                             void* zero, hipStream_t st);
 hipError_t launch_pack4(const Packed4& w, const uint8_t* codes, const void* scale, const void* zero, void* packed, hipStream_t st);
 hipError_t launch_matvec4(const Matvec4Args& a, int x_type, hipStream_t st);
+size_t matvec4_bytes(const Packed4& w, int64_t tokens, int x_type);     // of workspace
 // the same for one type of x, tokens > 0 (matvec4.h)
 template <typename X>
 hipError_t matvec4_of(const Matvec4Args& a, hipStream_t st);
+template <typename X>
+size_t matvec4_space(const Packed4& w, int64_t tokens);
 
 }  // namespace lb

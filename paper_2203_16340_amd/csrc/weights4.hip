@@ -121,6 +121,12 @@ hipError_t launch_pack4(const Packed4& w, const uint8_t* codes, const void* scal
     return hipGetLastError();
 }
 
+size_t matvec4_bytes(const Packed4& w, int64_t tokens, int x_type) {
+    size_t n = 0;
+    by_type(x_type, [&](auto x) { return n = matvec4_space<decltype(x)>(w, tokens), hipSuccess; });
+    return (n + 255) & ~(size_t)255;
+}
+
 hipError_t launch_matvec4(const Matvec4Args& a, int x_type, hipStream_t st) {
     if (a.tokens == 0) return hipSuccess;
     return by_type(x_type, [&](auto x) { return matvec4_of<decltype(x)>(a, st); });

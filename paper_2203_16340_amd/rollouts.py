@@ -33,8 +33,9 @@ def declare(L) -> None:
     for name, arg in (("packed4_bytes", w), ("draw_workspace_bytes", lg), ("verify_workspace_bytes", d)):
         f = getattr(L, "lbfgsb_" + name)
         f.restype, f.argtypes = size, [arg]
+    L.lbfgsb_matvec4_workspace_bytes.restype, L.lbfgsb_matvec4_workspace_bytes.argtypes = size, [w, i64, num]
     for name, args in (("quantize4", [num, i64, vp, w, vp]), ("pack4", [w, vp, size, vp]),
-                       ("matvec4", [w, vp, i64, num, i64, vp, num, i64, vp, vp]),
+                       ("matvec4", [w, vp, i64, num, i64, vp, num, i64, vp, vp, size, vp]),
                        ("draw_tokens", [lg, vp, vp, vp, vp, size, vp]), ("verify_draft", [d, vp, vp, vp, vp, size, vp])):
         f = getattr(L, "lbfgsb_" + name)
         f.restype, f.argtypes = num, args

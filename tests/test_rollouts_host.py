@@ -41,7 +41,8 @@ def test_weights_are_checked(bad):
     assert lib.lbfgsb_packed4_bytes(b) == 0
     assert lib.lbfgsb_quantize4(1, 1 << 25, 0x9000, b, None) == L.E_INVALID_ARG
     assert lib.lbfgsb_pack4(b, 0x10000, 1 << 40, None) == L.E_INVALID_ARG
-    assert lib.lbfgsb_matvec4(b, 0x10000, 1, 1, 70, 0x9000, 1, 100, 0x900000, None) == L.E_INVALID_ARG
+    assert lib.lbfgsb_matvec4(b, 0x10000, 1, 1, 70, 0x9000, 1, 100, 0x900000, 0x1000000, 1 << 40, None) == L.E_INVALID_ARG
+    assert lib.lbfgsb_matvec4_workspace_bytes(b, 100, 1) == 0
     assert lib.lbfgsb_last_error()
 
 
@@ -70,14 +71,21 @@ def test_quantising_and_packing_are_checked():
 def test_products_are_checked():
     lib, w = L.lib(), _weights()
 
-    def call(tokens=2, x_type=1, ld_x=70, x=0x100000, y_type=1, ld_y=100, y=0x200000, packed=0x10000, weights=C.byref(w)):
-        return lib.lbfgsb_matvec4(weights, packed, tokens, x_type, ld_x, x, y_type, ld_y, y, None)
+    def call(tokens=2, x_type=1, ld_x=70, x=0x100000, y_type=1, ld_y=100, y=0x200000, packed=0x10000, weights=C.byref(w), ws=0x1000000,
+             n=1 << 40):
+        return lib.lbfgsb_matvec4(weights, packed, tokens, x_type, ld_x, x, y_type, ld_y, y, ws, n, None)
 
     for kw in (dict(tokens=-1), dict(tokens=1 << 31), dict(x_type=0), dict(y_type=2), dict(x_type=2, y_type=3), dict(ld_x=69), dict(ld_y=99),
                dict(x=None), dict(y=None), dict(x=0x100002), dict(y=0x200001), dict(packed=None), dict(packed=0x10004), dict(weights=None),
                dict(y=0x100000), dict(y=0x100000 - 400), dict(y=0x10000 + 8192)):
         assert call(**kw) == L.E_INVALID_ARG, kw
     assert call(tokens=0, x=None, y=None, packed=None) == L.OK
+    assert lib.lbfgsb_matvec4_workspace_bytes(C.byref(w), 16, 1) == 0
+    for tokens, x_type in ((17, 1), (64, 2), (1000, 3)):
+        need = lib.lbfgsb_matvec4_workspace_bytes(C.byref(w), tokens, x_type)
+        assert need >= tokens * 70 * 2 and need % 256 == 0
+        for kw in (dict(n=need - 1), dict(ws=None), dict(ws=0x1000010)):
+            assert call(tokens=tokens, x_type=x_type, y_type=1, **kw) == L.E_INVALID_ARG
 
 
 def test_draws_are_checked():

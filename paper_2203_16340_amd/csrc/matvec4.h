@@ -9,8 +9,6 @@
 // the two halves of a word and four conversions of pairs with a scale of 2^9 make eight of them.
 #pragma once
 
-#include <type_traits>
-
 #include "weights4.h"
 
 namespace lb {
@@ -83,11 +81,6 @@ struct Parts<float> {
     }
 };
 
-// a scale's value; half: 16 bits are an f16 and no bf16
-__device__ __forceinline__ float value_of(float s, bool) { return s; }
-__device__ __forceinline__ float value_of(uint16_t s, bool half) {
-    return half ? (float)__builtin_bit_cast(_Float16, s) : __builtin_bit_cast(float, (unsigned)s << 16);
-}
 // NT scales that stand side by side
 template <typename S, int NT>
 struct Scales {
@@ -102,12 +95,13 @@ struct Shape {
 constexpr int row_waves_of(int T) { return T == 1 ? 1 : 4; }
 
 // x as operands, step by step, in units of 16 bytes (eight columns of a row): for each of a step's four instructions its four such, and for each of those the
-// rows one behind the other, so that 16 lanes read 256 bytes.  A 32-bit x is three planes of that.  Behind a step's operands (more than 16 rows) stand the
-// sums of x over its groups, or over its part of one: 4 / G times 16 T floats, in the order of the result registers.
+// rows one behind the other, so that 16 lanes read 256 bytes.  A 32-bit x is three planes of that.  Where x is laid out beforehand the rows are filled up to
+// 16 T, and behind a step's operands stand the sums of x over its groups, or over its part of one: 4 / G times 16 T floats, in the order of the
+// result registers.
 template <typename X>
 __host__ __device__ constexpr int operand_units(int rows) { return Parts<X>::N * 16 * rows; }
 template <typename X>
-__host__ __device__ constexpr int step_units(int G, int T, int rows) { return operand_units<X>(rows) + (T == 1 ? 0 : 16 / G * T); }
+__host__ __device__ constexpr int step_units(int G, int T) { return operand_units<X>(16 * T) + 16 / G * T; }
 __device__ __forceinline__ int unit_at(int part, int j, int kq, int rows, int row) { return ((part * 4 + j) * 4 + kq) * rows + row; }
 
 // (no wait for loads from memory, which stay on their way over it)
@@ -138,64 +132,56 @@ __device__ __forceinline__ void eight(const X* row, int col, int cols, bool some
     }
 }
 
-// What brings x to LDS, a few steps at a time; a thread's pieces of the next are on their way while these are used.
-// Up to 16 rows: from x itself.
-template <typename X, int G, int T>
-struct Stage {
-    typedef typename Operand<typename OperandOf<X>::type>::vec vec;
-    static constexpr int kPieces = 4;           // of a thread: enough for a step a wave
-    X piece[kPieces][8];
-    __device__ __forceinline__ static bool split(int tid, int k, int rows, int chunk_log2, int* row, int* step, int* j, int* kq) {
-        const int q = tid + k * (int)blockDim.x;
-        *kq = q & 3;
-        *j = (q >> 2) & 3;
-        *step = (q >> 4) & ((1 << chunk_log2) - 1);
-        *row = q >> (4 + chunk_log2);
-        return *row < rows;
-    }
-    __device__ __forceinline__ void load(const Matvec4Args& a, int64_t x0, int rows, int first, int chunk_log2) {
-        const int tid = fresh_thread();
+// All of x's (up to 16) rows to LDS, by a whole workgroup: four units of a thread on their way at once.
+template <typename X>
+__device__ __forceinline__ void bring_whole(const Matvec4Args& a, int64_t x0, int rows, typename Operand<typename OperandOf<X>::type>::vec* lds) {
+    const int tid = threadIdx.x, kq = tid & 3, j = (tid >> 2) & 3, steps = a.w.steps(), stride = (int)blockDim.x >> 4, units = operand_units<X>(rows);
+    int row = (tid >> 4) < steps ? 0 : rows, step = tid >> 4;
+    while (row < rows) {
+        X v[4][8];
+        int to[4];
 #pragma unroll
-        for (int k = 0; k < kPieces; ++k) {
-            int row, step, j, kq;
-            const bool some = split(tid, k, rows, chunk_log2, &row, &step, &j, &kq);
-            eight((const X*)a.x + (x0 + row) * a.ld_x, (first + step) * kStepCols + 32 * j + 8 * kq, a.w.cols, some, piece[k]);
+        for (int k = 0; k < 4; ++k) {
+            const bool some = row < rows;
+            to[k] = some ? step * units + unit_at(0, j, kq, rows, row) : -1;
+            eight((const X*)a.x + (x0 + (some ? row : 0)) * a.ld_x, step * kStepCols + 32 * j + 8 * kq, a.w.cols, some, v[k]);
+            step += stride;
+            if (step >= steps) {
+                step = tid >> 4;
+                ++row;
+            }
         }
-    }
-    __device__ __forceinline__ void store(vec* lds, int rows, int chunk_log2) const {
-        const int tid = fresh_thread();
 #pragma unroll
-        for (int k = 0; k < kPieces; ++k) {
-            int row, step, j, kq;
-            if (!split(tid, k, rows, chunk_log2, &row, &step, &j, &kq)) continue;
+        for (int k = 0; k < 4; ++k) {
+            if (to[k] < 0) continue;
             Parts<X> p;
-            p.set(piece[k]);
+            p.set(v[k]);
 #pragma unroll
-            for (int n = 0; n < Parts<X>::N; ++n) lds[step * step_units<X>(G, T, rows) + unit_at(n, j, kq, rows, row)] = p.p[n];
+            for (int n = 0; n < Parts<X>::N; ++n) lds[to[k] + n * 16 * rows] = p.p[n];
         }
     }
-    static bool fits(int chunk, int rows, int threads) { return chunk * 16 * rows <= kPieces * threads; }
-};
-// More rows: as k_operands4 laid them out, since every workgroup would do as much for them as for its products (65536 x 4096 with 48 rows: 83 us).
+}
+
+// What brings x, laid out by k_operands4, to LDS a few steps at a time; a thread's units of the next are on their way while these are used.
+// (Laid out by every workgroup for itself, 65536 x 4096 with 48 rows took 83 us: more instructions than the products.)
 template <typename X, int G, int T>
 struct LaidOut {
     typedef typename Operand<typename OperandOf<X>::type>::vec vec;
-    static constexpr int kPieces = (step_units<X>(G, T, 16 * T) + 64 * row_waves_of(T) - 1) / (64 * row_waves_of(T));
+    static constexpr int kUnits = step_units<X>(G, T), kPieces = (kUnits + 64 * row_waves_of(T) - 1) / (64 * row_waves_of(T));   // (a step a wave)
     vec piece[kPieces];
-    __device__ __forceinline__ void load(const Matvec4Args& a, int64_t x0, int rows, int first, int chunk_log2) {
-        const int units = step_units<X>(G, T, rows), steps = a.w.steps();
-        const vec* from = (const vec*)a.operands + x0 / (16 * T) * steps * step_units<X>(G, T, 16 * T) + (size_t)first * units;
-        const int most = min(1 << chunk_log2, steps - first) * units - 1, tid = fresh_thread();
+    __device__ __forceinline__ void load(const Matvec4Args& a, int64_t x0, int first, int chunk_log2) {
+        const int steps = a.w.steps();
+        const vec* from = (const vec*)a.operands + (x0 / (16 * T) * steps + first) * kUnits;
+        const int most = min(1 << chunk_log2, steps - first) * kUnits - 1, tid = fresh_thread();
 #pragma unroll
         for (int k = 0; k < kPieces; ++k) piece[k] = from[min(tid + k * (int)blockDim.x, most)];
     }
-    __device__ __forceinline__ void store(vec* lds, int rows, int chunk_log2) const {
-        const int all = step_units<X>(G, T, rows) << chunk_log2, tid = fresh_thread();
+    __device__ __forceinline__ void store(vec* lds, int chunk_log2) const {
+        const int all = kUnits << chunk_log2, tid = fresh_thread();
 #pragma unroll
         for (int k = 0; k < kPieces; ++k)
             if (tid + k * (int)blockDim.x < all) lds[tid + k * (int)blockDim.x] = piece[k];
     }
-    static bool fits(int chunk, int rows, int threads) { return chunk * step_units<X>(G, T, rows) <= kPieces * threads; }
 };
 
 // A thread for eight entries of x.
@@ -207,14 +193,13 @@ __global__ __launch_bounds__(256) void k_operands4(Matvec4Args a) {
     const int64_t token = at / steps, pass = token / (16 * T);
     if (token >= a.tokens) return;              // (16 lanes at a time: they share a row's step)
     const int step = (int)(at - token * steps), row = (int)(token - pass * (16 * T));
-    const int rows = (int)min(a.tokens - pass * (16 * T), (int64_t)(16 * T));
     X v[8];
     eight((const X*)a.x + token * a.ld_x, step * kStepCols + 32 * j + 8 * kq, a.w.cols, true, v);
-    vec* to = (vec*)a.operands + pass * steps * step_units<X>(G, T, 16 * T) + (size_t)step * step_units<X>(G, T, rows);
+    vec* to = (vec*)a.operands + (pass * steps + step) * step_units<X>(G, T);
     Parts<X> p;
     p.set(v);
 #pragma unroll
-    for (int n = 0; n < Parts<X>::N; ++n) to[unit_at(n, j, kq, rows, row)] = p.p[n];
+    for (int n = 0; n < Parts<X>::N; ++n) to[unit_at(n, j, kq, 16 * T, row)] = p.p[n];
     float sum = 0.0f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum += (float)v[e];
@@ -222,15 +207,15 @@ __global__ __launch_bounds__(256) void k_operands4(Matvec4Args a) {
     sum += dpp_move_f<kDppXor2>(sum);
     if (G >= 2) sum += dpp_move_f<kDppHalfMirror>(sum);
     if (G == 4) sum += dpp_move_f<kDppMirror>(sum);
-    if (kq == 0 && j % G == 0) ((float*)(to + operand_units<X>(rows)))[j / G * (16 * T) + (row & ~15) + 4 * (row & 3) + ((row >> 2) & 3)] = sum;
+    if (kq == 0 && j % G == 0) ((float*)(to + operand_units<X>(16 * T)))[j / G * (16 * T) + (row & ~15) + 4 * (row & 3) + ((row >> 2) & 3)] = sum;
 }
 
 // A wave's share of up to 16 T rows of x against NT tiles of a block.  The waves' sums are joined in LDS in a fixed order.
 // x's row i of 16 stands at row 4 (i % 4) + i / 4 of the operand, so that up to four rows take one of the four result registers; where there are
-// fewer rows the rest of the operand repeats the last, and what comes of it is not looked at.
-// S: what scales are held in, float or 16 bits.
-template <typename X, typename S, int G, int NT, int T>    // G: matrix instructions between two groups, 1, 2 or 4
-__global__ __launch_bounds__(512, T > 1 ? 2 : (sizeof(X) == 4 ? 3 : 4)) void k_matvec4(Matvec4Args a, Shape shape) {
+// fewer rows the rest of the operand is anything, and what comes of it is not looked at.
+// S: the scales' type.  WHOLE: all of x is in LDS from the start, and x has up to 16 rows.
+template <typename X, typename S, int G, int NT, int T, bool WHOLE>    // G: matrix instructions between two groups, 1, 2 or 4
+__global__ __launch_bounds__(512, T > 1 || (!WHOLE && sizeof(X) == 4) ? 2 : (WHOLE && (G != 2 || sizeof(S) + sizeof(X) < 6) ? 4 : 3)) void k_matvec4(Matvec4Args a, Shape shape) {
     extern __shared__ char shared[];
     typedef typename OperandOf<X>::type M;
     typedef typename Operand<M>::vec vec;
@@ -248,7 +233,6 @@ __global__ __launch_bounds__(512, T > 1 ? 2 : (sizeof(X) == 4 ? 3 : 4)) void k_m
     const char* codes = (const char*)a.packed + (size_t)block * steps * kStepBytes + tile * kTileBytes + lane * 16;
     const S* scales = (const S*)((const char*)a.packed + a.w.code_bytes()) + (size_t)block * groups * kBlockRows * (1 + a.w.zeros) + 4 * c + tile;
     const int each = kBlockRows * (1 + a.w.zeros);
-    const bool half_scales = a.w.scale_type == LBFGSB_F16;
 
     f4 y[NT][T];
 #pragma unroll
@@ -274,12 +258,13 @@ __global__ __launch_bounds__(512, T > 1 ? 2 : (sizeof(X) == 4 ? 3 : 4)) void k_m
     };
     int row_at[T];
 #pragma unroll
-    for (int u = 0; u < T; ++u) row_at[u] = kq * have + min(16 * u + 4 * (c & 3) + (c >> 2), have - 1);
+    for (int u = 0; u < T; ++u) row_at[u] = WHOLE ? kq * have + min(4 * (c & 3) + (c >> 2), have - 1) : kq * 16 * T + 16 * u + 4 * (c & 3) + (c >> 2);
     vec ones;
 #pragma unroll
     for (int e = 0; e < 8; ++e) ones[e] = (M)1.0f;
     auto multiply = [&](const Step& st, const vec* in) {            // in: the step's operands
-        const f4* totals = (const f4*)(in + operand_units<X>(have));
+        const int rows = WHOLE ? have : 16 * T;
+        const f4* totals = (const f4*)(in + operand_units<X>(16 * T));
         f4 sum[NT][T], all1;
         (void)totals;
 #pragma unroll
@@ -301,9 +286,9 @@ __global__ __launch_bounds__(512, T > 1 ? 2 : (sizeof(X) == 4 ? 3 : 4)) void k_m
             for (int u = 0; u < T; ++u)
 #pragma unroll
                 for (int n = 0; n < kParts; ++n) {
-                    const vec v = in[(n * 4 + j) * 4 * have + row_at[u]];
-                    // (up to 16 rows the matrix unit has time for their sums as well)
-                    if (T == 1) all1 = Operand<M>::product(v, ones, all1);
+                    const vec v = in[(n * 4 + j) * 4 * rows + row_at[u]];
+                    // (the matrix unit has time for their sums as well)
+                    if (WHOLE) all1 = Operand<M>::product(v, ones, all1);
 #pragma unroll
                     for (int t = 0; t < NT; ++t) sum[t][u] = Operand<M>::product(v, w[t], sum[t][u]);
                 }
@@ -311,10 +296,10 @@ __global__ __launch_bounds__(512, T > 1 ? 2 : (sizeof(X) == 4 ? 3 : 4)) void k_m
                 const int g = j / G;
 #pragma unroll
                 for (int u = 0; u < T; ++u) {
-                    const f4 all = T == 1 ? all1 : totals[(g * T + u) * 4 + kq];
+                    const f4 all = WHOLE ? all1 : totals[(g * T + u) * 4 + kq];
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
-                        const float scale = value_of(st.scale[g][t], half_scales), zero = a.w.zeros ? value_of(st.zero[g][t], half_scales) : 8.0f;
+                        const float scale = (float)st.scale[g][t], zero = a.w.zeros ? (float)st.zero[g][t] : 8.0f;
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
                             if (T > 1 || r == 0 || have > 4) y[t][u][r] = fmaf(scale, fmaf(-zero, all[r], sum[t][u][r]), y[t][u][r]);
@@ -329,24 +314,25 @@ __global__ __launch_bounds__(512, T > 1 ? 2 : (sizeof(X) == 4 ? 3 : 4)) void k_m
     constexpr int kDepth = NT == 1 ? 4 : 2;
     const int turns = (steps + waves - 1) / waves;
     auto step_of = [&](int i) { return min(part + i * waves, steps - 1); };
-    typename std::conditional<T == 1, Stage<X, G, T>, LaidOut<X, G, T>>::type stage;
+    LaidOut<X, G, T> stage;
     vec* lds = (vec*)shared;
-    const int per_step = step_units<X>(G, T, have), room = per_step << shape.chunk_log2;
-    stage.load(a, x0, have, 0, shape.chunk_log2);
+    const int per_step = WHOLE ? operand_units<X>(have) : step_units<X>(G, T), room = per_step << shape.chunk_log2;
+    if (!WHOLE) stage.load(a, x0, 0, shape.chunk_log2);
     Step at[kDepth];
 #pragma unroll
     for (int d = 0; d < kDepth; ++d) load(at[d], step_of(d));
-    stage.store(lds, have, shape.chunk_log2);
+    if (WHOLE) bring_whole<X>(a, x0, have, lds);
+    else stage.store(lds, shape.chunk_log2);
     barrier_for_lds();
     int chunk_at = 0, half = 0;                                     // first step of the chunk in LDS, and where it is
-    if (chunk < steps) stage.load(a, x0, have, chunk, shape.chunk_log2);
+    if (!WHOLE && chunk < steps) stage.load(a, x0, chunk, shape.chunk_log2);
     auto turn = [&](int i, const Step& st) {
-        if (i * waves >= chunk_at + chunk) {                        // (all waves come to a chunk's end in the same turn: a chunk is a number of turns)
+        if (!WHOLE && i * waves >= chunk_at + chunk) {              // (all waves come to a chunk's end in the same turn: a chunk is a number of turns)
             half ^= 1;
-            stage.store(lds + half * room, have, shape.chunk_log2);
+            stage.store(lds + half * room, shape.chunk_log2);
             barrier_for_lds();
             chunk_at += chunk;
-            if (chunk_at + chunk < steps) stage.load(a, x0, have, chunk_at + chunk, shape.chunk_log2);
+            if (chunk_at + chunk < steps) stage.load(a, x0, chunk_at + chunk, shape.chunk_log2);
         }
         const int s = part + i * waves;
         if (s < steps) multiply(st, lds + half * room + (s - chunk_at) * per_step);
@@ -395,7 +381,7 @@ __global__ __launch_bounds__(512, T > 1 ? 2 : (sizeof(X) == 4 ? 3 : 4)) void k_m
     }
 }
 
-template <typename X, typename S, int G, int NT, int T>
+template <typename X, typename S, int G, int NT, int T, bool WHOLE>
 hipError_t matvec4_in(const Matvec4Args& a, int step_waves, hipStream_t st) {
     constexpr int row_waves = row_waves_of(T);
     const int64_t units = a.w.blocks() * (4 / NT), steps = a.w.steps();
@@ -403,12 +389,10 @@ hipError_t matvec4_in(const Matvec4Args& a, int step_waves, hipStream_t st) {
     while (step_waves > steps) step_waves /= 2;
     Shape shape{row_waves, step_waves, 0};
     const int threads = row_waves * step_waves * 64;
-    // a chunk: whole turns of the waves, no more than the threads' pieces, and no more than there is
-    typedef typename std::conditional<T == 1, Stage<X, G, T>, LaidOut<X, G, T>>::type Bring;
     while ((1 << shape.chunk_log2) < step_waves) ++shape.chunk_log2;
-    while (Bring::fits(2 << shape.chunk_log2, have, threads) && (1 << shape.chunk_log2) < steps) ++shape.chunk_log2;
-    const size_t chunk_bytes = (size_t)step_units<X>(G, T, have) * 16 << shape.chunk_log2, sums = (size_t)step_waves * have * row_waves * 16 * NT * 4;
-    const size_t x_bytes = (1 << shape.chunk_log2) < steps ? 2 * chunk_bytes : chunk_bytes;
+    const size_t sums = (size_t)step_waves * have * row_waves * 16 * NT * 4;
+    const size_t x_bytes = WHOLE ? (size_t)steps * operand_units<X>(have) * 16
+                                 : ((size_t)step_units<X>(G, T) * 16 << shape.chunk_log2) * ((1 << shape.chunk_log2) < steps ? 2 : 1);
     // (a launch takes 65535 workgroups the second way and fewer than 2^32 threads)
     const int64_t tiles = (1 << 27) / (steps * 16 * T), pass = 16 * T * (tiles < 1 ? 1 : (tiles < 32768 ? tiles : 32768));
     for (int64_t x0 = 0; x0 < a.tokens; x0 += pass) {
@@ -416,12 +400,12 @@ hipError_t matvec4_in(const Matvec4Args& a, int step_waves, hipStream_t st) {
         p.x = (const char*)a.x + x0 * a.ld_x * sizeof(X);
         p.y = (char*)a.y + x0 * a.ld_y * (a.y_type == LBFGSB_F32 ? 4 : sizeof(X));
         p.tokens = a.tokens - x0 < pass ? a.tokens - x0 : pass;
-        if (T > 1) {
-            p.operands = (char*)a.operands + (size_t)(x0 / (16 * T)) * steps * step_units<X>(G, T, 16 * T) * 16;
+        if (!WHOLE) {
+            p.operands = (char*)a.operands + (size_t)(x0 / (16 * T)) * steps * step_units<X>(G, T) * 16;
             const int64_t blocks = (p.tokens * steps * 16 + 255) / 256;
             hipLaunchKernelGGL((k_operands4<X, G, T>), dim3((unsigned)blocks), dim3(256), 0, st, p);
         }
-        hipLaunchKernelGGL((k_matvec4<X, S, G, NT, T>), dim3((unsigned)((units + row_waves - 1) / row_waves), (unsigned)((p.tokens + 16 * T - 1) / (16 * T))),
+        hipLaunchKernelGGL((k_matvec4<X, S, G, NT, T, WHOLE>), dim3((unsigned)((units + row_waves - 1) / row_waves), (unsigned)((p.tokens + 16 * T - 1) / (16 * T))),
                            dim3(threads), x_bytes > sums ? x_bytes : sums, st, p, shape);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
@@ -429,13 +413,22 @@ hipError_t matvec4_in(const Matvec4Args& a, int step_waves, hipStream_t st) {
     return hipSuccess;
 }
 
+// Up to 16 rows of x are in LDS as a whole where they are no larger than this: two workgroups to a compute unit.
+constexpr int64_t kWholeBytes = 80 << 10;
+template <typename X>
+int64_t whole_bytes(const Packed4& w, int64_t tokens) { return tokens * w.steps() * operand_units<X>(1) * 16; }
+
 template <typename X, typename S, int G>
 hipError_t matvec4(const Matvec4Args& a, hipStream_t st) {
     const bool wide = a.w.blocks() >= 256;
     const int T = tiles_of(a.tokens, sizeof(X));
-    if (T == 1) return wide ? matvec4_in<X, S, G, G == 1 ? 2 : 4, 1>(a, 4, st) : matvec4_in<X, S, G, 1, 1>(a, 8, st);
-    if (T == 2) return wide ? matvec4_in<X, S, G, G == 1 ? 2 : 4, 2>(a, 2, st) : matvec4_in<X, S, G, 1, 2>(a, 2, st);
-    if constexpr (sizeof(X) == 2) return wide ? matvec4_in<X, S, G, G == 4 ? 4 : 2, 4>(a, 2, st) : matvec4_in<X, S, G, 1, 4>(a, 2, st);
+    const int64_t whole = T == 1 ? whole_bytes<X>(a.w, a.tokens) : 0;
+    if (T == 1 && whole <= kWholeBytes)
+        return wide ? matvec4_in<X, S, G, G == 1 ? 2 : 4, 1, true>(a, whole <= kWholeBytes / 2 ? 4 : 8, st) : matvec4_in<X, S, G, 1, 1, true>(a, 8, st);
+    if (T == 1) return wide ? matvec4_in<X, S, G, G == 1 ? 2 : 4, 1, false>(a, 4, st) : matvec4_in<X, S, G, 1, 1, false>(a, 8, st);
+    if (T == 2) return wide ? matvec4_in<X, S, G, G == 1 ? 2 : 4, 2, false>(a, 2, st) : matvec4_in<X, S, G, 1, 2, false>(a, 2, st);
+    if constexpr (sizeof(X) == 2)
+        return wide ? matvec4_in<X, S, G, G == 4 ? 4 : 2, 4, false>(a, 2, st) : matvec4_in<X, S, G, 1, 4, false>(a, 2, st);
     return hipErrorInvalidValue;
 }
 
@@ -450,12 +443,14 @@ hipError_t matvec4_by_group(const Matvec4Args& a, hipStream_t st) {
 template <typename X>
 size_t matvec4_space(const Packed4& w, int64_t tokens) {
     const int T = tiles_of(tokens, sizeof(X));
-    return T == 1 ? 0 : (size_t)((tokens + 16 * T - 1) / (16 * T)) * w.steps() * step_units<X>(depth_of(w.group_log2), T, 16 * T) * 16;
+    if (T == 1 && whole_bytes<X>(w, tokens) <= kWholeBytes) return 0;
+    return (size_t)((tokens + 16 * T - 1) / (16 * T)) * w.steps() * step_units<X>(depth_of(w.group_log2), T) * 16;
 }
 
 template <typename X>
 hipError_t matvec4_of(const Matvec4Args& a, hipStream_t st) {
-    return a.w.scale_type == LBFGSB_F32 ? matvec4_by_group<X, float>(a, st) : matvec4_by_group<X, uint16_t>(a, st);
+    return a.w.scale_type == LBFGSB_F32 ? matvec4_by_group<X, float>(a, st)
+                                        : (a.w.scale_type == LBFGSB_BF16 ? matvec4_by_group<X, __bf16>(a, st) : matvec4_by_group<X, _Float16>(a, st));
 }
 
 }  // namespace lb

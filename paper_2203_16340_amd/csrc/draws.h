@@ -8,9 +8,9 @@ namespace lb {
 constexpr int64_t kMaxDrawVocab = 1 << 21;
 constexpr int64_t kMaxDrafts = 128;
 
-// A row's entries are summed in blocks of this many bytes, a wave's two loads, which begin on 16-byte boundaries of the logits.
+// A row's entries are summed in blocks of this many bytes, a wave's four loads, which begin on 16-byte boundaries of the logits.
 // What is kept of a block, sum_j 2^((z_j - ref) c), tells where in the row a running sum is passed; the one block is then read again.
-constexpr int kBlockBytes = 2048;
+constexpr int kBlockBytes = 4096;
 struct BlockSum {
     float ref, sum;
 };
@@ -61,7 +61,7 @@ enum { kFromTarget = 0, kWithout = 1, kRest = 2 };
 
 // where the parts of a call's workspace are, in bytes (draws.hip); whole: how much there is of it
 struct VerifySpace {
-    size_t target, draft, rest, decision, whole;
+    size_t target, draft, rest, tickets, whole;
 };
 VerifySpace verify_space(int64_t requests, int64_t drafts, int64_t vocab, int size, bool draft_rows, bool draft_sums);
 size_t draw_space(int64_t rows, int64_t vocab, int size);

@@ -48,22 +48,22 @@ struct VerifyArgs {
     float* logp;
 };
 
-// What is drawn from at the end of a request, and where.
-struct Decision {
-    int t;                   // position; -1: the request has ended
-    int mode;                // kFromTarget ..
-    int x;                   // kWithout: the token that is left out
-    float m;                 // kRest: p_j = 2^((z_j - m) c) inv
-    float inv;
-    float q_ref, q_factor;   //        q_j = 2^((zq_j - q_ref) cq) q_factor
+// What is drawn from where a position's token is not accepted.
+enum { kFromTarget = 0, kWithout = 1, kRest = 2 };     // p; p without the token; max(p - q, 0)
+struct Position {
+    double sum;              // p_j = 2^((z_j - top) c) / sum
+    float top;
+    float q_ref, q_factor;   // q_j = 2^((zq_j - q_ref) cq) q_factor
+    int accepted, mode, x;   // x: the drafted token
+    float logp;              // its log-probability
 };
-enum { kFromTarget = 0, kWithout = 1, kRest = 2 };
 
-// where the parts of a call's workspace are, in bytes (draws.hip); whole: how much there is of it
+// where the parts of a call's workspace are, in bytes behind the blocks' sums of the target's rows (draws.hip); whole: how much there is of it
 struct VerifySpace {
-    size_t target, draft, rest, tickets, whole;
+    size_t draft, rest, tickets, whole;
 };
-VerifySpace verify_space(int64_t requests, int64_t drafts, int64_t vocab, int size, bool draft_rows, bool draft_sums);
+// drafter: its rows are there; both: they are summed as well
+VerifySpace verify_space(int64_t requests, int64_t drafts, int64_t vocab, int size, bool drafter, bool both);
 size_t draw_space(int64_t rows, int64_t vocab, int size);
 
 hipError_t launch_draw(const DrawArgs& a, int dtype, void* ws, hipStream_t st);

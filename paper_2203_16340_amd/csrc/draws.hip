@@ -5,9 +5,8 @@
 // passed, S being the whole row's, and that block alone is read again, lane by lane and entry by entry.  Sums of a block are in 32 bits and off by
 // 2^-24 of the block's own, all else is in 64 bits.
 //
-// Verification: sums of all the target's rows (and of the drafter's, where its log-probabilities are not at hand) in one launch; the first
-// token that is not accepted follows from them; in a second, workgroups sum blocks of max(p - q, 0) at it, and the last of a request's to be done
-// finds the token.
+// Verification: the same sums tell whether a drafted token is accepted; where the first is not, blocks of max(p - q, 0) are summed and walked through
+// alike.  A workgroup takes a request, position by position; few requests are taken in two launches, sums of all rows and then the rest, by many.
 #include "draws.h"
 
 namespace lb {
@@ -29,7 +28,7 @@ __device__ __forceinline__ float share_exact(float z, float ref, Factor c) {
 // A row as it is read in blocks: chunks of 16 bytes on boundaries of the logits, of which the first and the last may hold less of the row.
 template <typename T>
 struct Line {
-    static constexpr int E = Chunk<T>::E, kPer = kBlockBytes / 16, kLoads = kPer / 64, kEntries = kLoads * E;    // chunks of a block; a lane's
+    static constexpr int E = Chunk<T>::E, kPer = kBlockBytes / 16, kLoads = kPer / 64;      // chunks of a block, and of a lane's
     typedef typename Chunk<T>::vec vec;
     const T* row;
     int vocab, shift;        // shift: entries of the first chunk that come before the row
@@ -42,26 +41,23 @@ struct Line {
     __device__ __forceinline__ int blocks() const { return (vocab + shift + kPer * E - 1) / (kPer * E); }
     __device__ __forceinline__ int first(int chunk) const { return chunk * E - shift; }
     __device__ __forceinline__ int block_of(int entry) const { return (entry + shift) / (kPer * E); }
-    // the lane's chunk k of block b: SPREAD, 64 lanes beside each other; else the lane's four are beside each other
-    template <bool SPREAD>
-    static __device__ __forceinline__ int chunk(int b, int k, int lane) { return b * kPer + (SPREAD ? k * 64 + lane : lane * kLoads + k); }
+    // the lane's chunk k of block b
+    static __device__ __forceinline__ int chunk(int b, int k, int lane) { return b * kPer + k * 64 + lane; }
     // The lane's chunks of block b.  A chunk that is not whole in the row is asked for as the nearest whole one, and mended below: no
     // branch stands around the loads.
-    template <bool SPREAD>
     __device__ __forceinline__ void fetch(int b, int lane, vec (&v)[kLoads]) const {
         if (high < low) return;
 #pragma unroll
         for (int k = 0; k < kLoads; ++k) {
-            const int i = min(max(chunk<SPREAD>(b, k, lane), low), high);
+            const int i = min(max(chunk(b, k, lane), low), high);
             v[k] = *(const vec*)(row + first(i));
         }
     }
-    template <bool SPREAD>
     __device__ __forceinline__ void mend(int b, int lane, vec (&v)[kLoads]) const {
         if (b * kPer >= low && (b + 1) * kPer - 1 <= high) return;
 #pragma unroll
         for (int k = 0; k < kLoads; ++k) {
-            const int i = chunk<SPREAD>(b, k, lane);
+            const int i = chunk(b, k, lane);
             if (i >= low && i <= high) continue;
 #pragma unroll
             for (int e = 0; e < E; ++e) {
@@ -90,13 +86,13 @@ __device__ __forceinline__ void sum_blocks(const Line<T>& line, float c, int fir
     if (first >= end) return;
     float ref = -INFINITY, at = 0.0f;                // at: what differences are taken from (anchor(ref))
     vec next[kLoads];
-    line.template fetch<true>(first, lane, next);
+    line.fetch(first, lane, next);
     for (int b = first; b < end; b += step) {
         vec v[kLoads];
 #pragma unroll
         for (int k = 0; k < kLoads; ++k) v[k] = next[k];
-        if (b + step < end) line.template fetch<true>(b + step, lane, next);
-        line.template mend<true>(b, lane, v);
+        if (b + step < end) line.fetch(b + step, lane, next);
+        line.mend(b, lane, v);
         float sum = 0.0f;
 #pragma unroll
         for (int k = 0; k < kLoads; ++k) {
@@ -200,27 +196,59 @@ __device__ __forceinline__ Place find_block(int blocks, double u, At at) {
     return {__builtin_amdgcn_readlane(found, who), fmax(from_lane(left, who), 0.0), total};
 }
 
-// The entry, of a wave's N a lane, one lane's behind another's, whose running sum passes `left`: its number, -1 if none has a share.
-template <int N>
-__device__ __forceinline__ int find_entry(const float (&v)[N], double left) {
-    double own = 0.0;
+// The entry of a block whose running sum passes `left`: its number, -1 if none has a share.  values(k, v): the E values of the lane's chunk k, 64 lanes
+// beside each other.  First the chunks' sums over the wave, then the one chunk lane by lane and entry by entry: a lane holds E values and not all.
+template <int LOADS, int E, typename Values>
+__device__ __forceinline__ int find_entry(double left, Values values) {
+    double own[LOADS];
+    float v[E];
 #pragma unroll
-    for (int e = 0; e < N; ++e) own += (double)v[e];
-    const double running = wave_running(own);
-    const int who = holder(own, running, left);
-    if (who < 0) return -1;
+    for (int k = 0; k < LOADS; ++k) {
+        values(k, v);
+        own[k] = 0.0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) own[k] += (double)v[e];
+    }
+    int chunk = -1, last = -1;
+    double sum = 0.0, before = 0.0, before_last = 0.0, mine = 0.0, mine_last = 0.0;
+#pragma unroll
+    for (int k = 0; k < LOADS; ++k) {
+        const double all = wave_sum(own[k]);
+        if (all > 0.0) {
+            last = k;
+            before_last = sum;
+            mine_last = own[k];
+            if (chunk < 0 && sum + all > left) {
+                chunk = k;
+                before = sum;
+                mine = own[k];
+            }
+            sum += all;
+        }
+    }
+    if (last < 0) return -1;
+    if (chunk < 0) {                     // (rounding can leave none that is passed)
+        chunk = last;
+        before = before_last;
+        mine = mine_last;
+    }
+    const double goal = left - before, running = wave_running(mine);
+    const int who = holder(mine, running, goal);
+#pragma unroll
+    for (int k = 0; k < LOADS; ++k)
+        if (k == chunk) values(k, v);
     // (every lane looks among its own, the one in question tells)
-    double sum = running - own;
+    double at = running - mine;
     int found = 0;
     bool done = false;
 #pragma unroll
-    for (int e = 0; e < N; ++e)
+    for (int e = 0; e < E; ++e)
         if (v[e] > 0.0f && !done) {
             found = e;
-            sum += (double)v[e];
-            done = sum > left;
+            at += (double)v[e];
+            done = at > goal;
         }
-    return who * N + __builtin_amdgcn_readlane(found, who);
+    return (chunk * 64 + who) * E + __builtin_amdgcn_readlane(found, who);
 }
 
 // u in [0, 1)
@@ -233,43 +261,44 @@ struct Drawn {
     float logp;
 };
 
-// Entry of p, without entry `skip` (-1: none is left out) where anything else has a share.  By one wave.
+// Entry of p, without entry `skip` (-1: none is left out) where anything else has a share.  w: of the whole row.  By one wave.
 template <typename T>
-__device__ __forceinline__ Drawn draw_from(const T* row, int vocab, Factor c, double s, const BlockSum* table, int skip, float u) {
+__device__ __forceinline__ Drawn draw_from(const T* row, int vocab, Factor c, double s, const BlockSum* table, const Whole& w, int skip, float u) {
     typedef Line<T> L;
     const L line(row, vocab);
     const int lane = threadIdx.x & 63, blocks = line.blocks();
-    auto entries = [&](int b, float ref, int without, float (&v)[L::kEntries]) {
-        typename L::vec raw[L::kLoads];
-        line.template fetch<false>(b, lane, raw);
-        line.template mend<false>(b, lane, raw);
-#pragma unroll
-        for (int k = 0; k < L::kLoads; ++k)
-#pragma unroll
-            for (int e = 0; e < L::E; ++e) {
-                const bool gone = line.first(L::template chunk<false>(b, k, lane)) + e == without;
-                v[k * L::E + e] = gone ? 0.0f : share((float)raw[k][e], anchor(ref), c.c);
-            }
-    };
-    const Whole w = wave_whole(table, blocks, c);
     if (!has_mass(w.sum) || u != u) return {-1, NAN};
-    float v[L::kEntries], skipped = 0.0f;      // skipped: the sum of the block that is short of an entry
+    typename L::vec raw[L::kLoads];
+    auto open = [&](int b) {
+        line.fetch(b, lane, raw);
+        line.mend(b, lane, raw);
+    };
+    auto values = [&](int b, float ref, int k, float (&v)[L::E]) {
+        const int at = line.first(L::chunk(b, k, lane));
+#pragma unroll
+        for (int e = 0; e < L::E; ++e) v[e] = at + e == skip ? 0.0f : share((float)raw[k][e], anchor(ref), c.c);
+    };
+    float skipped = 0.0f;                // the sum of the block that is short of an entry
     const int short_block = skip >= 0 ? line.block_of(skip) : -1;
     if (skip >= 0) {
-        entries(short_block, table[short_block].ref, skip, v);
+        open(short_block);
+        float v[L::E];
 #pragma unroll
-        for (int e = 0; e < L::kEntries; ++e) skipped += v[e];
+        for (int k = 0; k < L::kLoads; ++k) {
+            values(short_block, table[short_block].ref, k, v);
+#pragma unroll
+            for (int e = 0; e < L::E; ++e) skipped += v[e];
+        }
         skipped = wave_sum_f(skipped);
     }
-    auto at = [&](int b) { return (double)(b == short_block ? skipped : table[b].sum) * (double)weight_of(table[b].ref, w.top, c); };
-    Place p = find_block(blocks, number(u), at);
+    Place p = find_block(blocks, number(u), [&](int b) { return (double)(b == short_block ? skipped : table[b].sum) * (double)weight_of(table[b].ref, w.top, c); });
     if (p.block < 0) {                   // (nothing else has a share: with the entry that was to be left out)
         skip = -1;
         p = find_block(blocks, number(u), [&](int b) { return (double)table[b].sum * (double)weight_of(table[b].ref, w.top, c); });
     }
     const float ref = table[p.block].ref;
-    entries(p.block, ref, skip, v);
-    const int found = find_entry(v, p.left / (double)weight_of(ref, w.top, c));
+    open(p.block);
+    const int found = find_entry<L::kLoads, L::E>(p.left / (double)weight_of(ref, w.top, c), [&](int k, float (&v)[L::E]) { values(p.block, ref, k, v); });
     if (found < 0) return {-1, NAN};
     const int token = line.first(p.block * L::kPer) + found;
     return {token, (float)(((double)(float)row[token] - (double)w.top) * s - log_d(w.sum))};
@@ -285,7 +314,7 @@ __global__ __launch_bounds__(1024) void k_draw_rows(DrawArgs a, int64_t first) {
     sum_blocks<T>(line, a.c.c, (int)(threadIdx.x >> 6), line.blocks(), (int)(blockDim.x >> 6), sums);
     __syncthreads();
     if (threadIdx.x >= 64) return;
-    const Drawn d = draw_from<T>(row, a.vocab, a.c, a.s, sums, -1, a.uniform[r]);
+    const Drawn d = draw_from<T>(row, a.vocab, a.c, a.s, sums, wave_whole(sums, line.blocks(), a.c), -1, a.uniform[r]);
     if (threadIdx.x == 0) {
         a.tokens[r] = d.token;
         a.logp[r] = d.logp;
@@ -303,7 +332,9 @@ __global__ __launch_bounds__(kDrawBlock) void k_block_sums(DrawArgs a, int piece
 template <typename T>
 __global__ __launch_bounds__(64) void k_draw(DrawArgs a, int64_t most, const BlockSum* table) {
     const int64_t r = blockIdx.x;
-    const Drawn d = draw_from<T>((const T*)a.z + r * a.ld, a.vocab, a.c, a.s, table + r * most, -1, a.uniform[r]);
+    const T* row = (const T*)a.z + r * a.ld;
+    table += r * most;
+    const Drawn d = draw_from<T>(row, a.vocab, a.c, a.s, table, wave_whole(table, Line<T>(row, a.vocab).blocks(), a.c), -1, a.uniform[r]);
     if (threadIdx.x == 0) {
         a.tokens[r] = d.token;
         a.logp[r] = d.logp;
@@ -322,14 +353,188 @@ __device__ __forceinline__ const T* row_of(const RowSet& s, int64_t i, int t) {
     return (const T*)s.z + i * s.ld_request + (int64_t)t * s.ld;
 }
 
-// Sums of the rows that may be asked for: the target's at positions up to a request's length, and (rows behind those) the drafter's before
+// What is known of a position before its rows are summed.  (Asked for early, so that nothing has to be waited for behind the sums.)
+template <typename T>
+struct Asked {
+    int x = 0;               // the drafted token
+    bool inside = false;     // it lies in the vocabulary
+    float u = 0.0f, given = 0.0f, z = 0.0f, zq = 0.0f;      // given: draft_logp; z, zq: its logits
+    Asked() = default;
+    __device__ __forceinline__ Asked(const VerifyArgs& a, int64_t i, int t, const T* row, const T* drow) {
+        const int64_t at = i * a.drafts + t, drafted = a.drafted[at];
+        u = a.uniform[at];
+        given = a.draft_logp ? a.draft_logp[at] : 0.0f;
+        inside = drafted >= 0 && drafted < a.vocab;
+        x = inside ? (int)drafted : 0;
+        z = (float)row[x];
+        zq = a.draft.z ? (float)drow[x] : 0.0f;
+    }
+};
+// Whether a position's token is accepted, and what is drawn from otherwise.  w: of the drafter's row, where it is summed.
+template <typename T>
+__device__ __forceinline__ Position judged(const VerifyArgs& a, const Asked<T>& k, const Whole& p, const Whole& w) {
+    Position v = {p.sum, p.top, 0.0f, 0.0f, 0, kFromTarget, 0, 0.0f};
+    if (!k.inside || !has_mass(p.sum)) return v;
+    double q = 1.0;
+    if (a.draft.z && !a.draft_logp) {
+        if (!has_mass(w.sum)) return v;
+        q = exp(((double)k.zq - (double)w.top) * a.draft_s) / w.sum;
+        v.q_ref = w.top;
+        v.q_factor = (float)(1.0 / w.sum);
+    } else if (a.draft.z) {
+        q = exp((double)k.given);
+        if (!(has_mass(q) && fabsf(k.zq) < INFINITY)) return v;
+        v.q_ref = k.zq;
+        v.q_factor = (float)q;
+    }
+    const double lp = ((double)k.z - (double)p.top) * a.s - log_d(p.sum);
+    v.mode = a.draft.z ? kRest : kWithout;
+    v.x = k.x;
+    v.accepted = q > 0.0 && (double)k.u * q < exp(lp);
+    v.logp = (float)lp;
+    return v;
+}
+__device__ __forceinline__ Position behind_last(const Whole& p) { return {p.sum, p.top, 0.0f, 0.0f, 0, kFromTarget, 0, 0.0f}; }
+
+// -1 and 0 from position `from` of a request on, by `threads` threads
+__device__ __forceinline__ void blanks(const VerifyArgs& a, int64_t i, int from, int thread, int threads) {
+    const int64_t out = i * (a.drafts + 1);
+    for (int t = from + thread; t <= a.drafts; t += threads) {
+        a.tokens[out + t] = -1;
+        a.logp[out + t] = 0.0f;
+    }
+}
+
+// max(p - q, 0) of the lane's entries of a block of target and drafter.  (A difference that is no number stays one, and p is drawn from instead.)
+template <typename T>
+struct Rest {
+    typedef Line<T> L;
+    typename L::vec p[L::kLoads], q[L::kLoads];
+    __device__ __forceinline__ void open(const L& line, const T* drow, int b) {
+        const int lane = threadIdx.x & 63;
+        line.fetch(b, lane, p);
+#pragma unroll
+        for (int k = 0; k < L::kLoads; ++k) q[k] = line.beside(drow, L::chunk(b, k, lane));
+        line.mend(b, lane, p);
+    }
+    __device__ __forceinline__ void values(const VerifyArgs& a, const Position& d, float inv, int k, float (&v)[L::E]) const {
+#pragma unroll
+        for (int e = 0; e < L::E; ++e) {
+            const float r = share_exact((float)p[k][e], d.top, a.c) * inv - share_exact((float)q[k][e], d.q_ref, a.draft_c) * d.q_factor;
+            v[e] = r <= 0.0f ? 0.0f : r;
+        }
+    }
+};
+
+// The last token of a request, at position t, by one wave.  rest(b): the sum of block b of max(p - q, 0), where that is drawn from.
+template <typename T, typename At>
+__device__ __forceinline__ void finish(const VerifyArgs& a, int64_t i, int t, const Position& d, const BlockSum* table, At rest) {
+    typedef Line<T> L;
+    const T* row = row_of<T>(a.target, i, t);
+    const float v = a.last_uniform[i];
+    Drawn got = {-1, NAN};
+    bool found = false;
+    if (d.mode == kRest && v == v) {
+        const L line(row, a.vocab);
+        const Place p = find_block(line.blocks(), number(v), rest);
+        if (p.block >= 0 && has_mass(p.total)) {         // (a sum that is no number makes the total one)
+            Rest<T> part;
+            part.open(line, row_of<T>(a.draft, i, t), p.block);
+            const float inv = (float)(1.0 / d.sum);
+            const int e = find_entry<L::kLoads, L::E>(p.left, [&](int k, float (&out)[L::E]) { part.values(a, d, inv, k, out); });
+            found = e >= 0;
+            if (found) {
+                got.token = line.first(p.block * L::kPer) + e;
+                got.logp = (float)(((double)(float)row[got.token] - (double)d.top) * a.s - log_d(d.sum));
+            }
+        }
+    }
+    if (!found) got = draw_from<T>(row, a.vocab, a.c, a.s, table, {d.top, d.sum}, d.mode == kWithout ? d.x : -1, v);
+    if ((threadIdx.x & 63) == 0) {
+        const int64_t out = i * (a.drafts + 1) + t;
+        a.tokens[out] = got.token;
+        a.logp[out] = got.logp;
+        a.count[i] = t + (got.token >= 0 ? 1 : 0);
+    }
+}
+
+// Sum of max(p - q, 0) over a block, by one wave.
+template <typename T>
+__device__ __forceinline__ double sum_rest(const VerifyArgs& a, const Position& d, const Line<T>& line, const T* drow, int b) {
+    Rest<T> part;
+    part.open(line, drow, b);
+    const float inv = (float)(1.0 / d.sum);
+    float sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < Line<T>::kLoads; ++k) {
+        float v[Line<T>::E];
+        part.values(a, d, inv, k, v);
+#pragma unroll
+        for (int e = 0; e < Line<T>::E; ++e) sum += v[e];
+    }
+    return wave_sum((double)sum);
+}
+
+// A workgroup a request, position by position, up to the first token that is not accepted: no row behind it is read.
+template <typename T>
+__global__ __launch_bounds__(1024) void k_verify_requests(VerifyArgs a, int64_t first, int64_t most) {
+    extern __shared__ BlockSum sums[];                  // of the target's row, then of the drafter's, or of the blocks of max(p - q, 0)
+    __shared__ Position at;
+    const int64_t i = first + blockIdx.x, out = i * (a.drafts + 1);
+    const int n = length_of(a, i), wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    if (n < 0) {
+        blanks(a, i, 0, threadIdx.x, blockDim.x);
+        if (threadIdx.x == 0) a.count[i] = 0;
+        return;
+    }
+    int t = 0;
+    for (;; ++t) {
+        const T *row = row_of<T>(a.target, i, t), *drow = a.draft.z && t < n ? row_of<T>(a.draft, i, t) : row;
+        const Line<T> line(row, a.vocab), dline(drow, a.vocab);
+        Asked<T> asked;
+        if (t < n) asked = Asked<T>(a, i, t, row, drow);
+        const bool both = a.draft.z && !a.draft_logp && t < n;
+        const int half = both && waves > 1 ? (waves + 1) / 2 : waves;
+        if (wave < half) sum_blocks<T>(line, a.c.c, wave, line.blocks(), half, sums);
+        if (both && (wave >= half || waves == 1)) sum_blocks<T>(dline, a.draft_c.c, waves == 1 ? 0 : wave - half, dline.blocks(), waves == 1 ? 1 : waves - half, sums + most);
+        __syncthreads();
+        if (wave == 0) {
+            const Whole p = wave_whole(sums, line.blocks(), a.c);
+            const Position v = t < n ? judged<T>(a, asked, p, both ? wave_whole(sums + most, dline.blocks(), a.draft_c) : Whole{0.0f, 0.0}) : behind_last(p);
+            if (threadIdx.x == 0) {
+                at = v;
+                if (v.accepted) {
+                    a.tokens[out + t] = asked.x;
+                    a.logp[out + t] = v.logp;
+                }
+            }
+        }
+        __syncthreads();
+        if (!at.accepted) break;                        // (at position n it is not)
+    }
+    blanks(a, i, t + 1, threadIdx.x, blockDim.x);
+    const Position d = at;
+    double* rest = (double*)(sums + most);
+    if (d.mode == kRest) {
+        const Line<T> line(row_of<T>(a.target, i, t), a.vocab);
+        const T* drow = row_of<T>(a.draft, i, t);
+        for (int b = wave; b < line.blocks(); b += waves) {
+            const double s = sum_rest<T>(a, d, line, drow, b);
+            if ((threadIdx.x & 63) == 0) rest[b] = s;
+        }
+        __syncthreads();
+    }
+    if (wave == 0) finish<T>(a, i, t, d, sums, [&](int b) { return rest[b]; });
+}
+
+// Few requests: their rows' blocks over many workgroups.  The target's rows up to a request's length, and (rows behind those) the drafter's before
 // it.  The requests' tickets are cleared for the next launch.
 template <typename T>
 __global__ __launch_bounds__(kDrawBlock) void k_verify_sums(VerifyArgs a, int64_t first, int pieces, int64_t most, BlockSum* target, BlockSum* draft,
                                                             unsigned* tickets) {
     int64_t r = first + blockIdx.x / (unsigned)pieces;
     const int piece = blockIdx.x % (unsigned)pieces;
-    if (tickets && piece == 0 && r < a.requests && threadIdx.x == 0) tickets[r] = 0;
+    if (piece == 0 && r < a.requests && threadIdx.x == 0) tickets[r] = 0;
     const int64_t of_target = a.requests * a.target.each;
     const bool drafter = r >= of_target;
     if (drafter) r -= of_target;
@@ -343,178 +548,68 @@ __global__ __launch_bounds__(kDrawBlock) void k_verify_sums(VerifyArgs a, int64_
                   (drafter ? draft : target) + r * most);
 }
 
-// One position, by one wave; every lane gets the result.
-struct Verdict {
-    int accepted;
-    float logp;              // of the drafted token, accepted
-    Decision next;           // what is drawn from otherwise
-};
+// The first token of a request that is not accepted, the sums of max(p - q, 0) there, and its last token.  Every workgroup finds out the first
+// for itself, and the last to be done the third (the sums are read in their own order, whichever that is): a launch each less.
 template <typename T>
-__device__ __forceinline__ Verdict judge(const VerifyArgs& a, int64_t i, int t, int64_t most, const BlockSum* target, const BlockSum* draft) {
-    const int64_t at = i * a.drafts + t;
-    const int64_t drafted = a.drafted[at];
-    const T *row = row_of<T>(a.target, i, t), *drow = a.draft.z ? row_of<T>(a.draft, i, t) : row;
-    const bool summed = a.draft.z && !a.draft_logp;
-    // (all that is needed is asked for before anything is waited for)
-    const int x = drafted >= 0 && drafted < a.vocab ? (int)drafted : 0;
-    const float u = a.uniform[at], given = a.draft_logp ? a.draft_logp[at] : 0.0f, z = (float)row[x], zq = (float)drow[x];
-    const Whole p = wave_whole(target + (i * a.target.each + t) * most, Line<T>(row, a.vocab).blocks(), a.c);
-    Verdict v = {0, 0.0f, {t, kFromTarget, 0, 0.0f, 0.0f, 0.0f, 0.0f}};
-    if (x != drafted || !has_mass(p.sum)) return v;
-    double q = 1.0;
-    if (a.draft.z) {
-        if (summed) {
-            const Whole w = wave_whole(draft + (i * a.draft.each + t) * most, Line<T>(drow, a.vocab).blocks(), a.draft_c);
-            if (!has_mass(w.sum)) return v;
-            q = exp(((double)zq - (double)w.top) * a.draft_s) / w.sum;
-            v.next.q_ref = w.top;
-            v.next.q_factor = (float)(1.0 / w.sum);
-        } else {
-            q = exp((double)given);
-            if (!(has_mass(q) && fabsf(zq) < INFINITY)) return v;
-            v.next.q_ref = zq;
-            v.next.q_factor = (float)q;
-        }
-        v.next.mode = kRest;
-        v.next.m = p.top;
-        v.next.inv = (float)(1.0 / p.sum);
-    } else {
-        v.next.mode = kWithout;
-        v.next.x = x;
+__global__ __launch_bounds__(kDrawBlock) void k_verify_rest(VerifyArgs a, int64_t first, int pieces, int64_t most, const BlockSum* target, const BlockSum* draft,
+                                                            double* rest, unsigned* tickets) {
+    __shared__ Position found[kDrawWaves];
+    __shared__ int last;
+    const int64_t i = first + blockIdx.x / (unsigned)pieces, out = i * (a.drafts + 1);
+    const int piece = blockIdx.x % (unsigned)pieces, n = length_of(a, i), wave = threadIdx.x >> 6;
+    if (n < 0) {
+        if (piece == 0) blanks(a, i, 0, threadIdx.x, kDrawBlock);
+        if (piece == 0 && threadIdx.x == 0) a.count[i] = 0;
+        return;
     }
-    const double lp = ((double)z - (double)p.top) * a.s - log_d(p.sum);
-    v.accepted = q > 0.0 && (double)u * q < exp(lp);
-    v.logp = (float)lp;
-    return v;
-}
-
-// Goes through a request's drafted tokens, four at a time.  `tell`: writes what is accepted and the blanks behind it.
-template <typename T>
-__device__ __forceinline__ Decision decide(const VerifyArgs& a, int64_t i, int64_t most, const BlockSum* target, const BlockSum* draft, bool tell) {
-    __shared__ Verdict found[kDrawWaves];
-    const int wave = threadIdx.x >> 6, n = length_of(a, i);
-    const int64_t out = i * (a.drafts + 1);
-    Decision d = {n, kFromTarget, 0, 0.0f, 0.0f, 0.0f, 0.0f};
-    int accepted = max(n, 0);
-    for (int t0 = 0; t0 < n; t0 += kDrawWaves) {
-        const int some = min(kDrawWaves, n - t0);
+    const BlockSum* table = target + i * a.target.each * most;
+    int t = 0;
+    Position d;
+    for (bool more = true; more;) {                     // four positions at a time
+        const int mine = t + wave, some = min(kDrawWaves, n + 1 - t);
         if (wave < some) {
-            const Verdict v = judge<T>(a, i, t0 + wave, most, target, draft);
-            if ((threadIdx.x & 63) == 0) found[wave] = v;
+            const T* row = row_of<T>(a.target, i, mine);
+            const int blocks = Line<T>(row, a.vocab).blocks();
+            if (mine < n) {
+                const T* drow = a.draft.z ? row_of<T>(a.draft, i, mine) : row;
+                const Asked<T> asked(a, i, mine, row, drow);
+                const Whole p = wave_whole(table + mine * most, blocks, a.c);
+                const Position v = judged<T>(a, asked, p, a.draft.z && !a.draft_logp ? wave_whole(draft + (i * a.draft.each + mine) * most, Line<T>(drow, a.vocab).blocks(), a.draft_c)
+                                                                                     : Whole{0.0f, 0.0});
+                if ((threadIdx.x & 63) == 0) found[wave] = v;
+            } else {
+                const Whole p = wave_whole(table + mine * most, blocks, a.c);
+                if ((threadIdx.x & 63) == 0) found[wave] = behind_last(p);
+            }
         }
         __syncthreads();
         int w = 0;
         while (w < some && found[w].accepted) ++w;
-        if (tell && (int)threadIdx.x < w) {
-            const int t = t0 + (int)threadIdx.x;
-            a.tokens[out + t] = a.drafted[i * a.drafts + t];
-            a.logp[out + t] = found[threadIdx.x].logp;
+        if (piece == 0 && (int)threadIdx.x < w) {
+            a.tokens[out + t + threadIdx.x] = a.drafted[i * a.drafts + t + threadIdx.x];
+            a.logp[out + t + threadIdx.x] = found[threadIdx.x].logp;
         }
-        if (w < some) {
-            d = found[w].next;
-            accepted = t0 + w;
-            break;
-        }
+        t += w;
+        more = w == some;                               // (at position n none is accepted)
+        if (!more) d = found[w];
         __syncthreads();
     }
-    if (tell)
-        for (int t = (n < 0 ? 0 : accepted + 1) + (int)threadIdx.x; t <= a.drafts; t += kDrawBlock) {
-            a.tokens[out + t] = -1;
-            a.logp[out + t] = 0.0f;
-        }
-    if (tell && n < 0 && threadIdx.x == 0) a.count[i] = 0;
-    return d;
-}
-
-// max(p - q, 0) of the lane's entries of block b.  (A difference that is no number stays one, and p is drawn from instead.)
-template <typename T, bool SPREAD>
-__device__ __forceinline__ void rest_of(const Line<T>& line, const T* drow, int b, const VerifyArgs& a, const Decision& d, float (&v)[Line<T>::kEntries]) {
-    typedef Line<T> L;
-    const int lane = threadIdx.x & 63;
-    typename L::vec p[L::kLoads], q[L::kLoads];
-    line.template fetch<SPREAD>(b, lane, p);
-#pragma unroll
-    for (int k = 0; k < L::kLoads; ++k) q[k] = line.beside(drow, L::template chunk<SPREAD>(b, k, lane));
-    line.template mend<SPREAD>(b, lane, p);
-#pragma unroll
-    for (int k = 0; k < L::kLoads; ++k)
-#pragma unroll
-        for (int e = 0; e < L::E; ++e) {
-            const float r = share_exact((float)p[k][e], d.m, a.c) * d.inv - share_exact((float)q[k][e], d.q_ref, a.draft_c) * d.q_factor;
-            v[k * L::E + e] = r <= 0.0f ? 0.0f : r;
-        }
-}
-
-// The last token of a request, by one wave.  rest: sums of the blocks of max(p - q, 0), where that is drawn from.
-template <typename T>
-__device__ __forceinline__ void finish(const VerifyArgs& a, int64_t i, const Decision& d, int64_t most, const BlockSum* target, const double* rest) {
-    typedef Line<T> L;
-    const T* row = row_of<T>(a.target, i, d.t);
-    const BlockSum* table = target + (i * a.target.each + d.t) * most;
-    const float v = a.last_uniform[i];
-    Drawn got = {-1, NAN};
-    bool found = false;
-    if (d.mode == kRest && v == v) {
-        const L line(row, a.vocab);
-        const Place p = find_block(line.blocks(), number(v), [&](int b) { return observe(&rest[b]); });
-        if (p.block >= 0 && has_mass(p.total)) {         // (a sum that is no number makes the total one)
-            found = true;
-            float part[L::kEntries];
-            rest_of<T, false>(line, row_of<T>(a.draft, i, d.t), p.block, a, d, part);
-            const int e = find_entry(part, p.left);
-            const Whole w = wave_whole(table, line.blocks(), a.c);
-            if (e >= 0) {
-                got.token = line.first(p.block * L::kPer) + e;
-                got.logp = (float)(((double)(float)row[got.token] - (double)w.top) * a.s - log_d(w.sum));
-            }
-        }
-    }
-    if (!found) got = draw_from<T>(row, a.vocab, a.c, a.s, table, d.mode == kWithout ? d.x : -1, v);
-    if ((threadIdx.x & 63) == 0) {
-        const int64_t out = i * (a.drafts + 1) + d.t;
-        a.tokens[out] = got.token;
-        a.logp[out] = got.logp;
-        a.count[i] = d.t + (got.token >= 0 ? 1 : 0);
-    }
-}
-
-// Where a request's first token that is not accepted is, the sums of max(p - q, 0) there, and its last token.  Every workgroup of a request finds
-// out the first for itself, and the last to be done the third (its sums are read in their own order, whichever that is): a launch each less.
-template <typename T>
-__global__ __launch_bounds__(kDrawBlock) void k_verify_rest(VerifyArgs a, int64_t first, int pieces, int64_t most, const BlockSum* target,
-                                                            const BlockSum* draft, double* rest, unsigned* tickets) {
-    __shared__ int last;
-    const int64_t i = first + blockIdx.x / (unsigned)pieces;
-    const int piece = blockIdx.x % (unsigned)pieces;
-    const Decision d = decide<T>(a, i, most, target, draft, piece == 0);
-    if (d.t < 0) return;
+    if (piece == 0) blanks(a, i, t + 1, threadIdx.x, kDrawBlock);
+    table += t * most;
     if (d.mode != kRest) {
-        if (piece == 0 && threadIdx.x < 64) finish<T>(a, i, d, most, target, nullptr);
+        if (piece == 0 && wave == 0) finish<T>(a, i, t, d, table, [](int) { return 0.0; });
         return;
     }
     double* sums = rest + i * most;
-    const Line<T> line(row_of<T>(a.target, i, d.t), a.vocab);
-    const T* drow = row_of<T>(a.draft, i, d.t);
+    const Line<T> line(row_of<T>(a.target, i, t), a.vocab);
+    const T* drow = row_of<T>(a.draft, i, t);
     const int blocks = line.blocks(), each = (blocks + pieces - 1) / pieces, end = min((piece + 1) * each, blocks);
-    for (int b = piece * each + (int)(threadIdx.x >> 6); b < end; b += kDrawWaves) {
-        float v[Line<T>::kEntries];
-        rest_of<T, true>(line, drow, b, a, d, v);
-        float sum = 0.0f;
-#pragma unroll
-        for (int e = 0; e < Line<T>::kEntries; ++e) sum += v[e];
-        const double s = wave_sum((double)sum);
+    for (int b = piece * each + wave; b < end; b += kDrawWaves) {
+        const double s = sum_rest<T>(a, d, line, drow, b);
         if ((threadIdx.x & 63) == 0) publish(&sums[b], s);
     }
     if (!arrive_is_last(&tickets[i], &last, (unsigned)pieces)) return;
-    if (threadIdx.x < 64) finish<T>(a, i, d, most, target, sums);
-}
-
-// The same without a drafter's rows.
-template <typename T>
-__global__ __launch_bounds__(kDrawBlock) void k_verify_draw(VerifyArgs a, int64_t first, int64_t most, const BlockSum* target) {
-    const int64_t i = first + blockIdx.x;
-    const Decision d = decide<T>(a, i, most, target, nullptr, true);
-    if (d.t >= 0 && threadIdx.x < 64) finish<T>(a, i, d, most, target, nullptr);
+    if (wave == 0) finish<T>(a, i, t, d, table, [&](int b) { return observe(&sums[b]); });
 }
 
 constexpr int64_t kWorkgroupsMax = 1 << 22;      // of a launch (which takes fewer than 2^32 threads): longer batches take several
@@ -537,12 +632,19 @@ hipError_t in_launches(int64_t rows, int64_t each, F f) {
     return hipSuccess;
 }
 
-// Waves that take a row together; 0: it is split over workgroups.
+// Waves that take a row together; 0: it is split over workgroups.  us of calls in a row, split / 4 / 8 / 16 waves: 8192 x 131072 bf16 398 / 363 / 358 / 381,
+// 1001 x 50021 f16 27.6 / 22.8 / 23.6 / 30.6, 300 x 131072 f32 37.1 / 42.5 / 35.8 / 39.1, 100 x 131072 bf16 12.2 / 15.5 / 13.8 / 12.8, 40 x 100000 f32 11.1 /
+// 23.0 / 15.1 / 13.4, 1 x 65536 bf16 10.4 / 9.4 / 8.3 / 7.8, 8 x 32768 9.5 / 7.2 / 6.7 / 6.5, 8192 x 4000 30 / 29 / 42 / 59.
 int row_waves(int64_t rows, int64_t blocks) {
-    if (rows <= 64 && blocks > 64) return 0;
-    const int64_t want = rows >= 2048 ? 4 : (rows >= 512 ? 8 : 16);
+    if (rows <= 128 && blocks > 56) return 0;
+    const int64_t want = rows <= 256 ? 16 : (blocks >= 32 ? 8 : 4);
     return (int)(want < blocks ? want : blocks);
 }
+
+// Whether a request's positions are taken one after another by one workgroup, which then reads no row in vain but goes no faster than its
+// compute unit.  us, so / by many workgroups: 256 requests of 5 drafts x 131072 f16 93 / 126, 256 of 2 x 20000 20 / 24, 200 of 4 x 131072 bf16 with both
+// sides summed 108 / 125, 128 of 4 x 131072 75 / 60, 128 of 4 x 32768 29.5 / 25.5, 2 of 3 x 32768 12.4 / 11.3.
+bool by_request(int64_t requests) { return requests >= 160; }
 
 template <typename T>
 hipError_t draw_rows(const DrawArgs& a, void* ws, hipStream_t st) {
@@ -564,26 +666,28 @@ hipError_t draw_rows(const DrawArgs& a, void* ws, hipStream_t st) {
 template <typename T>
 hipError_t verify_rows(const VerifyArgs& a, void* ws, hipStream_t st) {
     const int64_t most = blocks_of(a.vocab, sizeof(T)), n = a.requests;
-    const bool rest = a.draft.z != nullptr, sums = rest && !a.draft_logp;
-    const VerifySpace sp = verify_space(n, a.drafts, a.vocab, sizeof(T), rest, sums);
+    const bool both = a.draft.z && !a.draft_logp;
+    if (by_request(n)) {
+        const int64_t want = most * (both ? 2 : 1), waves = want < 16 ? want : 16;      // (of 4 kB each: a compute unit's share of the card)
+        return in_launches(n, 1, [&](int64_t first, int64_t c) {
+            hipLaunchKernelGGL(k_verify_requests<T>, dim3((unsigned)c), dim3((unsigned)waves * 64), most * (a.draft.z ? 2 : 1) * sizeof(BlockSum), st, a, first, most);
+        });
+    }
+    const VerifySpace sp = verify_space(n, a.drafts, a.vocab, sizeof(T), a.draft.z, both);
     char* at = (char*)ws;
-    BlockSum *target = (BlockSum*)(at + sp.target), *draft = (BlockSum*)(at + sp.draft);
-    double* parts = (double*)(at + sp.rest);
-    unsigned* tickets = rest ? (unsigned*)(at + sp.tickets) : nullptr;
-    const int64_t rows = n * a.target.each + (sums ? n * a.draft.each : 0);
+    BlockSum *target = (BlockSum*)at, *draft = (BlockSum*)(at + sp.draft);
+    double* rest = (double*)(at + sp.rest);
+    unsigned* tickets = (unsigned*)(at + sp.tickets);
+    const int64_t rows = n * a.target.each + (both ? n * a.draft.each : 0);
     int pieces = pieces_of(rows, most, 4096);
     hipError_t e = in_launches(rows, pieces, [&](int64_t first, int64_t c) {
         hipLaunchKernelGGL(k_verify_sums<T>, dim3((unsigned)(c * pieces)), dim3(kDrawBlock), 0, st, a, first, pieces, most, target, draft, tickets);
     });
     if (e != hipSuccess) return e;
-    if (!rest)
-        return in_launches(n, 1, [&](int64_t first, int64_t c) {
-            hipLaunchKernelGGL(k_verify_draw<T>, dim3((unsigned)c), dim3(kDrawBlock), 0, st, a, first, most, (const BlockSum*)target);
-        });
-    pieces = pieces_of(n, most, 1024);
+    pieces = a.draft.z ? pieces_of(n, most, 4096) : 1;
     return in_launches(n, pieces, [&](int64_t first, int64_t c) {
         hipLaunchKernelGGL(k_verify_rest<T>, dim3((unsigned)(c * pieces)), dim3(kDrawBlock), 0, st, a, first, pieces, most, (const BlockSum*)target,
-                           (const BlockSum*)draft, parts, tickets);
+                           (const BlockSum*)draft, rest, tickets);
     });
 }
 
@@ -601,14 +705,14 @@ size_t draw_space(int64_t rows, int64_t vocab, int size) {
     return rows == 0 || row_waves(rows, blocks) ? 0 : rounded((size_t)(rows * blocks) * sizeof(BlockSum));
 }
 
-VerifySpace verify_space(int64_t requests, int64_t drafts, int64_t vocab, int size, bool draft_rows, bool draft_sums) {
+VerifySpace verify_space(int64_t requests, int64_t drafts, int64_t vocab, int size, bool drafter, bool both) {
     const size_t most = (size_t)blocks_of(vocab, size), n = (size_t)requests;
+    if (n == 0 || by_request(requests)) return {0, 0, 0, 0};
     VerifySpace s;
-    s.target = 0;
     s.draft = rounded(n * (drafts + 1) * most * sizeof(BlockSum));
-    s.rest = s.draft + (draft_sums ? rounded(n * drafts * most * sizeof(BlockSum)) : 0);
-    s.tickets = s.rest + (draft_rows ? rounded(n * most * sizeof(double)) : 0);
-    s.whole = s.tickets + (draft_rows ? rounded(n * sizeof(unsigned)) : 0);
+    s.rest = s.draft + (both ? rounded(n * drafts * most * sizeof(BlockSum)) : 0);
+    s.tickets = s.rest + (drafter ? rounded(n * most * sizeof(double)) : 0);
+    s.whole = s.tickets + rounded(n * sizeof(unsigned));
     return s;
 }
 

@@ -54,8 +54,8 @@ int check_strides(const lbfgsb_drafts* d, int64_t ld, int64_t ld_request, int64_
 }
 
 VerifySpace space_of(const lbfgsb_drafts* d) {
-    const bool rest = d->draft_z && d->drafts > 0;
-    return verify_space(d->requests, d->drafts, d->vocab, (int)size_of(d->dtype), rest, rest && !d->draft_logp);
+    const bool drafter = d->draft_z && d->drafts > 0;
+    return verify_space(d->requests, d->drafts, d->vocab, (int)size_of(d->dtype), drafter, drafter && !d->draft_logp);
 }
 
 }  // namespace

@@ -134,11 +134,16 @@ def test_drafts_are_checked(bad):
 def test_outputs_and_workspace_of_a_verification():
     lib = L.lib()
     assert _verify(None) == _verify(_drafts(), tokens=None) == _verify(_drafts(), count=None) == _verify(_drafts(), logp=None) == L.E_INVALID_ARG
-    for kw in ({}, dict(draft_logp=None), dict(draft_z=None, draft_logp=None), dict(drafts=0)):
-        d = _drafts(**kw)
-        n = lib.lbfgsb_verify_workspace_bytes(C.byref(d))
-        assert n > 0 and n % 256 == 0
-        assert _verify(d, n=n - 1) == _verify(d, ws=None) == _verify(d, ws=0x100010) == L.E_INVALID_ARG
+    some = 0
+    for long in (dict(), dict(vocab=200000, ld=200000, ld_request=1000000, draft_ld=200000, draft_ld_request=800000, requests=24)):
+        for kw in ({}, dict(draft_logp=None), dict(draft_z=None, draft_logp=None), dict(drafts=0)):
+            d = _drafts(**long, **kw)
+            n = lib.lbfgsb_verify_workspace_bytes(C.byref(d))
+            assert n % 256 == 0
+            if n:                                         # (0: none is needed)
+                some += 1
+                assert _verify(d, n=n - 1) == _verify(d, ws=None) == _verify(d, ws=0x100010) == L.E_INVALID_ARG
+    assert some
     assert _verify(_drafts(requests=0, z=None), tokens=None, count=None, logp=None) == L.OK
     assert lib.lbfgsb_verify_workspace_bytes(None) == 0
 

@@ -124,6 +124,18 @@ def test_extreme_temperatures(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("offset,temperature", [(0.0, 0.004), (0.0, 1e-20), (300.0, 1.0), (-300.0, 1.0), (1000.0, 1.0), (-60000.0, 90.0), (700.0, 1.0)])
+def test_logits_far_from_zero(offset, temperature, dtype):
+    """Exponents of hundreds and thousands, on both sides of where they are formed another way."""
+    z = (logits_of((40, 2500), torch.float32, seed=9, spread=3.0 * min(temperature, 90.0)) + offset).to(TYPES[dtype]).to(DEV)
+    z[3, :1200] = torch.finfo(TYPES[dtype]).min
+    u = numbers(40, 3).to(DEV)
+    check_draw(z, u, temperature, L.draw_tokens(z, u, temperature=temperature))
+    many = z[:4].repeat(200, 1)
+    check_draw(many, numbers(800, 4).to(DEV), temperature, L.draw_tokens(many, numbers(800, 4).to(DEV), temperature=temperature))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("start", [0, 1, 3, 5])
 @pytest.mark.parametrize("rows", [6, 700])
 def test_rows_that_begin_anywhere(start, rows, dtype):

@@ -132,27 +132,31 @@ __device__ __forceinline__ void eight(const X* row, int col, int cols, bool some
     }
 }
 
-// All of x's (up to 16) rows to LDS, by a whole workgroup: four units of a thread on their way at once.
-template <typename X>
-__device__ __forceinline__ void bring_whole(const Matvec4Args& a, int64_t x0, int rows, typename Operand<typename OperandOf<X>::type>::vec* lds) {
+// All of x's (up to 16) rows to LDS, by a whole workgroup, N units of a thread on their way at once.
+template <typename X, int N>
+__device__ __forceinline__ void bring_by(const Matvec4Args& a, int64_t x0, int rows, typename Operand<typename OperandOf<X>::type>::vec* lds) {
     const int tid = threadIdx.x, kq = tid & 3, j = (tid >> 2) & 3, steps = a.w.steps(), stride = (int)blockDim.x >> 4, units = operand_units<X>(rows);
-    int row = (tid >> 4) < steps ? 0 : rows, step = tid >> 4;
+    int row = 0, step = tid >> 4;
+    auto settle = [&] {
+        while (step >= steps) {
+            step -= steps;
+            ++row;
+        }
+    };
+    settle();
     while (row < rows) {
-        X v[4][8];
-        int to[4];
+        X v[N][8];
+        int to[N];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < N; ++k) {
             const bool some = row < rows;
             to[k] = some ? step * units + unit_at(0, j, kq, rows, row) : -1;
             eight((const X*)a.x + (x0 + (some ? row : 0)) * a.ld_x, step * kStepCols + 32 * j + 8 * kq, a.w.cols, some, v[k]);
             step += stride;
-            if (step >= steps) {
-                step = tid >> 4;
-                ++row;
-            }
+            settle();
         }
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < N; ++k) {
             if (to[k] < 0) continue;
             Parts<X> p;
             p.set(v[k]);
@@ -160,6 +164,15 @@ __device__ __forceinline__ void bring_whole(const Matvec4Args& a, int64_t x0, in
             for (int n = 0; n < Parts<X>::N; ++n) lds[to[k] + n * 16 * rows] = p.p[n];
         }
     }
+}
+// (Two at a time, 50021 x 2600 with 5 rows of f16 would wait four times, and four at a time twice: 20.8 us, with eight 19.8.  But eight where there are
+// two cost 131072 x 4096 with one row 47.9 us for 44.9.)
+template <typename X>
+__device__ __forceinline__ void bring_whole(const Matvec4Args& a, int64_t x0, int rows, typename Operand<typename OperandOf<X>::type>::vec* lds) {
+    const int all = rows * a.w.steps(), stride = (int)blockDim.x >> 4;      // a thread's units: all / stride
+    if (all <= 2 * stride) bring_by<X, 2>(a, x0, rows, lds);
+    else if (sizeof(X) == 4 || all <= 4 * stride) bring_by<X, 4>(a, x0, rows, lds);
+    else if constexpr (sizeof(X) == 2) bring_by<X, 8>(a, x0, rows, lds);
 }
 
 // What brings x, laid out by k_operands4, to LDS a few steps at a time; a thread's units of the next are on their way while these are used.
@@ -426,9 +439,13 @@ hipError_t matvec4(const Matvec4Args& a, hipStream_t st) {
     if (T == 1 && whole <= kWholeBytes)
         return wide ? matvec4_in<X, S, G, G == 1 ? 2 : 4, 1, true>(a, whole <= kWholeBytes / 2 ? 4 : 8, st) : matvec4_in<X, S, G, 1, 1, true>(a, 8, st);
     if (T == 1) return wide ? matvec4_in<X, S, G, G == 1 ? 2 : 4, 1, false>(a, 4, st) : matvec4_in<X, S, G, 1, 1, false>(a, 8, st);
-    if (T == 2) return wide ? matvec4_in<X, S, G, G == 1 ? 2 : 4, 2, false>(a, 2, st) : matvec4_in<X, S, G, 1, 2, false>(a, 2, st);
-    if constexpr (sizeof(X) == 2)
+    // (us for 65536 x 4096, groups of 128, two / four tiles of the weights to a wave: 32 rows of bf16 40.3 / 43.8, of f32 78 / 67, 48 of bf16 48.5 / 52.7,
+    // 64 73 / 61; and the 48 with four tiles of x 57)
+    if (T == 2) return wide ? matvec4_in<X, S, G, sizeof(X) == 2 || G == 1 ? 2 : 4, 2, false>(a, 2, st) : matvec4_in<X, S, G, 1, 2, false>(a, 2, st);
+    if constexpr (sizeof(X) == 2) {
+        if (T == 3) return wide ? matvec4_in<X, S, G, 2, 3, false>(a, 2, st) : matvec4_in<X, S, G, 1, 3, false>(a, 2, st);
         return wide ? matvec4_in<X, S, G, G == 4 ? 4 : 2, 4, false>(a, 2, st) : matvec4_in<X, S, G, 1, 4, false>(a, 2, st);
+    }
     return hipErrorInvalidValue;
 }
 

@@ -34,7 +34,7 @@ struct Matvec4Args {
 };
 
 // tiles of 16 rows of x that are multiplied in one pass over the weights
-inline int tiles_of(int64_t tokens, size_t size_x) { return tokens <= 16 ? 1 : (tokens <= 32 || size_x == 4 ? 2 : 4); }
+inline int tiles_of(int64_t tokens, size_t size_x) { return tokens <= 16 ? 1 : (tokens <= 32 || size_x == 4 ? 2 : (tokens <= 48 ? 3 : 4)); }
 // matrix instructions between two groups
 inline int depth_of(int group_log2) { return group_log2 == 5 ? 1 : (group_log2 == 6 ? 2 : 4); }
 

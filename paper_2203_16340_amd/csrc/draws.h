@@ -58,9 +58,14 @@ struct Position {
     float logp;              // its log-probability
 };
 
+struct Asked {
+    int x, inside;           // the drafted token; it lies in the vocabulary
+    float u, given, z, zq;   // given: draft_logp; z, zq: its logits
+};
+
 // where the parts of a call's workspace are, in bytes behind the blocks' sums of the target's rows (draws.hip); whole: how much there is of it
 struct VerifySpace {
-    size_t draft, rest, tickets, whole;
+    size_t draft, rest, asked, tickets, whole;
 };
 // drafter: its rows are there; both: they are summed as well
 VerifySpace verify_space(int64_t requests, int64_t drafts, int64_t vocab, int size, bool drafter, bool both);

@@ -18,7 +18,12 @@ constexpr int kDrawBlock = 256, kDrawWaves = kDrawBlock / 64;
 // 2^((z - ref) c) as it enters the sums of blocks: c is the factor's first part alone (2^-25 of the distance to the wave's largest so far,
 // to one side; joins of blocks take both parts).
 __device__ __forceinline__ float share(float z, float ref, float c) { return exp2_hw((z - ref) * c); }
-// The same with the factor's second part and the rounding of the exponent put right: for differences p - q, and references that are not the largest.
+// The same with the factor's second part: for differences p - q.  (It takes no part where it is small against a distance without end.)
+__device__ __forceinline__ float share_both(float z, float ref, Factor c) {
+    const float d = z - ref;
+    return exp2_hw(fmaf(d, c.c, fmaxf(d, -1000.0f) * c.low));
+}
+// And with the rounding of the exponent put right: for references that are not the largest.
 __device__ __forceinline__ float share_exact(float z, float ref, Factor c) {
     const float d = z - ref, a = d * c.c, e = exp2_hw(a);
     const float rest = a > -1000.0f && a < 1000.0f ? fmaf(d, c.low, fmaf(d, c.c, -a)) : 0.0f;
@@ -180,16 +185,33 @@ struct Place {
     int block;               // -1: no block has a share
     double left, total;
 };
-template <typename At>
+template <int FEW, typename At>          // FEW: sums of a lane that are asked for at once, and once, if there are no more: each may be a trip to memory
 __device__ __forceinline__ Place find_block(int blocks, double u, At at) {
     const int lane = threadIdx.x & 63, each = (blocks + 63) / 64, from = min(lane * each, blocks), to = min(from + each, blocks);
-    double own = 0.0;
-    for (int b = from; b < to; ++b) own += at(b);
+    double own = 0.0, few[FEW];
+    if (each <= FEW) {
+#pragma unroll
+        for (int k = 0; k < FEW; ++k) few[k] = from + k < to ? at(from + k) : 0.0;
+#pragma unroll
+        for (int k = 0; k < FEW; ++k) own += few[k];
+    } else {
+        for (int b = from; b < to; ++b) own += at(b);
+    }
     const double running = wave_running(own), total = from_lane(running, 63), goal = u * total;
     const int who = holder(own, running, goal);
     double sum = running - own, left = goal - sum;
     int found = from;
-    if (each > 1)
+    if (each <= FEW) {
+        bool done = false;
+#pragma unroll
+        for (int k = 0; k < FEW; ++k)
+            if (few[k] > 0.0 && !done) {
+                found = from + k;
+                left = goal - sum;
+                sum += few[k];
+                done = sum > goal;
+            }
+    } else {
         for (int b = from; b < to; ++b) {
             const double v = at(b);
             if (!(v > 0.0)) continue;
@@ -198,6 +220,7 @@ __device__ __forceinline__ Place find_block(int blocks, double u, At at) {
             sum += v;
             if (sum > goal) break;
         }
+    }
     if (who < 0) return {-1, 0.0, total};
     return {__builtin_amdgcn_readlane(found, who), fmax(from_lane(left, who), 0.0), total};
 }
@@ -297,10 +320,10 @@ __device__ __forceinline__ Drawn draw_from(const T* row, int vocab, Factor c, do
         }
         skipped = wave_sum_f(skipped);
     }
-    Place p = find_block(blocks, number(u), [&](int b) { return (double)(b == short_block ? skipped : table[b].sum) * (double)weight_of(table[b].ref, w.top, c); });
+    Place p = find_block<1>(blocks, number(u), [&](int b) { return (double)(b == short_block ? skipped : table[b].sum) * (double)weight_of(table[b].ref, w.top, c); });
     if (p.block < 0) {                   // (nothing else has a share: with the entry that was to be left out)
         skip = -1;
-        p = find_block(blocks, number(u), [&](int b) { return (double)table[b].sum * (double)weight_of(table[b].ref, w.top, c); });
+        p = find_block<1>(blocks, number(u), [&](int b) { return (double)table[b].sum * (double)weight_of(table[b].ref, w.top, c); });
     }
     const float ref = table[p.block].ref;
     open(p.block);
@@ -359,26 +382,21 @@ __device__ __forceinline__ const T* row_of(const RowSet& s, int64_t i, int t) {
     return (const T*)s.z + i * s.ld_request + (int64_t)t * s.ld;
 }
 
-// What is known of a position before its rows are summed.  (Asked for early, so that nothing has to be waited for behind the sums.)
+// What is known of a position before its rows are summed, asked for early: two trips to memory, one behind the other.
 template <typename T>
-struct Asked {
-    int x = 0;               // the drafted token
-    bool inside = false;     // it lies in the vocabulary
-    float u = 0.0f, given = 0.0f, z = 0.0f, zq = 0.0f;      // given: draft_logp; z, zq: its logits
-    Asked() = default;
-    __device__ __forceinline__ Asked(const VerifyArgs& a, int64_t i, int t, const T* row, const T* drow) {
-        const int64_t at = i * a.drafts + t, drafted = a.drafted[at];
-        u = a.uniform[at];
-        given = a.draft_logp ? a.draft_logp[at] : 0.0f;
-        inside = drafted >= 0 && drafted < a.vocab;
-        x = inside ? (int)drafted : 0;
-        z = (float)row[x];
-        zq = a.draft.z ? (float)drow[x] : 0.0f;
-    }
-};
+__device__ __forceinline__ Asked ask(const VerifyArgs& a, int64_t i, int t, const T* row, const T* drow) {
+    const int64_t at = i * a.drafts + t, drafted = a.drafted[at];
+    Asked k;
+    k.u = a.uniform[at];
+    k.given = a.draft_logp ? a.draft_logp[at] : 0.0f;
+    k.inside = drafted >= 0 && drafted < a.vocab;
+    k.x = k.inside ? (int)drafted : 0;
+    k.z = (float)row[k.x];
+    k.zq = a.draft.z ? (float)drow[k.x] : 0.0f;
+    return k;
+}
 // Whether a position's token is accepted, and what is drawn from otherwise.  w: of the drafter's row, where it is summed.
-template <typename T>
-__device__ __forceinline__ Position judged(const VerifyArgs& a, const Asked<T>& k, const Whole& p, const Whole& w) {
+__device__ __forceinline__ Position judged(const VerifyArgs& a, const Asked& k, const Whole& p, const Whole& w) {
     Position v = {p.sum, p.top, 0.0f, 0.0f, 0, kFromTarget, 0, 0.0f};
     if (!k.inside || !has_mass(p.sum)) return v;
     double q = 1.0;
@@ -411,28 +429,17 @@ __device__ __forceinline__ void blanks(const VerifyArgs& a, int64_t i, int from,
     }
 }
 
-// max(p - q, 0) of the lane's entries of a block of target and drafter.  (A difference that is no number stays one, and p is drawn from instead.)
+// max(p - q, 0) of a chunk.  (A difference that is no number stays one, and p is drawn from instead.)
 template <typename T>
-struct Rest {
-    typedef Line<T> L;
-    typename L::vec p[L::kLoads], q[L::kLoads];
-    __device__ __forceinline__ void open(const L& line, const T* drow, int b) {
-        const int lane = threadIdx.x & 63;
-        line.fetch(b, lane, p);
+__device__ __forceinline__ void rest_of(const VerifyArgs& a, const Position& d, float inv, typename Line<T>::vec p, typename Line<T>::vec q, float (&v)[Line<T>::E]) {
 #pragma unroll
-        for (int k = 0; k < L::kLoads; ++k) q[k] = line.beside(drow, L::chunk(b, k, lane));
-        line.mend(b, lane, p);
+    for (int e = 0; e < Line<T>::E; ++e) {
+        const float r = share_both((float)p[e], d.top, a.c) * inv - share_exact((float)q[e], d.q_ref, a.draft_c) * d.q_factor;
+        v[e] = r <= 0.0f ? 0.0f : r;
     }
-    __device__ __forceinline__ void values(const VerifyArgs& a, const Position& d, float inv, int k, float (&v)[L::E]) const {
-#pragma unroll
-        for (int e = 0; e < L::E; ++e) {
-            const float r = share_exact((float)p[k][e], d.top, a.c) * inv - share_exact((float)q[k][e], d.q_ref, a.draft_c) * d.q_factor;
-            v[e] = r <= 0.0f ? 0.0f : r;
-        }
-    }
-};
+}
 
-// The last token of a request, at position t, by one wave.  rest(b): the sum of block b of max(p - q, 0), where that is drawn from.
+// The last token of a request, at position t, by one wave.  rest(k): the sum of max(p - q, 0) over 64 chunks from 64 k on, where that is drawn from.
 template <typename T, typename At>
 __device__ __forceinline__ void finish(const VerifyArgs& a, int64_t i, int t, const Position& d, const BlockSum* table, At rest) {
     typedef Line<T> L;
@@ -442,15 +449,14 @@ __device__ __forceinline__ void finish(const VerifyArgs& a, int64_t i, int t, co
     bool found = false;
     if (d.mode == kRest && v == v) {
         const L line(row, a.vocab);
-        const Place p = find_block(line.blocks(), number(v), rest);
+        const Place p = find_block<8>(line.blocks() * L::kLoads, number(v), rest);
         if (p.block >= 0 && has_mass(p.total)) {         // (a sum that is no number makes the total one)
-            Rest<T> part;
-            part.open(line, row_of<T>(a.draft, i, t), p.block);
-            const float inv = (float)(1.0 / d.sum);
-            const int e = find_entry<L::kLoads, L::E>(p.left, [&](int k, float (&out)[L::E]) { part.values(a, d, inv, k, out); });
+            const int chunk = p.block * 64 + (int)(threadIdx.x & 63);
+            const typename L::vec z = line.beside(row, chunk), zq = line.beside(row_of<T>(a.draft, i, t), chunk);
+            const int e = find_entry<1, L::E>(p.left, [&](int, float (&out)[L::E]) { rest_of<T>(a, d, (float)(1.0 / d.sum), z, zq, out); });
             found = e >= 0;
             if (found) {
-                got.token = line.first(p.block * L::kPer) + e;
+                got.token = line.first(p.block * 64) + e;
                 got.logp = (float)(((double)(float)row[got.token] - (double)d.top) * a.s - log_d(d.sum));
             }
         }
@@ -464,27 +470,33 @@ __device__ __forceinline__ void finish(const VerifyArgs& a, int64_t i, int t, co
     }
 }
 
-// Sum of max(p - q, 0) over a block, by one wave.
-template <typename T>
-__device__ __forceinline__ double sum_rest(const VerifyArgs& a, const Position& d, const Line<T>& line, const T* drow, int b) {
-    Rest<T> part;
-    part.open(line, drow, b);
+// Sums of max(p - q, 0) over a block's chunks of 64 lanes, by one wave: put(number, sum).  (Finer than the blocks: the one wave that finds the token
+// has a chunk to go through then.)
+template <typename T, typename Put>
+__device__ __forceinline__ void sum_rest(const VerifyArgs& a, const Position& d, const Line<T>& line, const T* drow, int b, Put put) {
+    typedef Line<T> L;
+    typename L::vec p[L::kLoads], q[L::kLoads];
+    const int lane = threadIdx.x & 63;
+    line.fetch(b, lane, p);
+#pragma unroll
+    for (int k = 0; k < L::kLoads; ++k) q[k] = line.beside(drow, L::chunk(b, k, lane));
+    line.mend(b, lane, p);
     const float inv = (float)(1.0 / d.sum);
-    float sum = 0.0f;
 #pragma unroll
-    for (int k = 0; k < Line<T>::kLoads; ++k) {
-        float v[Line<T>::E];
-        part.values(a, d, inv, k, v);
+    for (int k = 0; k < L::kLoads; ++k) {
+        float v[L::E], sum = 0.0f;
+        rest_of<T>(a, d, inv, p[k], q[k], v);
 #pragma unroll
-        for (int e = 0; e < Line<T>::E; ++e) sum += v[e];
+        for (int e = 0; e < L::E; ++e) sum += v[e];
+        const double all = wave_sum((double)sum);
+        if (lane == 0) put(b * L::kLoads + k, all);
     }
-    return wave_sum((double)sum);
 }
 
 // A workgroup a request, position by position, up to the first token that is not accepted: no row behind it is read.
 template <typename T>
 __global__ __launch_bounds__(1024) void k_verify_requests(VerifyArgs a, int64_t first, int64_t most) {
-    extern __shared__ BlockSum sums[];                  // of the target's row, then of the drafter's, or of the blocks of max(p - q, 0)
+    extern __shared__ BlockSum sums[];                  // of the target's row, then of the drafter's, or of the chunks of max(p - q, 0)
     __shared__ Position at;
     const int64_t i = first + blockIdx.x, out = i * (a.drafts + 1);
     const int n = length_of(a, i), wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
@@ -497,8 +509,8 @@ __global__ __launch_bounds__(1024) void k_verify_requests(VerifyArgs a, int64_t 
     for (;; ++t) {
         const T *row = row_of<T>(a.target, i, t), *drow = a.draft.z && t < n ? row_of<T>(a.draft, i, t) : row;
         const Line<T> line(row, a.vocab), dline(drow, a.vocab);
-        Asked<T> asked;
-        if (t < n) asked = Asked<T>(a, i, t, row, drow);
+        Asked asked = {};
+        if (t < n) asked = ask<T>(a, i, t, row, drow);
         const bool both = a.draft.z && !a.draft_logp && t < n;
         const int half = both && waves > 1 ? (waves + 1) / 2 : waves;
         if (wave < half) sum_blocks<T>(line, a.c.c, wave, line.blocks(), half, sums);
@@ -506,7 +518,7 @@ __global__ __launch_bounds__(1024) void k_verify_requests(VerifyArgs a, int64_t 
         __syncthreads();
         if (wave == 0) {
             const Whole p = wave_whole(sums, line.blocks(), a.c);
-            const Position v = t < n ? judged<T>(a, asked, p, both ? wave_whole(sums + most, dline.blocks(), a.draft_c) : Whole{0.0f, 0.0}) : behind_last(p);
+            const Position v = t < n ? judged(a, asked, p, both ? wave_whole(sums + most, dline.blocks(), a.draft_c) : Whole{0.0f, 0.0}) : behind_last(p);
             if (threadIdx.x == 0) {
                 at = v;
                 if (v.accepted) {
@@ -524,20 +536,17 @@ __global__ __launch_bounds__(1024) void k_verify_requests(VerifyArgs a, int64_t 
     if (d.mode == kRest) {
         const Line<T> line(row_of<T>(a.target, i, t), a.vocab);
         const T* drow = row_of<T>(a.draft, i, t);
-        for (int b = wave; b < line.blocks(); b += waves) {
-            const double s = sum_rest<T>(a, d, line, drow, b);
-            if ((threadIdx.x & 63) == 0) rest[b] = s;
-        }
+        for (int b = wave; b < line.blocks(); b += waves) sum_rest<T>(a, d, line, drow, b, [&](int k, double s) { rest[k] = s; });
         __syncthreads();
     }
-    if (wave == 0) finish<T>(a, i, t, d, sums, [&](int b) { return rest[b]; });
+    if (wave == 0) finish<T>(a, i, t, d, sums, [&](int k) { return rest[k]; });
 }
 
 // Few requests: their rows' blocks over many workgroups.  The target's rows up to a request's length, and (rows behind those) the drafter's before
-// it.  The requests' tickets are cleared for the next launch.
+// it.  For the next launch what has to be asked for is there in one piece, and the requests' tickets are cleared.
 template <typename T>
 __global__ __launch_bounds__(kDrawBlock) void k_verify_sums(VerifyArgs a, int64_t first, int pieces, int64_t most, BlockSum* target, BlockSum* draft,
-                                                            unsigned* tickets) {
+                                                            Asked* asked, unsigned* tickets) {
     int64_t r = first + blockIdx.x / (unsigned)pieces;
     const int piece = blockIdx.x % (unsigned)pieces;
     if (piece == 0 && r < a.requests && threadIdx.x == 0) tickets[r] = 0;
@@ -548,39 +557,42 @@ __global__ __launch_bounds__(kDrawBlock) void k_verify_sums(VerifyArgs a, int64_
     const int64_t i = r / set.each;
     const int t = (int)(r - i * set.each), n = length_of(a, i);
     if (n < 0 || t > n - (drafter ? 1 : 0)) return;
-    const Line<T> line(row_of<T>(set, i, t), a.vocab);
+    const T* row = row_of<T>(set, i, t);
+    const Line<T> line(row, a.vocab);
     const int blocks = line.blocks(), each = (blocks + pieces - 1) / pieces;
+    if (piece == 0 && !drafter && t < n && threadIdx.x == 0) asked[i * a.drafts + t] = ask<T>(a, i, t, row, a.draft.z ? row_of<T>(a.draft, i, t) : row);
     sum_blocks<T>(line, drafter ? a.draft_c.c : a.c.c, piece * each + (int)(threadIdx.x >> 6), min((piece + 1) * each, blocks), kDrawWaves,
                   (drafter ? draft : target) + r * most);
 }
 
 // The first token of a request that is not accepted, the sums of max(p - q, 0) there, and its last token.  Every workgroup finds out the first
 // for itself, and the last to be done the third (the sums are read in their own order, whichever that is): a launch each less.
+constexpr int kRestWaves = 8;            // of a workgroup: as many positions are judged at once
 template <typename T>
-__global__ __launch_bounds__(kDrawBlock) void k_verify_rest(VerifyArgs a, int64_t first, int pieces, int64_t most, const BlockSum* target, const BlockSum* draft,
-                                                            double* rest, unsigned* tickets) {
-    __shared__ Position found[kDrawWaves];
+__global__ __launch_bounds__(kRestWaves * 64) void k_verify_rest(VerifyArgs a, int64_t first, int pieces, int64_t most, const BlockSum* target,
+                                                                 const BlockSum* draft, const Asked* asked, double* rest, unsigned* tickets) {
+    __shared__ Position found[kRestWaves];
     __shared__ int last;
     const int64_t i = first + blockIdx.x / (unsigned)pieces, out = i * (a.drafts + 1);
     const int piece = blockIdx.x % (unsigned)pieces, n = length_of(a, i), wave = threadIdx.x >> 6;
     if (n < 0) {
-        if (piece == 0) blanks(a, i, 0, threadIdx.x, kDrawBlock);
+        if (piece == 0) blanks(a, i, 0, threadIdx.x, blockDim.x);
         if (piece == 0 && threadIdx.x == 0) a.count[i] = 0;
         return;
     }
     const BlockSum* table = target + i * a.target.each * most;
     int t = 0;
     Position d;
-    for (bool more = true; more;) {                     // four positions at a time
-        const int mine = t + wave, some = min(kDrawWaves, n + 1 - t);
+    for (bool more = true; more;) {
+        const int mine = t + wave, some = min(kRestWaves, n + 1 - t);
         if (wave < some) {
             const T* row = row_of<T>(a.target, i, mine);
             const int blocks = Line<T>(row, a.vocab).blocks();
             if (mine < n) {
                 const T* drow = a.draft.z ? row_of<T>(a.draft, i, mine) : row;
-                const Asked<T> asked(a, i, mine, row, drow);
+                const Asked known = asked[i * a.drafts + mine];
                 const Whole p = wave_whole(table + mine * most, blocks, a.c);
-                const Position v = judged<T>(a, asked, p, a.draft.z && !a.draft_logp ? wave_whole(draft + (i * a.draft.each + mine) * most, Line<T>(drow, a.vocab).blocks(), a.draft_c)
+                const Position v = judged(a, known, p, a.draft.z && !a.draft_logp ? wave_whole(draft + (i * a.draft.each + mine) * most, Line<T>(drow, a.vocab).blocks(), a.draft_c)
                                                                                      : Whole{0.0f, 0.0});
                 if ((threadIdx.x & 63) == 0) found[wave] = v;
             } else {
@@ -592,7 +604,7 @@ __global__ __launch_bounds__(kDrawBlock) void k_verify_rest(VerifyArgs a, int64_
         int w = 0;
         while (w < some && found[w].accepted) ++w;
         if (piece == 0 && (int)threadIdx.x < w) {
-            a.tokens[out + t + threadIdx.x] = a.drafted[i * a.drafts + t + threadIdx.x];
+            a.tokens[out + t + threadIdx.x] = found[threadIdx.x].x;
             a.logp[out + t + threadIdx.x] = found[threadIdx.x].logp;
         }
         t += w;
@@ -600,29 +612,26 @@ __global__ __launch_bounds__(kDrawBlock) void k_verify_rest(VerifyArgs a, int64_
         if (!more) d = found[w];
         __syncthreads();
     }
-    if (piece == 0) blanks(a, i, t + 1, threadIdx.x, kDrawBlock);
+    if (piece == 0) blanks(a, i, t + 1, threadIdx.x, blockDim.x);
     table += t * most;
     if (d.mode != kRest) {
         if (piece == 0 && wave == 0) finish<T>(a, i, t, d, table, [](int) { return 0.0; });
         return;
     }
-    double* sums = rest + i * most;
+    double* sums = rest + i * most * Line<T>::kLoads;
     const Line<T> line(row_of<T>(a.target, i, t), a.vocab);
     const T* drow = row_of<T>(a.draft, i, t);
     const int blocks = line.blocks(), each = (blocks + pieces - 1) / pieces, end = min((piece + 1) * each, blocks);
-    for (int b = piece * each + wave; b < end; b += kDrawWaves) {
-        const double s = sum_rest<T>(a, d, line, drow, b);
-        if ((threadIdx.x & 63) == 0) publish(&sums[b], s);
-    }
+    for (int b = piece * each + wave; b < end; b += kRestWaves) sum_rest<T>(a, d, line, drow, b, [&](int k, double s) { publish(&sums[k], s); });
     if (!arrive_is_last(&tickets[i], &last, (unsigned)pieces)) return;
-    if (wave == 0) finish<T>(a, i, t, d, table, [&](int b) { return observe(&sums[b]); });
+    if (wave == 0) finish<T>(a, i, t, d, table, [&](int k) { return observe(&sums[k]); });
 }
 
 constexpr int64_t kWorkgroupsMax = 1 << 22;      // of a launch (which takes fewer than 2^32 threads): longer batches take several
 
 // Pieces of each of `rows` rows: enough workgroups to fill the card, as far as each of their waves has a block.
-int pieces_of(int64_t rows, int64_t blocks, int64_t workgroups) {
-    const int64_t want = (workgroups + rows - 1) / rows, most = (blocks + kDrawWaves - 1) / kDrawWaves;
+int pieces_of(int64_t rows, int64_t blocks, int waves, int64_t workgroups) {
+    const int64_t want = (workgroups + rows - 1) / rows, most = (blocks + waves - 1) / waves;
     return (int)(want < most ? want : most);
 }
 
@@ -660,7 +669,7 @@ hipError_t draw_rows(const DrawArgs& a, void* ws, hipStream_t st) {
         return in_launches(a.rows, 1, [&](int64_t first, int64_t n) {
             hipLaunchKernelGGL(k_draw_rows<T>, dim3((unsigned)n), dim3(waves * 64), most * sizeof(BlockSum), st, a, first);
         });
-    const int pieces = pieces_of(a.rows, most, 2048);
+    const int pieces = pieces_of(a.rows, most, kDrawWaves, 2048);
     BlockSum* table = (BlockSum*)ws;
     hipLaunchKernelGGL(k_block_sums<T>, dim3((unsigned)(a.rows * pieces)), dim3(kDrawBlock), 0, st, a, pieces, most, table);
     hipError_t e = hipGetLastError();
@@ -676,24 +685,25 @@ hipError_t verify_rows(const VerifyArgs& a, void* ws, hipStream_t st) {
     if (by_request(n)) {
         const int64_t want = most * (both ? 2 : 1), waves = want < 16 ? want : 16;      // (of 4 kB each: a compute unit's share of the card)
         return in_launches(n, 1, [&](int64_t first, int64_t c) {
-            hipLaunchKernelGGL(k_verify_requests<T>, dim3((unsigned)c), dim3((unsigned)waves * 64), most * (a.draft.z ? 2 : 1) * sizeof(BlockSum), st, a, first, most);
+            hipLaunchKernelGGL(k_verify_requests<T>, dim3((unsigned)c), dim3((unsigned)waves * 64), most * (a.draft.z ? 1 + kBlockBytes / 1024 : 1) * sizeof(BlockSum), st, a, first, most);
         });
     }
     const VerifySpace sp = verify_space(n, a.drafts, a.vocab, sizeof(T), a.draft.z, both);
     char* at = (char*)ws;
     BlockSum *target = (BlockSum*)at, *draft = (BlockSum*)(at + sp.draft);
     double* rest = (double*)(at + sp.rest);
+    Asked* asked = (Asked*)(at + sp.asked);
     unsigned* tickets = (unsigned*)(at + sp.tickets);
     const int64_t rows = n * a.target.each + (both ? n * a.draft.each : 0);
-    int pieces = pieces_of(rows, most, 4096);
+    int pieces = pieces_of(rows, most, kDrawWaves, 4096);
     hipError_t e = in_launches(rows, pieces, [&](int64_t first, int64_t c) {
-        hipLaunchKernelGGL(k_verify_sums<T>, dim3((unsigned)(c * pieces)), dim3(kDrawBlock), 0, st, a, first, pieces, most, target, draft, tickets);
+        hipLaunchKernelGGL(k_verify_sums<T>, dim3((unsigned)(c * pieces)), dim3(kDrawBlock), 0, st, a, first, pieces, most, target, draft, asked, tickets);
     });
     if (e != hipSuccess) return e;
-    pieces = a.draft.z ? pieces_of(n, most, 4096) : 1;
+    pieces = a.draft.z ? pieces_of(n, most, kRestWaves, 2048) : 1;
     return in_launches(n, pieces, [&](int64_t first, int64_t c) {
-        hipLaunchKernelGGL(k_verify_rest<T>, dim3((unsigned)(c * pieces)), dim3(kDrawBlock), 0, st, a, first, pieces, most, (const BlockSum*)target,
-                           (const BlockSum*)draft, rest, tickets);
+        hipLaunchKernelGGL(k_verify_rest<T>, dim3((unsigned)(c * pieces)), dim3(kRestWaves * 64), 0, st, a, first, pieces, most, (const BlockSum*)target,
+                           (const BlockSum*)draft, (const Asked*)asked, rest, tickets);
     });
 }
 
@@ -713,11 +723,12 @@ size_t draw_space(int64_t rows, int64_t vocab, int size) {
 
 VerifySpace verify_space(int64_t requests, int64_t drafts, int64_t vocab, int size, bool drafter, bool both) {
     const size_t most = (size_t)blocks_of(vocab, size), n = (size_t)requests;
-    if (n == 0 || by_request(requests)) return {0, 0, 0, 0};
+    if (n == 0 || by_request(requests)) return {0, 0, 0, 0, 0};
     VerifySpace s;
     s.draft = rounded(n * (drafts + 1) * most * sizeof(BlockSum));
     s.rest = s.draft + (both ? rounded(n * drafts * most * sizeof(BlockSum)) : 0);
-    s.tickets = s.rest + (drafter ? rounded(n * most * sizeof(double)) : 0);
+    s.asked = s.rest + (drafter ? rounded(n * most * (kBlockBytes / 1024) * sizeof(double)) : 0);
+    s.tickets = s.asked + rounded(n * drafts * sizeof(Asked));
     s.whole = s.tickets + rounded(n * sizeof(unsigned));
     return s;
 }

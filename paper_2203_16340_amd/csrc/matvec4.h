@@ -400,6 +400,8 @@ hipError_t matvec4_in(const Matvec4Args& a, int step_waves, hipStream_t st) {
     const int64_t units = a.w.blocks() * (4 / NT), steps = a.w.steps();
     const int have = a.tokens < 16 * T ? (int)a.tokens : 16 * T;
     while (step_waves > steps) step_waves /= 2;
+    if (!WHOLE)                          // (a step a wave, twice: no more than a compute unit's LDS)
+        while ((size_t)step_units<X>(G, T) * 16 * 2 * step_waves > (128 << 10)) step_waves /= 2;
     Shape shape{row_waves, step_waves, 0};
     const int threads = row_waves * step_waves * 64;
     while ((1 << shape.chunk_log2) < step_waves) ++shape.chunk_log2;

@@ -17,7 +17,7 @@ pytestmark = pytest.mark.gpu
 TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
 ROOM = 4e-6
 SHAPES = [(1, 1), (1, 2), (3, 7), (5, 64), (2, 511), (3, 1024), (4, 1025), (3, 4096), (4, 4097), (130, 1000), (2, 50021), (1, 131073), (3, 262147),
-          (300, 2049), (1500, 333)]
+          (300, 2049), (1500, 333), (260, 70001)]
 
 
 def logits_of(shape, dtype, seed=0, spread=3.0):
@@ -222,7 +222,8 @@ def check_verify(got, z, x, u, v, s=1.0, draft=None, draft_logp=None, lengths=No
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("n,drafts,vocab", [(1, 1, 1), (1, 1, 2), (2, 3, 7), (3, 1, 1000), (40, 4, 333), (5, 9, 1025), (4, 2, 4097), (2, 3, 50021), (1, 5, 131073)])
+@pytest.mark.parametrize("n,drafts,vocab", [(1, 1, 1), (1, 1, 2), (2, 3, 7), (3, 1, 1000), (40, 4, 333), (5, 9, 1025), (4, 2, 4097), (2, 3, 50021), (1, 5, 131073), (2, 128, 40),
+                                            (170, 3, 333), (161, 2, 5001)])
 def test_verification(n, drafts, vocab, dtype):
     z, zq, x, lq, u, v = drafts_of(n, drafts, vocab, TYPES[dtype])
     on = [t.to(DEV) for t in (z, zq, x, lq, u, v)]
@@ -237,11 +238,12 @@ def test_verification(n, drafts, vocab, dtype):
     check_verify(got, z, x, u, v)
 
 
+@pytest.mark.parametrize("n", [24, 168])
 @pytest.mark.parametrize("dtype", TYPES)
-def test_lengths_and_temperatures(dtype):
-    n, drafts, vocab = 24, 6, 777
+def test_lengths_and_temperatures(dtype, n):
+    drafts, vocab = 6, 777
     z, zq, x, lq, u, v = drafts_of(n, drafts, vocab, TYPES[dtype], seed=4)
-    lengths = torch.tensor([0, 1, 2, 3, 4, 5, 6, 7, 100, -1, -100, 2] * 2)
+    lengths = torch.tensor([0, 1, 2, 3, 4, 5, 6, 7, 100, -1, -100, 2] * (n // 12))
     # what stands behind a request's length is not looked at
     for i in range(n):
         k = min(int(lengths[i]), drafts)
@@ -265,9 +267,10 @@ def test_a_drafter_that_is_the_target():
     check_verify(got, z, x, u, v, draft=z[:, :5])
 
 
+@pytest.mark.parametrize("n", [10, 165])
 @pytest.mark.parametrize("dtype", TYPES)
-def test_rows_without_a_distribution_and_tokens_outside_the_vocabulary(dtype):
-    n, drafts, vocab = 10, 3, 1100
+def test_rows_without_a_distribution_and_tokens_outside_the_vocabulary(dtype, n):
+    drafts, vocab = 3, 1100
     z, zq, x, lq, u, v = drafts_of(n, drafts, vocab, TYPES[dtype], seed=6, noise=0.05)
     u[:] = 0.05                                     # nearly everything that can be accepted is
     z[0, 1] = -torch.inf                            # no target at position 1
@@ -289,17 +292,19 @@ def test_rows_without_a_distribution_and_tokens_outside_the_vocabulary(dtype):
     check_verify(got, z, x, u, v)
 
 
-def test_all_the_mass_on_the_refused_token():
+@pytest.mark.parametrize("n", [1, 160])
+def test_all_the_mass_on_the_refused_token(n):
     """p is 1 at the drafted token, and refused by a number of 1: nothing is left but that token."""
-    z = torch.full((1, 2, 50), -200.0, device=DEV)
-    z[0, 0, 11] = z[0, 1, 3] = 0.0
-    x = torch.tensor([[11]], device=DEV)
-    got = L.verify_draft(z, x, torch.ones(1, 1, device=DEV), torch.full((1,), 0.5, device=DEV))
-    assert got.tokens.tolist() == [[11, -1]] and got.count.tolist() == [1]
+    z = torch.full((n, 2, 50), -200.0, device=DEV)
+    z[:, 0, 11] = z[:, 1, 3] = 0.0
+    x = torch.full((n, 1), 11, device=DEV)
+    got = L.verify_draft(z, x, torch.ones(n, 1, device=DEV), torch.full((n,), 0.5, device=DEV))
+    assert got.tokens.tolist() == [[11, -1]] * n and got.count.tolist() == [1] * n
 
 
-def test_positions_that_lie_anywhere():
-    n, drafts, vocab = 5, 3, 1203
+@pytest.mark.parametrize("n", [5, 163])
+def test_positions_that_lie_anywhere(n):
+    drafts, vocab = 3, 1203
     z, zq, x, lq, u, v = drafts_of(n, drafts, vocab, torch.bfloat16, seed=8)
     store = torch.full((drafts + 1, n, vocab + 9), torch.nan, dtype=torch.bfloat16, device=DEV)
     zs = store.transpose(0, 1)[:, :, 3:3 + vocab]

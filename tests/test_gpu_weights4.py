@@ -72,6 +72,20 @@ def test_products(tokens, rows, cols, x_type, scale_type):
             check(L.matvec4(x, w, dtype=torch.float32), x, codes, scale, z, cols, group)
 
 
+# x in LDS as a whole, at its largest and past it, and laid out beforehand; few rows of weights and many; tiles of x by their number
+LONG = [(16, 70, 2560), (16, 70, 2570), (9, 80, 5000), (12, 16390, 2700), (40, 16390, 300), (50, 16390, 300), (70, 16390, 200), (130, 100, 260)]
+
+
+@pytest.mark.parametrize("x_type,scale_type", [("f32", "f32"), ("bf16", "f16"), ("f16", "bf16")])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("tokens,rows,cols", LONG)
+def test_longer_products(tokens, rows, cols, group, x_type, scale_type):
+    codes, scale, z = plain(rows, cols, group, TYPES[scale_type], True)
+    w = packed(codes, scale, z, cols, group)
+    x = torch.randn(tokens, cols, generator=torch.Generator().manual_seed(cols)).to(TYPES[x_type]).to(DEV)
+    check(L.matvec4(x, w, dtype=torch.float32), x, codes, scale, z, cols, group)
+
+
 def test_every_code_and_column_is_where_it_belongs():
     """x picks one column at a time: y is then that column's weights to the bit."""
     rows, cols, group = 70, 261, 32

@@ -581,13 +581,13 @@ typedef struct {
     const float* last_uniform;        /* requests entries: v */
 } lbfgsb_drafts;
 /* With p_t and q_t the two distributions at position t and x_t the drafted token: x_t is accepted if q_t(x_t) > 0 and u_t q_t(x_t) <
- * p_t(x_t).  At the first x_t that is not, a token is drawn by v (as above, from the running sums) from max(p_t - q_t, 0), or from p_t where that is
+ * p_t(x_t) (a u_t below 0 counts as 0, NaN accepts nothing).  At the first x_t that is not, a token is drawn by v (as above, from the running sums) from max(p_t - q_t, 0), or from p_t where that is
  * 0 throughout; after all accepted, from p at the position behind them.
  *   draft_z NULL:     q_t = 1 at x_t, 0 elsewhere.
  *   draft_logp given: q_t(j) = exp(draft_logp_t + (draft_z_tj - draft_z_tx) / draft_temperature).
  * A drafted token outside the vocabulary, and one whose q_t(x_t) is not finite (its own logit or draft_logp infinite or NaN; without draft_logp: NaN or
  * +infinity anywhere in the drafter's row, or -infinity throughout), counts as q_t = 0: it is not accepted and p_t is drawn from.  With draft_logp the
- * drafter's row is read only where its token is not accepted; if that gives no finite q_t, p_t is drawn from.
+ * drafter's row is read only where its token is not accepted; if that gives a q_t(j) that is NaN or past 2^127, p_t is drawn from.
  * Positions behind a request's length are not read, whatever they hold.
  * tokens, logp: requests x (drafts + 1): what is emitted, accepted tokens and then the drawn one, with the target's log-probabilities;
  * -1 and 0 behind it.  count: requests entries, how many are emitted.  Where the drawn token's row has no distribution, or v is NaN, the token is

@@ -50,14 +50,18 @@ struct VerifyArgs {
 
 // What is drawn from where a position's token is not accepted.
 enum { kFromTarget = 0, kWithout = 1, kRest = 2 };     // p; p without the token; max(p - q, 0)
+struct Exponent {            // of 2, in two parts
+    float high, low;
+};
 struct Position {
     double sum;              // p_j = 2^((z_j - top) c) / sum
     float top;
-    float q_ref, q_factor;   // q_j = 2^((zq_j - q_ref) cq) q_factor
+    Exponent p;              //     = 2^((z_j - top) c + p)
+    float q_ref;
+    Exponent q;              // q_j = 2^((zq_j - q_ref) cq + q)
     int accepted, mode, x;   // x: the drafted token
     float logp;              // its log-probability
 };
-
 struct Asked {
     int x, inside;           // the drafted token; it lies in the vocabulary
     float u, given, z, zq;   // given: draft_logp; z, zq: its logits

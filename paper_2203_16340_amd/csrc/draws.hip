@@ -18,16 +18,15 @@ constexpr int kDrawBlock = 256, kDrawWaves = kDrawBlock / 64;
 // 2^((z - ref) c) as it enters the sums of blocks: c is the factor's first part alone (2^-25 of the distance to the wave's largest so far,
 // to one side; joins of blocks take both parts).
 __device__ __forceinline__ float share(float z, float ref, float c) { return exp2_hw((z - ref) * c); }
-// The same with the factor's second part: for differences p - q.  (It takes no part where it is small against a distance without end.)
-__device__ __forceinline__ float share_both(float z, float ref, Factor c) {
-    const float d = z - ref;
-    return exp2_hw(fmaf(d, c.c, fmaxf(d, -1000.0f) * c.low));
+// 2^((z - ref) c + e), with the second parts of both, for differences p - q.  (Where z is the largest's equal or not far from it the first exponent is
+// small, whatever its parts are, and so is its rounding.  The second takes no part where it is small against a distance without end.)
+__device__ __forceinline__ float mass(float z, float ref, Factor c, Exponent e) {
+    const float d = z - ref, x = exp2_hw(fmaf(d, c.c, e.high));
+    return fmaf(x, fmaf(fmaxf(d, -1000.0f), c.low, e.low) * 0.693147181f, x);
 }
-// And with the rounding of the exponent put right: for references that are not the largest.
-__device__ __forceinline__ float share_exact(float z, float ref, Factor c) {
-    const float d = z - ref, a = d * c.c, e = exp2_hw(a);
-    const float rest = a > -1000.0f && a < 1000.0f ? fmaf(d, c.low, fmaf(d, c.c, -a)) : 0.0f;
-    return fmaf(e, rest * 0.693147181f, e);
+__device__ __forceinline__ Exponent exponent_of(double log) {       // of e to one of 2
+    const double x = log * 1.44269504088896340736;
+    return {(float)x, (float)(x - (double)(float)x)};
 }
 
 // A row as it is read in blocks: chunks of 16 bytes on boundaries of the logits, of which the first and the last may hold less of the row.
@@ -397,28 +396,30 @@ __device__ __forceinline__ Asked ask(const VerifyArgs& a, int64_t i, int t, cons
 }
 // Whether a position's token is accepted, and what is drawn from otherwise.  w: of the drafter's row, where it is summed.
 __device__ __forceinline__ Position judged(const VerifyArgs& a, const Asked& k, const Whole& p, const Whole& w) {
-    Position v = {p.sum, p.top, 0.0f, 0.0f, 0, kFromTarget, 0, 0.0f};
+    Position v = {p.sum, p.top, {}, 0.0f, {}, 0, kFromTarget, 0, 0.0f};
     if (!k.inside || !has_mass(p.sum)) return v;
-    double q = 1.0;
+    double log_q = 0.0;
     if (a.draft.z && !a.draft_logp) {
         if (!has_mass(w.sum)) return v;
-        q = exp(((double)k.zq - (double)w.top) * a.draft_s) / w.sum;
+        const double log_sum = log_d(w.sum);
+        log_q = ((double)k.zq - (double)w.top) * a.draft_s - log_sum;
         v.q_ref = w.top;
-        v.q_factor = (float)(1.0 / w.sum);
+        v.q = exponent_of(-log_sum);
     } else if (a.draft.z) {
-        q = exp((double)k.given);
-        if (!(has_mass(q) && fabsf(k.zq) < INFINITY)) return v;
+        log_q = (double)k.given;
+        if (!(has_mass(exp(log_q)) && fabsf(k.zq) < INFINITY)) return v;
         v.q_ref = k.zq;
-        v.q_factor = (float)q;
+        v.q = exponent_of(log_q);
     }
-    const double lp = ((double)k.z - (double)p.top) * a.s - log_d(p.sum);
+    const double log_sum = log_d(p.sum), lp = ((double)k.z - (double)p.top) * a.s - log_sum, q = exp(log_q);
+    v.p = exponent_of(-log_sum);
     v.mode = a.draft.z ? kRest : kWithout;
     v.x = k.x;
-    v.accepted = q > 0.0 && (double)k.u * q < exp(lp);
+    v.accepted = q > 0.0 && (double)(k.u < 0.0f ? 0.0f : k.u) * q < exp(lp);
     v.logp = (float)lp;
     return v;
 }
-__device__ __forceinline__ Position behind_last(const Whole& p) { return {p.sum, p.top, 0.0f, 0.0f, 0, kFromTarget, 0, 0.0f}; }
+__device__ __forceinline__ Position behind_last(const Whole& p) { return {p.sum, p.top, {}, 0.0f, {}, 0, kFromTarget, 0, 0.0f}; }
 
 // -1 and 0 from position `from` of a request on, by `threads` threads
 __device__ __forceinline__ void blanks(const VerifyArgs& a, int64_t i, int from, int thread, int threads) {
@@ -431,11 +432,11 @@ __device__ __forceinline__ void blanks(const VerifyArgs& a, int64_t i, int from,
 
 // max(p - q, 0) of a chunk.  (A difference that is no number stays one, and p is drawn from instead.)
 template <typename T>
-__device__ __forceinline__ void rest_of(const VerifyArgs& a, const Position& d, float inv, typename Line<T>::vec p, typename Line<T>::vec q, float (&v)[Line<T>::E]) {
+__device__ __forceinline__ void rest_of(const VerifyArgs& a, const Position& d, typename Line<T>::vec p, typename Line<T>::vec q, float (&v)[Line<T>::E]) {
 #pragma unroll
     for (int e = 0; e < Line<T>::E; ++e) {
-        const float r = share_both((float)p[e], d.top, a.c) * inv - share_exact((float)q[e], d.q_ref, a.draft_c) * d.q_factor;
-        v[e] = r <= 0.0f ? 0.0f : r;
+        const float at_q = mass((float)q[e], d.q_ref, a.draft_c, d.q), r = mass((float)p[e], d.top, a.c, d.p) - at_q;
+        v[e] = !(at_q < INFINITY) ? NAN : (r <= 0.0f ? 0.0f : r);
     }
 }
 
@@ -453,7 +454,7 @@ __device__ __forceinline__ void finish(const VerifyArgs& a, int64_t i, int t, co
         if (p.block >= 0 && has_mass(p.total)) {         // (a sum that is no number makes the total one)
             const int chunk = p.block * 64 + (int)(threadIdx.x & 63);
             const typename L::vec z = line.beside(row, chunk), zq = line.beside(row_of<T>(a.draft, i, t), chunk);
-            const int e = find_entry<1, L::E>(p.left, [&](int, float (&out)[L::E]) { rest_of<T>(a, d, (float)(1.0 / d.sum), z, zq, out); });
+            const int e = find_entry<1, L::E>(p.left, [&](int, float (&out)[L::E]) { rest_of<T>(a, d, z, zq, out); });
             found = e >= 0;
             if (found) {
                 got.token = line.first(p.block * 64) + e;
@@ -481,11 +482,10 @@ __device__ __forceinline__ void sum_rest(const VerifyArgs& a, const Position& d,
 #pragma unroll
     for (int k = 0; k < L::kLoads; ++k) q[k] = line.beside(drow, L::chunk(b, k, lane));
     line.mend(b, lane, p);
-    const float inv = (float)(1.0 / d.sum);
 #pragma unroll
     for (int k = 0; k < L::kLoads; ++k) {
         float v[L::E], sum = 0.0f;
-        rest_of<T>(a, d, inv, p[k], q[k], v);
+        rest_of<T>(a, d, p[k], q[k], v);
 #pragma unroll
         for (int e = 0; e < L::E; ++e) sum += v[e];
         const double all = wave_sum((double)sum);

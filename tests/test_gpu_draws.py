@@ -292,6 +292,34 @@ def test_rows_without_a_distribution_and_tokens_outside_the_vocabulary(dtype, n)
     check_verify(got, z, x, u, v)
 
 
+@pytest.mark.parametrize("n", [6, 160])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_drafted_tokens_that_are_next_to_impossible(dtype, n):
+    """Log-probabilities of -60 to -110, a target that has masked the token: p - q is what it would be for any other."""
+    vocab = 900
+    z, zq, x, lq, u, v = drafts_of(n, 1, vocab, TYPES[dtype], seed=12)
+    depth = torch.linspace(60, 110, n).to(TYPES[dtype])
+    x[:, 0] = 17
+    z[:, 0, 17] = -torch.inf
+    zq[torch.arange(n), 0, 17] = -depth
+    lq = torch.tensor([[ref.log_softmax(zq[i, 0].double().numpy(), 1.0)[17]] for i in range(n)]).float()
+    for logp in (None, lq):
+        got = L.verify_draft(z.to(DEV), x.to(DEV), u.to(DEV), v.to(DEV), draft_logits=zq.to(DEV), draft_logp=None if logp is None else lq.to(DEV))
+        assert (got.count == 1).all()
+        check_verify(got, z, x, u, v, draft=zq, draft_logp=logp)
+
+
+def test_numbers_outside_their_range_accept_no_masked_token():
+    z = torch.zeros(3, 2, 50, device=DEV)
+    z[:, 0, 4] = -torch.inf
+    x = torch.full((3, 1), 4, device=DEV)
+    got = L.verify_draft(z, x, torch.tensor([[-1.0], [torch.nan], [2.0]], device=DEV), torch.full((3,), 0.5, device=DEV))
+    assert (got.count == 1).all() and (got.tokens[:, 0] != 4).all()
+    x[:] = 5
+    got = L.verify_draft(z, x, torch.tensor([[-1.0], [torch.nan], [2.0]], device=DEV), torch.full((3,), 0.5, device=DEV))
+    assert got.count.tolist() == [2, 1, 1]
+
+
 @pytest.mark.parametrize("n", [1, 160])
 def test_all_the_mass_on_the_refused_token(n):
     """p is 1 at the drafted token, and refused by a number of 1: nothing is left but that token."""

@@ -15,8 +15,9 @@ namespace {
 
 constexpr int kDrawBlock = 256, kDrawWaves = kDrawBlock / 64;
 
-// 2^((z - ref) c) as it enters the sums of blocks: c is the factor's first part alone (2^-25 of the distance to the wave's largest so far,
-// to one side; joins of blocks take both parts).
+// 2^((z - ref) c) as it enters the sums of blocks: c is the factor's first part alone, which is off by 2^-25 of the distance to the wave's largest so
+// far, to one side (1e-8 of it at temperature 1); joins of blocks take both parts.  (Both at every entry: 1001 x 50021 f16 24.5 us for 21.6, 256
+// requests of 5 drafts 101 for 93.)
 __device__ __forceinline__ float share(float z, float ref, float c) { return exp2_hw((z - ref) * c); }
 // 2^((z - ref) c + e), with the second parts of both, for differences p - q.  (Where z is the largest's equal or not far from it the first exponent is
 // small, whatever its parts are, and so is its rounding.  The second takes no part where it is small against a distance without end.)

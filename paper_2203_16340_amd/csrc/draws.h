@@ -50,7 +50,7 @@ struct VerifyArgs {
 
 // What is drawn from where a position's token is not accepted.
 enum { kFromTarget = 0, kWithout = 1, kRest = 2 };     // p; p without the token; max(p - q, 0)
-struct Exponent {            // of 2, in two parts
+struct Exponent {            // of 2, in two parts, the second times ln 2
     float high, low;
 };
 struct Position {

@@ -23,11 +23,11 @@ __device__ __forceinline__ float share(float z, float ref, float c) { return exp
 // small, whatever its parts are, and so is its rounding.  The second takes no part where it is small against a distance without end.)
 __device__ __forceinline__ float mass(float z, float ref, Factor c, Exponent e) {
     const float d = z - ref, x = exp2_hw(fmaf(d, c.c, e.high));
-    return fmaf(x, fmaf(fmaxf(d, -1000.0f), c.low, e.low) * 0.693147181f, x);
+    return fmaf(x, fmaf(fmaxf(d, -1000.0f), c.low * 0.693147181f, e.low), x);
 }
 __device__ __forceinline__ Exponent exponent_of(double log) {       // of e to one of 2
     const double x = log * 1.44269504088896340736;
-    return {(float)x, (float)(x - (double)(float)x)};
+    return {(float)x, (float)((x - (double)(float)x) * 0.69314718055994530942)};
 }
 
 // A row as it is read in blocks: chunks of 16 bytes on boundaries of the logits, of which the first and the last may hold less of the row.
@@ -432,13 +432,13 @@ __device__ __forceinline__ void blanks(const VerifyArgs& a, int64_t i, int from,
     }
 }
 
-// max(p - q, 0) of a chunk.  (A difference that is no number stays one, and p is drawn from instead.)
+// max(p - q, 0) of a chunk.  (A difference that is no number, or without end, makes one that is none, and p is drawn from instead.)
 template <typename T>
 __device__ __forceinline__ void rest_of(const VerifyArgs& a, const Position& d, typename Line<T>::vec p, typename Line<T>::vec q, float (&v)[Line<T>::E]) {
 #pragma unroll
     for (int e = 0; e < Line<T>::E; ++e) {
-        const float at_q = mass((float)q[e], d.q_ref, a.draft_c, d.q), r = mass((float)p[e], d.top, a.c, d.p) - at_q;
-        v[e] = !(at_q < INFINITY) ? NAN : (r <= 0.0f ? 0.0f : r);
+        const float r = mass((float)p[e], d.top, a.c, d.p) - mass((float)q[e], d.q_ref, a.draft_c, d.q);
+        v[e] = r > 0.0f ? r : r * 0.0f;
     }
 }
 
@@ -473,25 +473,29 @@ __device__ __forceinline__ void finish(const VerifyArgs& a, int64_t i, int t, co
     }
 }
 
-// Sums of max(p - q, 0) over a block's chunks of 64 lanes, by one wave: put(number, sum).  (Finer than the blocks: the one wave that finds the token
-// has a chunk to go through then.)
+// Sums of max(p - q, 0) over 64 chunks each, number first, first + step, ... < end, by one wave, two of them at once: put(number, sum).  (Finer than the
+// blocks: the work spreads, and the one wave that finds the token has 64 chunks to go through.)
+constexpr int kRestAtOnce = 2;
 template <typename T, typename Put>
-__device__ __forceinline__ void sum_rest(const VerifyArgs& a, const Position& d, const Line<T>& line, const T* drow, int b, Put put) {
+__device__ __forceinline__ void sum_rest(const VerifyArgs& a, const Position& d, const Line<T>& line, const T* drow, int first, int end, int step, Put put) {
     typedef Line<T> L;
-    typename L::vec p[L::kLoads], q[L::kLoads];
     const int lane = threadIdx.x & 63;
-    line.fetch(b, lane, p);
+    for (int n = first; n < end; n += kRestAtOnce * step) {
+        typename L::vec p[kRestAtOnce], q[kRestAtOnce];
 #pragma unroll
-    for (int k = 0; k < L::kLoads; ++k) q[k] = line.beside(drow, L::chunk(b, k, lane));
-    line.mend(b, lane, p);
+        for (int k = 0; k < kRestAtOnce; ++k) {
+            p[k] = line.beside(line.row, (n + k * step) * 64 + lane);
+            q[k] = line.beside(drow, (n + k * step) * 64 + lane);
+        }
 #pragma unroll
-    for (int k = 0; k < L::kLoads; ++k) {
-        float v[L::E], sum = 0.0f;
-        rest_of<T>(a, d, p[k], q[k], v);
+        for (int k = 0; k < kRestAtOnce; ++k) {
+            float v[L::E], sum = 0.0f;
+            rest_of<T>(a, d, p[k], q[k], v);
 #pragma unroll
-        for (int e = 0; e < L::E; ++e) sum += v[e];
-        const double all = wave_sum((double)sum);
-        if (lane == 0) put(b * L::kLoads + k, all);
+            for (int e = 0; e < L::E; ++e) sum += v[e];
+            const double all = wave_sum((double)sum);
+            if (lane == 0 && n + k * step < end) put(n + k * step, all);
+        }
     }
 }
 
@@ -539,7 +543,7 @@ __global__ __launch_bounds__(1024) void k_verify_requests(VerifyArgs a, int64_t 
     if (d.mode == kRest) {
         const Line<T> line(row_of<T>(a.target, i, t), a.vocab);
         const T* drow = row_of<T>(a.draft, i, t);
-        for (int b = wave; b < line.blocks(); b += waves) sum_rest<T>(a, d, line, drow, b, [&](int k, double s) { rest[k] = s; });
+        sum_rest<T>(a, d, line, drow, wave, line.blocks() * Line<T>::kLoads, waves, [&](int k, double s) { rest[k] = s; });
         __syncthreads();
     }
     if (wave == 0) finish<T>(a, i, t, d, sums, [&](int k) { return rest[k]; });
@@ -625,8 +629,8 @@ __global__ __launch_bounds__(kRestWaves * 64) void k_verify_rest(VerifyArgs a, i
     double* sums = rest + i * most * Line<T>::kLoads;
     const Line<T> line(row_of<T>(a.target, i, t), a.vocab);
     const T* drow = row_of<T>(a.draft, i, t);
-    const int blocks = line.blocks(), each = (blocks + pieces - 1) / pieces, end = min((piece + 1) * each, blocks);
-    for (int b = piece * each + wave; b < end; b += kRestWaves) sum_rest<T>(a, d, line, drow, b, [&](int k, double s) { publish(&sums[k], s); });
+    const int all = line.blocks() * Line<T>::kLoads, each = (all + pieces - 1) / pieces;
+    sum_rest<T>(a, d, line, drow, piece * each + wave, min((piece + 1) * each, all), kRestWaves, [&](int k, double s) { publish(&sums[k], s); });
     if (!arrive_is_last(&tickets[i], &last, (unsigned)pieces)) return;
     if (wave == 0) finish<T>(a, i, t, d, table, [&](int k) { return observe(&sums[k]); });
 }
@@ -704,7 +708,7 @@ hipError_t verify_rows(const VerifyArgs& a, void* ws, hipStream_t st) {
         hipLaunchKernelGGL(k_verify_sums<T>, dim3((unsigned)(c * pieces)), dim3(kDrawBlock), 0, st, a, first, pieces, most, target, draft, asked, tickets);
     });
     if (e != hipSuccess) return e;
-    pieces = a.draft.z ? pieces_of(n, most, kRestWaves, 2048) : 1;
+    pieces = a.draft.z ? pieces_of(n, most * Line<T>::kLoads / kRestAtOnce, kRestWaves, 2048) : 1;
     return in_launches(n, pieces, [&](int64_t first, int64_t c) {
         hipLaunchKernelGGL(k_verify_rest<T>, dim3((unsigned)(c * pieces)), dim3(kRestWaves * 64), 0, st, a, first, pieces, most, (const BlockSum*)target,
                            (const BlockSum*)draft, (const Asked*)asked, rest, tickets);

@@ -92,7 +92,7 @@ struct Shape {
     int row_waves, step_waves;
     int chunk_log2;          // steps of x that are in LDS at a time: at least one for each of the waves that share them
 };
-constexpr int row_waves_of(int T) { return T == 1 ? 1 : 4; }
+constexpr int row_waves_of(int T) { return T == 1 ? 1 : 4; }     // the least
 
 // x as operands, step by step, in units of 16 bytes (eight columns of a row): for each of a step's four instructions its four such, and for each of those the
 // rows one behind the other, so that 16 lanes read 256 bytes.  A 32-bit x is three planes of that.  Where x is laid out beforehand the rows are filled up to
@@ -398,8 +398,7 @@ __global__ __launch_bounds__(512, T > 1 || (!WHOLE && sizeof(X) == 4) ? 2 : (WHO
 }
 
 template <typename X, typename S, int G, int NT, int T, bool WHOLE>
-hipError_t matvec4_in(const Matvec4Args& a, int step_waves, hipStream_t st) {
-    constexpr int row_waves = row_waves_of(T);
+hipError_t matvec4_in(const Matvec4Args& a, int row_waves, int step_waves, hipStream_t st) {
     const int64_t units = a.w.blocks() * (4 / NT), steps = a.w.steps();
     const int have = a.tokens < 16 * T ? (int)a.tokens : 16 * T;
     while (step_waves > steps) step_waves /= 2;
@@ -438,18 +437,30 @@ int64_t whole_bytes(const Packed4& w, int64_t tokens) { return tokens * w.steps(
 
 template <typename X, typename S, int G>
 hipError_t matvec4(const Matvec4Args& a, hipStream_t st) {
-    const bool wide = a.w.blocks() >= 256;
     const int T = tiles_of(a.tokens, sizeof(X));
     const int64_t whole = T == 1 ? whole_bytes<X>(a.w, a.tokens) : 0;
-    if (T == 1 && whole <= kWholeBytes)
-        return wide ? matvec4_in<X, S, G, G == 1 ? 2 : 4, 1, true>(a, whole <= kWholeBytes / 2 ? 4 : 8, st) : matvec4_in<X, S, G, 1, 1, true>(a, 8, st);
-    if (T == 1) return wide ? matvec4_in<X, S, G, G == 1 ? 2 : 4, 1, false>(a, 4, st) : matvec4_in<X, S, G, 1, 1, false>(a, 8, st);
-    // (us for 65536 x 4096, groups of 128, two / four tiles of the weights to a wave: 32 rows of bf16 40.3 / 43.8, of f32 78 / 67, 48 of bf16 48.5 / 52.7,
-    // 64 73 / 61; and the 48 with four tiles of x 57)
-    if (T == 2) return wide ? matvec4_in<X, S, G, sizeof(X) == 2 || G == 1 ? 2 : 4, 2, false>(a, 2, st) : matvec4_in<X, S, G, 1, 2, false>(a, 2, st);
+    if (T == 1) {
+        // More than one row of x is brought to LDS for two blocks of W at once, where that leaves a workgroup for every compute unit.  us, one / two:
+        // 8 rows of bf16 x 65536 x 4096 41 / 32, 16 38.1 / 37.0, 5 of f16 x 50021 x 2600 21.3 / 19.9, 3 of f32 x 32768 x 2048 18.1 / 16.6, but one of
+        // bf16 x 131072 x 4096 44.8 / 45.5 and 4 x 16384 x 4096 12.4 / 13.7, which eight waves take in 11.2.
+        const bool many = a.w.blocks() >= 512;
+        const int beside = a.tokens > 1 && many ? 2 : 1, share = beside == 1 && (!many || whole > kWholeBytes / 2) ? 8 : 4;
+        const bool wide = a.w.blocks() >= 256;
+        constexpr int NT = G == 1 ? 2 : 4;
+        if (whole <= kWholeBytes) return wide ? matvec4_in<X, S, G, NT, 1, true>(a, beside, share, st) : matvec4_in<X, S, G, 1, 1, true>(a, 1, 8, st);
+        return wide ? matvec4_in<X, S, G, NT, 1, false>(a, beside, share, st) : matvec4_in<X, S, G, 1, 1, false>(a, 1, 8, st);
+    }
+    // Tiles of the weights to a wave: more of them read less of x, fewer leave more workgroups.  us for rows of W x 4096, groups of 128, one / two / four tiles:
+    //            8192              16384             32768             65536
+    // 32 bf16    19.4 / 26.0       20.5 / 26.7       27.2 / 29.1       48.0 / 38.7 / 43.8
+    // 48 bf16    24.9 / 30.3       25.9 / 31.3       35.2 / 33.5       59.5 / 45.8 / 52.7
+    // 64 bf16    26.9 / 37.6 / 54  28.3 / 38.5 / 55  39.1 / 41.5 / 56  68.0 / 74.1 / 60.7
+    // 32 f32     31.0 / - / 57     32.6 / - / 57     57.3 / - / 59     107 / 78 / 66.8
+    const bool large = a.w.blocks() >= 768;
+    if (T == 2) return large ? matvec4_in<X, S, G, sizeof(X) == 2 || G == 1 ? 2 : 4, 2, false>(a, 4, 2, st) : matvec4_in<X, S, G, 1, 2, false>(a, 4, 2, st);
     if constexpr (sizeof(X) == 2) {
-        if (T == 3) return wide ? matvec4_in<X, S, G, 2, 3, false>(a, 2, st) : matvec4_in<X, S, G, 1, 3, false>(a, 2, st);
-        return wide ? matvec4_in<X, S, G, G == 4 ? 4 : 2, 4, false>(a, 2, st) : matvec4_in<X, S, G, 1, 4, false>(a, 2, st);
+        if (T == 3) return a.w.blocks() >= 512 ? matvec4_in<X, S, G, 2, 3, false>(a, 4, 2, st) : matvec4_in<X, S, G, 1, 3, false>(a, 4, 2, st);
+        return large ? matvec4_in<X, S, G, G == 4 ? 4 : 2, 4, false>(a, 4, 2, st) : matvec4_in<X, S, G, 1, 4, false>(a, 4, 2, st);
     }
     return hipErrorInvalidValue;
 }

@@ -73,7 +73,8 @@ def test_products(tokens, rows, cols, x_type, scale_type):
 
 
 # x in LDS as a whole, at its largest and past it, and laid out beforehand; few rows of weights and many; tiles of x by their number
-LONG = [(16, 70, 2560), (16, 70, 2570), (9, 80, 5000), (12, 16390, 2700), (40, 16390, 300), (50, 16390, 300), (70, 16390, 200), (130, 100, 260)]
+LONG = [(16, 70, 2560), (16, 70, 2570), (9, 80, 5000), (12, 16390, 2700), (40, 32800, 130), (20, 49200, 130),
+        (50, 49200, 130), (70, 49200, 64), (6, 33000, 200), (130, 100, 260)]
 
 
 @pytest.mark.parametrize("x_type,scale_type", [("f32", "f32"), ("bf16", "f16"), ("f16", "bf16")])

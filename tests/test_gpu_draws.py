@@ -346,6 +346,25 @@ def test_positions_that_lie_anywhere(n):
         check_verify(got, z, x, u, v, draft=zq, draft_logp=None if logp is None else lq)
 
 
+def test_the_drafters_temperature_is_the_targets_unless_given():
+    z, zq, x, lq, u, v = (t.to(DEV) for t in drafts_of(6, 3, 400, torch.float32, seed=15))
+    a = L.verify_draft(z, x, u, v, draft_logits=zq, temperature=0.7)
+    b = L.verify_draft(z, x, u, v, draft_logits=zq, temperature=0.7, draft_temperature=0.7)
+    c = L.verify_draft(z, x, u, v, draft_logits=zq, temperature=0.7, draft_temperature=1.0)
+    assert all(torch.equal(p, q) for p, q in zip(a, b)) and not torch.equal(a.logp, c.logp)
+
+
+def test_results_carry_no_history_and_inference_mode_is_no_matter():
+    z, zq, x, lq, u, v = (t.to(DEV) for t in drafts_of(6, 3, 400, torch.float32, seed=16))
+    plain = L.verify_draft(z, x, u, v, draft_logits=zq, draft_logp=lq), L.draw_tokens(z[:, 0], v)
+    z.requires_grad_()
+    for got in (L.verify_draft(z, x, u, v, draft_logits=zq, draft_logp=lq), L.draw_tokens(z[:, 0], v)):
+        assert not any(t.requires_grad for t in got)
+    with torch.inference_mode():
+        again = L.verify_draft(z, x, u, v, draft_logits=zq, draft_logp=lq), L.draw_tokens(z[:, 0], v)
+    assert all(torch.equal(p, q) for a, b in zip(plain, again) for p, q in zip(a, b))
+
+
 def test_no_drafts_is_a_draw():
     z, u = logits_of((7, 1, 3000), torch.float16).to(DEV), numbers(7).to(DEV)
     none = torch.empty(7, 0, dtype=torch.int64, device=DEV)

@@ -238,6 +238,58 @@ def test_refusals():
         L.matvec4(store, w, out=store[:, :64])
 
 
+def test_history_inference_mode_and_a_result_that_was_kept():
+    codes, scale, z = plain(200, 256, 64, torch.float32, True)
+    w = packed(codes, scale, z, 256, 64)
+    x = torch.randn(20, 256, device=DEV, generator=torch.Generator(DEV).manual_seed(9))
+    want = L.matvec4(x, w)
+    assert not L.matvec4(x.clone().requires_grad_(), w).requires_grad
+    with torch.inference_mode():
+        out = torch.empty(20, 200, device=DEV)
+        assert torch.equal(L.matvec4(x, w, out=out), want)
+    # a way back that kept the tensor which is written over is refused, as after any operation in place
+    leaf = torch.ones(20, 200, device=DEV, requires_grad=True)
+    kept = torch.tanh(leaf)
+    loss = kept.sum()
+    L.matvec4(x, w, out=kept.detach())
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+
+
+def test_calls_on_two_streams_at_once():
+    """With a workspace each: x is laid out there."""
+    codes, scale, z = plain(3000, 512, 128, torch.float16, True)
+    w = packed(codes, scale, z, 512, 128)
+    xs = [torch.randn(40, 512, device=DEV, generator=torch.Generator(DEV).manual_seed(k)).half() for k in range(2)]
+    want = [L.matvec4(x, w) for x in xs]
+    streams = [torch.cuda.Stream() for _ in xs]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for k, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                got[k].append(L.matvec4(xs[k], w))
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, want[k]) for k in range(2) for g in got[k])
+
+
+@pytest.mark.parametrize("tokens", [17, 40, 64])
+def test_a_replayed_graph_of_more_rows(tokens):
+    codes, scale, z = plain(500, 300, 32, torch.bfloat16, False)
+    w = packed(codes, scale, z, 300, 32)
+    x = torch.zeros(tokens, 300, device=DEV, dtype=torch.bfloat16)
+    L.matvec4(x, w)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = L.matvec4(x, w)
+    for seed in range(4):
+        x.copy_(torch.randn(tokens, 300, device=DEV, generator=torch.Generator(DEV).manual_seed(seed)))
+        graph.replay()
+        want = L.matvec4(x, w)
+        torch.cuda.synchronize()
+        assert torch.equal(y, want)
+
+
 def test_a_replayed_graph_and_another_stream():
     codes, scale, z = plain(1000, 512, 128, torch.float16, True)
     w = packed(codes, scale, z, 512, 128)

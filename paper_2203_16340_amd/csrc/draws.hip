@@ -574,7 +574,7 @@ __global__ __launch_bounds__(kDrawBlock) void k_verify_sums(VerifyArgs a, int64_
 
 // The first token of a request that is not accepted, the sums of max(p - q, 0) there, and its last token.  Every workgroup finds out the first
 // for itself, and the last to be done the third (the sums are read in their own order, whichever that is): a launch each less.  32 requests of 4
-// drafts x 131072 bf16 14 us behind 11 for the sums (42 MB): seven trips to memory one behind the other.
+// drafts x 131072 bf16 12 us behind 11 for the sums (42 MB): trips to memory one behind the other, not bytes (11 MB).
 constexpr int kRestWaves = 8;            // of a workgroup: as many positions are judged at once
 template <typename T>
 __global__ __launch_bounds__(kRestWaves * 64) void k_verify_rest(VerifyArgs a, int64_t first, int pieces, int64_t most, const BlockSum* target,

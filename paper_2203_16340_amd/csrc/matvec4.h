@@ -81,11 +81,19 @@ struct Parts<float> {
     }
 };
 
-// NT scales that stand side by side
+// NT scales that stand side by side.  As uint16_t they are the bits of bf16 or f16, and which is asked at each, two instructions more: one kernel for both where
+// x is laid out, which the compiler takes a third less time for (65536 x 4096 with 48 rows 52.1 us, with kernels of their own 50.2).  Where x is in LDS
+// from the start each type has its own (one row with 131072 x 4096 43.9 us for 44.6, 5 with 50021 x 2600 17.5 for 18.0).
 template <typename S, int NT>
 struct Scales {
     typedef S vec __attribute__((ext_vector_type(NT)));
 };
+template <typename S>
+__device__ __forceinline__ float scale_of(S s, bool) { return (float)s; }
+template <>
+__device__ __forceinline__ float scale_of<uint16_t>(uint16_t s, bool bf16) {
+    return bf16 ? __builtin_bit_cast(float, (uint32_t)s << 16) : (float)__builtin_bit_cast(_Float16, s);
+}
 
 // What a launch is made of: waves of a workgroup that take rows beside each other, and waves that share their steps.
 struct Shape {
@@ -165,7 +173,7 @@ __device__ __forceinline__ void bring_by(const Matvec4Args& a, int64_t x0, int r
         }
     }
 }
-// (Two at a time, 50021 x 2600 with 5 rows of f16 would wait four times, and four at a time twice: 20.8 us, with eight 19.8.  But eight where there are
+// (With a block of W to a workgroup, 50021 x 2600 with 5 rows of f16 waited four times two at a time, and twice four at a time: 20.8 us, with eight 19.8.  But eight where there are
 // two cost 131072 x 4096 with one row 47.9 us for 44.9.)
 template <typename X>
 __device__ __forceinline__ void bring_whole(const Matvec4Args& a, int64_t x0, int rows, typename Operand<typename OperandOf<X>::type>::vec* lds) {
@@ -228,7 +236,7 @@ __global__ __launch_bounds__(256) void k_operands4(Matvec4Args a) {
 // fewer rows the rest of the operand is anything, and what comes of it is not looked at.
 // S: the scales' type.  WHOLE: all of x is in LDS from the start, and x has up to 16 rows.
 // One row with 131072 x 4096 takes 43.8 us, 6.3 TB/s (loads without products 42.8).  Below some 100 MB it is what comes before the first product and behind the
-// last that counts, 7 to 9 us: 50021 x 2600 with 5 rows 18.9 (loads alone 16.3).  65536 x 4096 with 48 rows 47 behind k_operands4's 3.3: LDS, 24 000 of
+// last that counts, 7 to 9 us: 50021 x 2600 with 5 rows 17.5.  65536 x 4096 with 48 rows 47 behind k_operands4's 3.3: LDS, 24 000 of
 // 100 000 cycles, and waits at its barriers.
 template <typename X, typename S, int G, int NT, int T, bool WHOLE>    // G: matrix instructions between two groups, 1, 2 or 4
 __global__ __launch_bounds__(512, T > 1 || (!WHOLE && sizeof(X) == 4) ? 2 : (WHOLE && (G != 2 || sizeof(S) + sizeof(X) < 6) ? 4 : 3)) void k_matvec4(Matvec4Args a, Shape shape) {
@@ -249,6 +257,7 @@ __global__ __launch_bounds__(512, T > 1 || (!WHOLE && sizeof(X) == 4) ? 2 : (WHO
     const char* codes = (const char*)a.packed + (size_t)block * steps * kStepBytes + tile * kTileBytes + lane * 16;
     const S* scales = (const S*)((const char*)a.packed + a.w.code_bytes()) + (size_t)block * groups * kBlockRows * (1 + a.w.zeros) + 4 * c + tile;
     const int each = kBlockRows * (1 + a.w.zeros);
+    const bool bf16 = a.w.scale_type == LBFGSB_BF16;
 
     f4 y[NT][T];
 #pragma unroll
@@ -315,7 +324,7 @@ __global__ __launch_bounds__(512, T > 1 || (!WHOLE && sizeof(X) == 4) ? 2 : (WHO
                     const f4 all = WHOLE ? all1 : totals[(g * T + u) * 4 + kq];
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
-                        const float scale = (float)st.scale[g][t], zero = a.w.zeros ? (float)st.zero[g][t] : 8.0f;
+                        const float scale = scale_of(st.scale[g][t], bf16), zero = a.w.zeros ? scale_of(st.zero[g][t], bf16) : 8.0f;
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
                             if (T > 1 || r == 0 || have > 4) y[t][u][r] = fmaf(scale, fmaf(-zero, all[r], sum[t][u][r]), y[t][u][r]);
@@ -447,7 +456,14 @@ hipError_t matvec4(const Matvec4Args& a, hipStream_t st) {
         const int beside = a.tokens > 1 && many ? 2 : 1, share = beside == 1 && (!many || whole > kWholeBytes / 2) ? 8 : 4;
         const bool wide = a.w.blocks() >= 256;
         constexpr int NT = G == 1 ? 2 : 4;
-        if (whole <= kWholeBytes) return wide ? matvec4_in<X, S, G, NT, 1, true>(a, beside, share, st) : matvec4_in<X, S, G, 1, 1, true>(a, 1, 8, st);
+        if (whole <= kWholeBytes && wide) {
+            if constexpr (sizeof(S) == 2)
+                return a.w.scale_type == LBFGSB_BF16 ? matvec4_in<X, __bf16, G, NT, 1, true>(a, beside, share, st)
+                                                     : matvec4_in<X, _Float16, G, NT, 1, true>(a, beside, share, st);
+            else
+                return matvec4_in<X, S, G, NT, 1, true>(a, beside, share, st);
+        }
+        if (whole <= kWholeBytes) return matvec4_in<X, S, G, 1, 1, true>(a, 1, 8, st);
         return wide ? matvec4_in<X, S, G, NT, 1, false>(a, beside, share, st) : matvec4_in<X, S, G, 1, 1, false>(a, 1, 8, st);
     }
     // Tiles of the weights to a wave: more of them read less of x, fewer leave more workgroups.  us for rows of W x 4096, groups of 128, one / two / four tiles:
@@ -482,8 +498,7 @@ size_t matvec4_space(const Packed4& w, int64_t tokens) {
 
 template <typename X>
 hipError_t matvec4_of(const Matvec4Args& a, hipStream_t st) {
-    return a.w.scale_type == LBFGSB_F32 ? matvec4_by_group<X, float>(a, st)
-                                        : (a.w.scale_type == LBFGSB_BF16 ? matvec4_by_group<X, __bf16>(a, st) : matvec4_by_group<X, _Float16>(a, st));
+    return a.w.scale_type == LBFGSB_F32 ? matvec4_by_group<X, float>(a, st) : matvec4_by_group<X, uint16_t>(a, st);
 }
 
 }  // namespace lb

@@ -82,7 +82,7 @@ struct Parts<float> {
 };
 
 // NT scales that stand side by side.  As uint16_t they are the bits of bf16 or f16, and which is asked at each, two instructions more: one kernel for both where
-// x is laid out, which the compiler takes a third less time for (65536 x 4096 with 48 rows 52.1 us, with kernels of their own 50.2).  Where x is in LDS
+// x is laid out, which the compiler takes a third less time for (65536 x 4096 with 48 rows 50.3 us, with kernels of their own 50.2).  Where x is in LDS
 // from the start each type has its own (one row with 131072 x 4096 43.9 us for 44.6, 5 with 50021 x 2600 17.5 for 18.0).
 template <typename S, int NT>
 struct Scales {

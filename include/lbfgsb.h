@@ -543,7 +543,7 @@ int lbfgsb_pack4(const lbfgsb_weights4* weights_host, void* packed, size_t packe
 
 /* y = x W^T: x is `tokens` rows of weights_host->cols entries of x_type, y as many rows of weights_host->rows entries of y_type
  * (LBFGSB_F32 or x_type), ld_x and ld_y elements apart; rows may start on any element.  packed (16-byte aligned) is what lbfgsb_pack4
- * made of these weights; of the struct the sizes, scale_type and whether zero is NULL are read.  Made for a few tokens: every 64 of them (32 where x is
+ * made of these weights, lbfgsb_packed4_bytes of it (its size is not passed, so nothing here can check it); of the struct the sizes, scale_type and whether zero is NULL are read.  Made for a few tokens: every 64 of them (32 where x is
  * F32) read the weights once more.  tokens = 0 is allowed.  The workspace goes by lbfgsb_matvec4_workspace_bytes, as for the losses (0 for few and short rows).
  * Products are exact, sums in 32 bits, the result is rounded once.  y_r is not finite (NaN or infinite) where x_r holds NaN or infinity, or where
  * |x_r| over a group adds up past 2^124.  y must not overlap x or packed. */

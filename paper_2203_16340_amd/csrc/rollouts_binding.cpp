@@ -61,11 +61,23 @@ auto pack4(const Tensor& codes, const Tensor& scale, const Maybe& zero, int64_t 
     return std::make_tuple(rc, packed, type);
 }
 
+// Whether the tensor holds what the products read of weights of these sizes (lbfgsb_matvec4 has only its address).  False: the sizes are of no weights.
+bool holds(const Tensor& packed, const lbfgsb_weights4& w) {
+    const size_t need = lbfgsb_packed4_bytes(&w);
+    if (need == 0) return false;
+    if (packed.scalar_type() != at::kByte || !packed.is_contiguous()) throw py::type_error("the packed weights must be a contiguous Byte tensor");
+    if ((size_t)packed.numel() < need)
+        throw py::value_error("the packed weights must have " + std::to_string(need) + " bytes for their rows, cols, group, scales and zeros, got " +
+                              std::to_string(packed.numel()));
+    return true;
+}
+
 auto matvec4(const Tensor& x, const Tensor& packed, int64_t rows, int64_t cols, int64_t group, int scale_type, bool zero, py::object dtype,
              const Maybe& out, int64_t stream) {
+    const lbfgsb_weights4 w = weights_of(rows, cols, group, scale_type, zero);
+    if (!holds(packed, w)) return std::make_tuple((int)LBFGSB_E_INVALID_ARG, Tensor());
     const int x_type = logit_type(x, "x");
     const at::Device dev = x.device();
-    const lbfgsb_weights4 w = weights_of(rows, cols, group, scale_type, zero);
     if (x.size(1) != cols) throw py::value_error("x must have " + std::to_string(cols) + " columns, got " + std::to_string(x.size(1)));
     if (packed.device() != dev) throw py::type_error("x and the weights must be on the same device");
     Tensor y;

@@ -49,7 +49,7 @@ class Codes4(NamedTuple):
 
 class Weights4:
     """Weights of 4 bits as matvec4 reads them (pack4 makes them): `rows` outputs, `cols` inputs, a scale (and zero) for every `group`
-    columns of a row."""
+    columns of a row.  A `packed` that was stored is given back with the same numbers; matvec4 refuses one that is too short for them."""
 
     def __init__(self, packed, rows: int, cols: int, group: int, scale_type: int, has_zero: bool):
         self.packed, self.rows, self.cols, self.group = packed, rows, cols, group

@@ -131,8 +131,12 @@ struct Chunk {
 // ---- statistics of a softmax -----------------------------------------------------------------------------------------
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 // (how far below the maximum, in powers of two: no further than counts, so that 0 times it is 0; -infinity - -infinity, which is
-// no number, ends here as well)
-__device__ __forceinline__ float below(float m, float top, Factor c) { return fmaxf(c(m - top), -1000.0f); }
+// no number, ends here as well.  The factor's second part counts only where the first has told that the distance does: times one to the type's
+// lowest value it may be past the end, to the other side)
+__device__ __forceinline__ float below(float m, float top, Factor c) {
+    const float d = m - top;
+    return d * c.c > -1000.0f ? fmaxf(c(d), -1000.0f) : -1000.0f;
+}
 __device__ __forceinline__ Stat rescaled(Stat a, float top, Factor c) {
     const float d = below(a.m, top, c), f = exp2_hw(d);
     return {top, a.s * f, (a.t + d * a.s) * f};

@@ -635,7 +635,7 @@ __global__ __launch_bounds__(kRestWaves * 64) void k_verify_rest(VerifyArgs a, i
     if (wave == 0) finish<T>(a, i, t, d, table, [&](int k) { return observe(&sums[k]); });
 }
 
-constexpr int64_t kWorkgroupsMax = 1 << 22;      // of a launch (which takes fewer than 2^32 threads): longer batches take several
+constexpr int64_t kThreadsMax = (1ll << 32) - 1;      // of a launch: longer batches take several
 
 // Pieces of each of `rows` rows: enough workgroups to fill the card, as far as each of their waves has a block.
 int pieces_of(int64_t rows, int64_t blocks, int waves, int64_t workgroups) {
@@ -643,10 +643,10 @@ int pieces_of(int64_t rows, int64_t blocks, int waves, int64_t workgroups) {
     return (int)(want < most ? want : most);
 }
 
-// f(first, count): workgroups of `each` for rows first .. first + count - 1
+// f(first, count): `each` workgroups of so many threads for each of the rows first .. first + count - 1
 template <typename F>
-hipError_t in_launches(int64_t rows, int64_t each, F f) {
-    const int64_t most = kWorkgroupsMax / each;
+hipError_t in_launches(int64_t rows, int64_t each, int64_t threads, F f) {
+    const int64_t most = kThreadsMax / (each * threads);
     for (int64_t r = 0; r < rows; r += most) {
         f(r, rows - r < most ? rows - r : most);
         const hipError_t e = hipGetLastError();
@@ -674,7 +674,7 @@ hipError_t draw_rows(const DrawArgs& a, void* ws, hipStream_t st) {
     const int64_t most = blocks_of(a.vocab, sizeof(T));
     const int waves = row_waves(a.rows, most);
     if (waves)
-        return in_launches(a.rows, 1, [&](int64_t first, int64_t n) {
+        return in_launches(a.rows, 1, waves * 64, [&](int64_t first, int64_t n) {
             hipLaunchKernelGGL(k_draw_rows<T>, dim3((unsigned)n), dim3(waves * 64), most * sizeof(BlockSum), st, a, first);
         });
     const int pieces = pieces_of(a.rows, most, kDrawWaves, 2048);
@@ -692,7 +692,7 @@ hipError_t verify_rows(const VerifyArgs& a, void* ws, hipStream_t st) {
     const bool both = a.draft.z && !a.draft_logp;
     if (by_request(n)) {
         const int64_t want = most * (both ? 2 : 1), waves = want < 16 ? want : 16;      // (of 4 kB each: a compute unit's share of the card)
-        return in_launches(n, 1, [&](int64_t first, int64_t c) {
+        return in_launches(n, 1, waves * 64, [&](int64_t first, int64_t c) {
             hipLaunchKernelGGL(k_verify_requests<T>, dim3((unsigned)c), dim3((unsigned)waves * 64), most * (a.draft.z ? 1 + kBlockBytes / 1024 : 1) * sizeof(BlockSum), st, a, first, most);
         });
     }
@@ -704,12 +704,12 @@ hipError_t verify_rows(const VerifyArgs& a, void* ws, hipStream_t st) {
     unsigned* tickets = (unsigned*)(at + sp.tickets);
     const int64_t rows = n * a.target.each + (both ? n * a.draft.each : 0);
     int pieces = pieces_of(rows, most, kDrawWaves, 4096);
-    hipError_t e = in_launches(rows, pieces, [&](int64_t first, int64_t c) {
+    hipError_t e = in_launches(rows, pieces, kDrawBlock, [&](int64_t first, int64_t c) {
         hipLaunchKernelGGL(k_verify_sums<T>, dim3((unsigned)(c * pieces)), dim3(kDrawBlock), 0, st, a, first, pieces, most, target, draft, asked, tickets);
     });
     if (e != hipSuccess) return e;
     pieces = a.draft.z ? pieces_of(n, most * Line<T>::kLoads / kRestAtOnce, kRestWaves, 2048) : 1;
-    return in_launches(n, pieces, [&](int64_t first, int64_t c) {
+    return in_launches(n, pieces, kRestWaves * 64, [&](int64_t first, int64_t c) {
         hipLaunchKernelGGL(k_verify_rest<T>, dim3((unsigned)(c * pieces)), dim3(kRestWaves * 64), 0, st, a, first, pieces, most, (const BlockSum*)target,
                            (const BlockSum*)draft, (const Asked*)asked, rest, tickets);
     });

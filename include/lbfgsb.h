@@ -545,7 +545,8 @@ int lbfgsb_pack4(const lbfgsb_weights4* weights_host, void* packed, size_t packe
  * (LBFGSB_F32 or x_type), ld_x and ld_y elements apart; rows may start on any element.  packed (16-byte aligned) is what lbfgsb_pack4
  * made of these weights, lbfgsb_packed4_bytes of it (its size is not passed, so nothing here can check it); of the struct the sizes, scale_type and whether zero is NULL are read.  Made for a few tokens: every 64 of them (32 where x is
  * F32) read the weights once more.  tokens = 0 is allowed.  The workspace goes by lbfgsb_matvec4_workspace_bytes, as for the losses (0 for few and short rows).
- * Products are exact, sums in 32 bits, the result is rounded once.  y_r is not finite (NaN or infinite) where x_r holds NaN or infinity, or where
+ * Products of codes and x are exact (of an x in F32, what lies below 2^-126 may be lost), sums in 32 bits, the result is rounded once.  A zero's part is
+ * taken from a group's sum, so the roundings are of sum |scale| (code + |zero|) |x|, not of sum |w| |x|.  y_r is not finite (NaN or infinite) where x_r holds NaN or infinity, or where
  * |x_r| over a group adds up past 2^124.  y must not overlap x or packed. */
 int lbfgsb_matvec4(const lbfgsb_weights4* weights_host, const void* packed, int64_t tokens, int x_type, int64_t ld_x, const void* x,
                    int y_type, int64_t ld_y, void* y, void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -556,7 +556,8 @@ size_t lbfgsb_matvec4_workspace_bytes(const lbfgsb_weights4* weights_host, int64
  *     token = the smallest j with p_0 + ... + p_j > u,   logp = log p_token.
  * A masked entry (-infinity) is never drawn; one of less than 2^-100 of the row's largest may count as 0.  u below 0 counts as 0, 1 and above as
  * the last number below 1.  A row without a distribution (all -infinity; NaN or +infinity in it), and one with u = NaN, gives token -1 and logp NaN.
- * The sums are good for 2e-7: a u that is nearer than that to a token's border may give its neighbour.  vocab <= 2^21; grad is not
+ * p, its running sums and logp are off by less than 4e-6 (of themselves; logp absolutely, and rounded once): a u that is nearer than that to a token's border
+ * may give its neighbour.  Most is lost where the mass lies in a long tail of equal entries: 3e-7 of a running sum, 2e-6 of logp.  vocab <= 2^21; grad is not
  * looked at.  The workspace goes by the size that lbfgsb_draw_workspace_bytes gives, as for the losses. */
 size_t lbfgsb_draw_workspace_bytes(const lbfgsb_logits* logits_host);
 int lbfgsb_draw_tokens(const lbfgsb_logits* logits_host, const float* uniform, int64_t* tokens, float* logp, void* workspace,
@@ -586,6 +587,8 @@ typedef struct {
  * 0 throughout; after all accepted, from p at the position behind them.
  *   draft_z NULL:     q_t = 1 at x_t, 0 elsewhere.
  *   draft_logp given: q_t(j) = exp(draft_logp_t + (draft_z_tj - draft_z_tx) / draft_temperature).
+ * p_t and q_t are off by less than 4e-6 of themselves as well; with draft_logp q_t may be by 2^-24 |draft_logp_t| more.  u_t q_t(x_t) and p_t(x_t) are
+ * compared in 64 bits: below 1e-307 they may count as 0.
  * A drafted token outside the vocabulary, and one whose q_t(x_t) is not finite (its own logit or draft_logp infinite or NaN; without draft_logp: NaN or
  * +infinity anywhere in the drafter's row, or -infinity throughout), counts as q_t = 0: it is not accepted and p_t is drawn from.  With draft_logp the
  * drafter's row is read only where its token is not accepted; if that gives a q_t(j) that is NaN or past 2^127, p_t is drawn from.

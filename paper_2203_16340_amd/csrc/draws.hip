@@ -2,8 +2,11 @@
 //
 // A token is the first entry at which the running sum of p passes u.  With e_j = 2^((z_j - ref) c) a row is read once, in blocks of
 // 4 kB whose sums are kept (8 bytes a block: 0.2 % of the row); in 64 bits the blocks' sums tell the block in which u S is
-// passed, S being the whole row's, and that block alone is read again, lane by lane and entry by entry.  Sums of a block are in 32 bits and off by
-// 2^-24 of the block's own, all else is in 64 bits.
+// passed, S being the whole row's, and that block alone is read again, lane by lane and entry by entry.
+// Exponentials, a block's sum and the weight that brings it to the row's largest are in 32 bits, sums over blocks, the walk and logarithms in 64.  With
+// units of 2^-24: an exponent -a of 2 is off by 2.5 a ln 2 (difference, product, the factor's second part) and what lies there, of 2^21 entries at
+// most, is 2^(21 - a) / (1 + 2^(21 - a)) of the row, so that S is off by 28 at most (a = 17 or 18); the two exponentials by 4, a block's sum of
+// 2048 by 14: 46 units, 2.8e-6.  Measured, at a tail of equal entries that holds most of the row: borders 2.9e-7, log p 2.1e-6.
 //
 // Verification: the same sums tell whether a drafted token is accepted; where the first is not, blocks of max(p - q, 0) are summed and walked through
 // alike.  A workgroup takes a request, position by position; few requests are taken in two launches, sums of all rows and then the rest, by many.
@@ -20,7 +23,8 @@ constexpr int kDrawBlock = 256, kDrawWaves = kDrawBlock / 64;
 // requests of 5 drafts 101 for 93.)
 __device__ __forceinline__ float share(float z, float ref, float c) { return exp2_hw((z - ref) * c); }
 // 2^((z - ref) c + e), with the second parts of both, for differences p - q.  (Where z is the largest's equal or not far from it the first exponent is
-// small, whatever its parts are, and so is its rounding.  The second takes no part where it is small against a distance without end.)
+// small, whatever its parts are, and so is its rounding.  The second takes no part where it is small against a distance without end.  With draft_logp the
+// drafter's ref is the drafted token's logit, which may be far below the largest: what z - ref loses there is 2^-24 of the token's -log q.)
 __device__ __forceinline__ float mass(float z, float ref, Factor c, Exponent e) {
     const float d = z - ref, x = exp2_hw(fmaf(d, c.c, e.high));
     return fmaf(x, fmaf(fmaxf(d, -1000.0f), c.low * 0.693147181f, e.low), x);

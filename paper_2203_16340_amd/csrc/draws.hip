@@ -669,8 +669,14 @@ int row_waves(int64_t rows, int64_t blocks) {
 }
 
 // Whether a request's positions are taken one after another by one workgroup, which then reads no row in vain but goes no faster than its
-// compute unit.  us, so / by many workgroups: 256 requests of 5 drafts x 131072 f16 93 / 126, 256 of 2 x 20000 20 / 24, 200 of 4 x 131072 bf16 with both
-// sides summed 108 / 125, 128 of 4 x 131072 75 / 60, 128 of 4 x 32768 29.5 / 25.5, 2 of 3 x 32768 12.4 / 11.3.
+// compute unit.  us, so / by many workgroups, log-probabilities given where not said:
+//                                  128          144          160          192          256 requests
+// 4 drafts x 131072 bf16           72 / 60      72 / 64      74 / 67      75 / 78      77 / 95
+// the same, both sides summed      103 / 88     104 / 96     104 / 104    106 / 118    113 / 148
+// 5 x 131072 f16                   85 / 68      85 / 74      86 / 79      87 / 94      90 / 111
+// 3 x 50021 f32                    42 / 40      41 / 43      42 / 46      44 / 54      47 / 66
+// 2 x 32768 f16                    19.8 / 19.9  20.3 / 21.0  20.4 / 22.9  21.0 / 25.4  22.7 / 30.1
+// 2 of 3 x 32768 12.4 / 11.3.  They meet between 128 and 190, whatever the drafts and entries are; from 160 on neither is more than a tenth behind where it is taken.
 bool by_request(int64_t requests) { return requests >= 160; }
 
 template <typename T>

@@ -82,8 +82,8 @@ struct Parts<float> {
 };
 
 // NT scales that stand side by side.  As uint16_t they are the bits of bf16 or f16, and which is asked at each, two instructions more: one kernel for both where
-// x is laid out, which the compiler takes a third less time for (65536 x 4096 with 48 rows 50.3 us, with kernels of their own 50.2).  Where x is in LDS
-// from the start each type has its own (one row with 131072 x 4096 43.9 us for 44.6, 5 with 50021 x 2600 17.5 for 18.0).
+// x is laid out, and where W has fewer than 256 blocks, which the compiler takes a third less time for (65536 x 4096 with 48 rows 50.3 us, with kernels of
+// their own 50.2).  With more blocks and x in LDS from the start each type has its own (one row with 131072 x 4096 43.9 us for 44.6, 5 with 50021 x 2600 17.5 for 18.0).
 template <typename S, int NT>
 struct Scales {
     typedef S vec __attribute__((ext_vector_type(NT)));
@@ -238,6 +238,8 @@ __global__ __launch_bounds__(256) void k_operands4(Matvec4Args a) {
 // One row with 131072 x 4096 takes 43.8 us, 6.3 TB/s (loads without products 42.8).  Below some 100 MB it is what comes before the first product and behind the
 // last that counts, 7 to 9 us: 50021 x 2600 with 5 rows 17.5.  65536 x 4096 with 48 rows 47 behind k_operands4's 3.3: LDS, 24 000 of
 // 100 000 cycles, and waits at its barriers.
+// Waves a unit: as many, up to four, as the registers allow without spills.  With two matrix instructions a group and 32-bit scales or 32-bit x it takes 132 to 152 of them, which four
+// waves do not have (16 to 152 bytes a lane would be spilled), x laid out first 136 to 156; x in 32 bits laid out, and more than one tile, up to 256.
 template <typename X, typename S, int G, int NT, int T, bool WHOLE>    // G: matrix instructions between two groups, 1, 2 or 4
 __global__ __launch_bounds__(512, T > 1 || (!WHOLE && sizeof(X) == 4) ? 2 : (WHOLE && (G != 2 || sizeof(S) + sizeof(X) < 6) ? 4 : 3)) void k_matvec4(Matvec4Args a, Shape shape) {
     extern __shared__ char shared[];
@@ -452,6 +454,9 @@ hipError_t matvec4(const Matvec4Args& a, hipStream_t st) {
         // More than one row of x is brought to LDS for two blocks of W at once, where that leaves a workgroup for every compute unit.  us, one / two:
         // 8 rows of bf16 x 65536 x 4096 41 / 32, 16 38.1 / 37.0, 5 of f16 x 50021 x 2600 21.3 / 19.9, 3 of f32 x 32768 x 2048 18.1 / 16.6, but one of
         // bf16 x 131072 x 4096 44.8 / 45.5 and 4 x 16384 x 4096 12.4 / 13.7, which eight waves take in 11.2.
+        // The steps of many blocks are shared by eight waves where a row of x takes more than half of its room, which leaves two workgroups a compute unit, else by
+        // four, of which there are four.  us, four / eight waves: one row of bf16 x 131072 x 4096 44 / 49, x 20600 208 / 209, x 30000 302 / 293, x 40900 409 / 396, of f32 x
+        // 131072 x 6900 90 / 97, x 32800 x 13000 71 / 60.
         const bool many = a.w.blocks() >= 512;
         const int beside = a.tokens > 1 && many ? 2 : 1, share = beside == 1 && (!many || whole > kWholeBytes / 2) ? 8 : 4;
         const bool wide = a.w.blocks() >= 256;

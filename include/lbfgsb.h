@@ -543,7 +543,8 @@ int lbfgsb_pack4(const lbfgsb_weights4* weights_host, void* packed, size_t packe
 
 /* y = x W^T: x is `tokens` rows of weights_host->cols entries of x_type, y as many rows of weights_host->rows entries of y_type
  * (LBFGSB_F32 or x_type), ld_x and ld_y elements apart; rows may start on any element.  packed (16-byte aligned) is what lbfgsb_pack4
- * made of these weights, lbfgsb_packed4_bytes of it (its size is not passed, so nothing here can check it); of the struct the sizes, scale_type and whether zero is NULL are read.  Made for a few tokens: every 64 of them (32 where x is
+ * made of these weights, lbfgsb_packed4_bytes of it (its size is not passed, so nothing here can check it); of the struct the sizes, scale_type and
+ * whether zero is NULL are read.  Made for a few tokens: every 64 of them (32 where x is
  * F32) read the weights once more.  tokens = 0 is allowed.  The workspace goes by lbfgsb_matvec4_workspace_bytes, as for the losses (0 for few and short rows).
  * Products of codes and x are exact (of an x in F32, what lies below 2^-126 may be lost), sums in 32 bits, the result is rounded once.  A zero's part is
  * taken from a group's sum, so the roundings are of sum |scale| (code + |zero|) |x|, not of sum |w| |x|.  y_r is not finite (NaN or infinite) where x_r holds NaN or infinity, or where
@@ -589,8 +590,8 @@ typedef struct {
  *   draft_logp given: q_t(j) = exp(draft_logp_t + (draft_z_tj - draft_z_tx) / draft_temperature).
  * p_t and q_t are off by less than 4e-6 of themselves as well; with draft_logp q_t may be by 2^-24 |draft_logp_t| more.  u_t q_t(x_t) and p_t(x_t) are
  * compared in 64 bits: below 1e-307 they may count as 0.
- * A drafted token outside the vocabulary, and one whose q_t(x_t) is not finite (its own logit or draft_logp infinite or NaN; without draft_logp: NaN or
- * +infinity anywhere in the drafter's row, or -infinity throughout), counts as q_t = 0: it is not accepted and p_t is drawn from.  With draft_logp the
+ * A drafted token outside the vocabulary, and one for which there is no q_t (with draft_logp: that or the token's own logit infinite or NaN; without: NaN or
+ * +infinity anywhere in the drafter's row, or -infinity throughout), counts as q_t = 0 everywhere: it is not accepted and p_t is drawn from.  With draft_logp the
  * drafter's row is read only where its token is not accepted; if that gives a q_t(j) that is NaN or past 2^127, p_t is drawn from.
  * Positions behind a request's length are not read, whatever they hold.
  * tokens, logp: requests x (drafts + 1): what is emitted, accepted tokens and then the drawn one, with the target's log-probabilities;
